@@ -60,7 +60,9 @@ typedef struct {
   int32_t bos, pad, eos, mask;
   int32_t dtype;       /* AD_F32: fp32 weights and arithmetic; AD_BF16: bf16 weights,
                           bf16 GEMM/attention operands, fp32 accumulation, fp32 residual
-                          stream, LayerNorm, softmax and logits                        */
+                          stream, LayerNorm, softmax and logits; AD_BF16_KV_E4M3, AD_BF16_KV_I8:
+                          AD_BF16 with the verifier's key/value caches (the decoder's own and the
+                          encoder memory's) in 8 bits, as ad_kv8_append holds them              */
   int32_t tie_output;  /* 1: the embedding table is also the output projection        */
   int32_t debug_logits;/* 1: keep the last forward's full logits for ad_debug_logits  */
 } ad_config;
@@ -74,7 +76,7 @@ typedef struct {
 } ad_stats;
 
 enum { AD_OK = 0, AD_EINVAL = -1, AD_ESTATE = -2, AD_ENOMEM = -3, AD_EDEVICE = -4 };
-enum { AD_F32 = 0, AD_BF16 = 1 };
+enum { AD_F32 = 0, AD_BF16 = 1, AD_BF16_KV_E4M3 = 2, AD_BF16_KV_I8 = 3 };
 enum { AD_VERIFIER = 0, AD_DRAFTER = 1 };
 
 /* ---- sizes and weight layout (host only, no GPU needed) ------------------------------- */
@@ -289,6 +291,81 @@ int ad_get_option(ad_ctx* ctx, int option, int* value);
  * tau is ignored then.  Costs a second pass of the output projection per call.
  * AD_EINVAL: beta outside [1, vocab], tau negative or not finite. */
 int ad_set_gadpp(ad_ctx* ctx, int32_t beta, float tau);
+
+/* ---- key/value caches in 8 bits ------------------------------------------------------------------
+ * The caches of an AD_BF16_KV_* context, for callers with layers of their own.  A cache is one block of DEVICE memory
+ * of the caller's (ad_kv8_bytes, 256-byte aligned; its contents need no clearing).  Tokens 32 c .. 32 c + 31 of a
+ * sequence are its block c; for every head a block has one scale for its keys and one for its values:
+ *   AD_KV_E4M3  the least power of two u >= 2^-126 with max |x| <= 448 u; a value is the nearest e4m3 number to x / u
+ *               (ties to even) times u
+ *   AD_KV_I8    u = max |x| / 127; a value is the nearest whole number to x / u (ties to even) times u
+ * (u = 1 where all are zero.)  A growing cache (closed = 0) is appended to block after block of rows; a row at position t reads every
+ * block before its own, t / 32, in 8 bits and its own in bf16 up to itself.  So what a row reads depends on the tokens up to it
+ * alone, not on how many came in a call or which were taken back, and its result, bit for bit, on the cache's description and those tokens.
+ * A closed cache (an encoder's memory) is written in one call per sequence and read in 8 bits throughout.
+ * A token with a key or value of a head that is not finite reads as NaN there, and so does its whole block once in 8 bits; rows that
+ * do not see it are not touched by it.
+ *
+ * The calls enqueue kernels on `hip_stream` of the current device and return; they allocate nothing, copy nothing and may be captured
+ * into graphs.  `row_start` [n_seq + 1], `length` [n_seq] and the like are DEVICE arrays here, read when the kernels run: sequence b has
+ * the packed rows row_start[b] .. row_start[b + 1] - 1.  Tables are held to what the host arguments say (`rows` packed rows in all, at
+ * most `max_rows` for a sequence, the capacity): what lies beyond is left out and its outputs are left as they were.
+ * Calls on one cache that overlap in time race unless both only read it. */
+enum { AD_KV_E4M3 = 0, AD_KV_I8 = 1 };
+typedef struct {
+  int32_t n_seq;       /* 1 .. 4096                                                          */
+  int32_t n_heads;     /* heads of the keys and values, 1 .. 256                             */
+  int32_t head_width;  /* 32, 64 or 128                                                      */
+  int32_t capacity;    /* most tokens of a sequence, 1 .. 2^24                               */
+  int32_t k_max;       /* most rows of a sequence in one call, 1 .. 65536 (closed: unused)   */
+  int32_t format;      /* AD_KV_E4M3 or AD_KV_I8                                             */
+  int32_t closed;      /* 0: grows; 1: written at once                                       */
+} ad_kv8_config;
+/* AD_EINVAL with a message in ad_last_error(NULL) for a description outside these limits. */
+int ad_kv8_check(const ad_kv8_config* cfg);
+size_t ad_kv8_bytes(const ad_kv8_config* cfg);   /* 0 if cfg is invalid */
+
+/* Appends keys and values: row i of sequence b becomes token length[b] + i (closed: length[b] must be 0, other sequences are left
+ * as they are).  k, v: bf16 [rows, n_heads, head_width], rows k_stride / v_stride elements apart (multiples of 8; 16-byte aligned).
+ * Taking tokens back is appending behind a smaller length: any since the start of the last append, or a multiple of 32. */
+int ad_kv8_append(const ad_kv8_config* cfg, void* cache, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                  const int32_t* row_start, const int32_t* length, int32_t rows, int32_t max_rows, void* hip_stream);
+/* The values the cache stands for: tokens begin[b] .. of sequence b, as the row at position length[b] reads them, go to packed rows
+ * row_start[b] .. of k_out and v_out, [rows, n_heads, head_width] of `dtype` (AD_F32: exactly, AD_BF16: rounded to nearest; e4m3's are
+ * exact).  Tokens from length[b] on are not there. */
+int ad_kv8_read(const ad_kv8_config* cfg, const void* cache, const int32_t* row_start, const int32_t* begin, const int32_t* length,
+                int32_t rows, int32_t max_rows, int32_t dtype, void* k_out, void* v_out, void* hip_stream);
+/* Attention, softmax(scale q k^T) v over what each row sees.  Growing: the rows at positions length[b] .. (append them first); closed:
+ * every row sees length[b] tokens, a row of an empty memory becomes 0.  q, out: bf16 [rows, q_heads, head_width] with row strides
+ * as above; query heads h * q_heads / n_heads .. share head h.  max_keys: at least the most tokens a row sees (growing: length[b] + rows
+ * of b).  `workspace`: ad_kv8_attend_bytes of device memory that no call overlapping in time uses, 256-byte aligned (null where 0 bytes). */
+size_t ad_kv8_attend_bytes(const ad_kv8_config* cfg, int32_t q_heads, int32_t rows, int32_t max_keys);
+int ad_kv8_attend(const ad_kv8_config* cfg, const void* cache, const void* q, int64_t q_stride, int32_t q_heads,
+                  const int32_t* row_start, const int32_t* length, int32_t rows, int32_t max_rows, int32_t max_keys, float scale,
+                  void* out, int64_t out_stride, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* ---- acceptance of sampled blocks ---------------------------------------------------------------
+ * Verification of drafted tokens where the output is drawn from the model's probabilities instead of being its arg max.  Row i of a
+ * sequence has scores x_i over the vocabulary (what the model says in that place), p_i = softmax(x_i / T), a drafted token d_i and the
+ * drafter's probabilities q_i.  Token d_i stands where accept_u_i q_i(d_i) < p_i(d_i); the first one that does not is replaced by the least t with
+ * r(0) + .. + r(t) > pick_u (r(0) + .. + r(vocab - 1)), r = max(p_i - q_i, 0), and the sequence's block ends there.  With accept_u and pick_u uniform
+ * in [0, 1) the tokens are distributed as drawn from p one by one.  draft_probs = NULL: the drafter is certain of its tokens (q_i = 1 at d_i:
+ * a guide, an arg max).  AD_NEVER, or any id outside the vocabulary, stands for no draft: the row's token is drawn from p_i.
+ * Sums over the vocabulary are kept in 64 bits, so that the same numbers give the same tokens.
+ *   logits       DEVICE, AD_F32 or AD_BF16, [rows, vocab], rows logits_stride elements apart; -inf: never drawn
+ *   draft        DEVICE [rows]: d_i of the packed rows, sequence by sequence (row_start as above)
+ *   draft_probs  DEVICE fp32 [rows, vocab], rows probs_stride apart, or NULL
+ *   temperature  DEVICE [n_seq] T, or NULL (1)
+ *   accept_u     DEVICE [rows]; pick_u: DEVICE [n_seq]
+ *   n_accept     DEVICE [n_seq] out: tokens of the sequence's block, the replacement included
+ *   tokens       DEVICE [rows] out: those tokens, AD_NEVER behind them
+ * A sequence whose next row has no distribution (no finite score, a NaN or +inf among them, T not a positive number) ends before that row.
+ * `workspace`: ad_accept_sampled_bytes of device memory, as ad_kv8_attend's.  Enqueues kernels on `hip_stream`, as the calls above. */
+size_t ad_accept_sampled_bytes(int32_t n_seq, int32_t rows, int32_t vocab);
+int ad_accept_sampled(const void* logits, int32_t dtype, int64_t logits_stride, int32_t vocab, const int32_t* draft,
+                      const float* draft_probs, int64_t probs_stride, const float* temperature, const float* accept_u, const float* pick_u,
+                      const int32_t* row_start, int32_t n_seq, int32_t rows, int32_t max_rows, int32_t* n_accept, int32_t* tokens,
+                      void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /* ---- host-only logic, exposed so that it can be tested without a GPU -------------------------- */
 

@@ -18,7 +18,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libad_mi355x.so")
 
 AD_OK, AD_EINVAL, AD_ESTATE, AD_ENOMEM, AD_EDEVICE = 0, -1, -2, -3, -4
-AD_F32, AD_BF16 = 0, 1
+AD_F32, AD_BF16, AD_BF16_KV_E4M3, AD_BF16_KV_I8 = 0, 1, 2, 3
+AD_KV_E4M3, AD_KV_I8 = 0, 1
 AD_VERIFIER, AD_DRAFTER = 0, 1
 AD_NEVER = -1
 
@@ -28,6 +29,7 @@ EXPORTS = [
     "ad_create", "ad_destroy", "ad_last_error", "ad_encode", "ad_verify", "ad_verify_static", "ad_draft_nat", "ad_output",
     "ad_decode_greedy", "ad_decode_iad", "ad_decode_gad", "ad_debug_logits", "ad_time_verify_forward",
     "ad_suffix_match", "ad_host_simulate", "ad_set_option", "ad_get_option", "ad_calibration_copy", "ad_set_gadpp", "ad_time_output_projection", "ad_calibration_mfma",
+    "ad_kv8_check", "ad_kv8_bytes", "ad_kv8_append", "ad_kv8_read", "ad_kv8_attend_bytes", "ad_kv8_attend", "ad_accept_sampled_bytes", "ad_accept_sampled",
 ]
 AD_OPT_GRAPHS = 3
 AD_OPT_GRAPHS_CAPTURED = 4
@@ -54,6 +56,10 @@ class AdStats(C.Structure):
 
     def as_dict(self):
         return {n: getattr(self, n) for n, _ in self._fields_}
+
+
+class AdKv8Config(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_seq", "n_heads", "head_width", "capacity", "k_max", "format", "closed")]
 
 
 class AdError(RuntimeError):
@@ -118,6 +124,17 @@ def lib():
     L.ad_host_simulate.argtypes = [C.c_int, _I32P, C.c_int, _I32P, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int,
                                    _I32P, _I32P, _I32P, C.c_int, sp]
     L.ad_host_simulate.restype = C.c_int
+    kvp, vp, i32, i64 = C.POINTER(AdKv8Config), C.c_void_p, C.c_int32, C.c_int64
+    L.ad_kv8_check.argtypes = [kvp]; L.ad_kv8_check.restype = C.c_int
+    L.ad_kv8_bytes.argtypes = [kvp]; L.ad_kv8_bytes.restype = C.c_size_t
+    L.ad_kv8_append.argtypes = [kvp, vp, vp, i64, vp, i64, vp, vp, i32, i32, vp]; L.ad_kv8_append.restype = C.c_int
+    L.ad_kv8_read.argtypes = [kvp, vp, vp, vp, vp, i32, i32, i32, vp, vp, vp]; L.ad_kv8_read.restype = C.c_int
+    L.ad_kv8_attend_bytes.argtypes = [kvp, i32, i32, i32]; L.ad_kv8_attend_bytes.restype = C.c_size_t
+    L.ad_kv8_attend.argtypes = [kvp, vp, vp, i64, i32, vp, vp, i32, i32, i32, C.c_float, vp, i64, vp, C.c_size_t, vp]
+    L.ad_kv8_attend.restype = C.c_int
+    L.ad_accept_sampled_bytes.argtypes = [i32, i32, i32]; L.ad_accept_sampled_bytes.restype = C.c_size_t
+    L.ad_accept_sampled.argtypes = [vp, i32, i64, i32, vp, vp, i64, vp, vp, vp, vp, i32, i32, i32, vp, vp, vp, C.c_size_t, vp]
+    L.ad_accept_sampled.restype = C.c_int
     _lib = L
     return L
 

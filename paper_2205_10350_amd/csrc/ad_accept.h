@@ -1,0 +1,30 @@
+// Acceptance of drafted tokens under sampled decoding (ad_accept_sampled.hip).
+#pragma once
+
+#include "ad_internal.h"
+
+namespace ad {
+
+struct AcceptArgs {
+  const void* logits;            // [rows, vocab], rows `stride` elements apart
+  size_t stride;
+  const int* draft;              // [rows]
+  const float* probs;            // [rows, vocab], rows probs_stride apart; null: drafted tokens are certain
+  size_t probs_stride;
+  const float* temperature;      // [n_seq]; null: 1
+  const float *accept_u, *pick_u;   // [rows], [n_seq]
+  const int* row_start;          // [n_seq + 1]
+  int vocab, n_seq, rows, max_rows;
+  int* n_accept;                 // [n_seq], may be null
+  int* tokens;                   // [rows]
+  int keep;                      // 1: rows without a decided token keep what `tokens` holds
+  // the launcher's: per row and piece of the vocabulary, per sequence and piece
+  int pieces;
+  double* piece_sum;
+  float* piece_max;
+  double* rest_sum;
+};
+size_t accept_bytes(int n_seq, int rows, int vocab);
+void launch_accept_sampled(int dtype, AcceptArgs a, void* ws, hipStream_t s);
+
+}  // namespace ad

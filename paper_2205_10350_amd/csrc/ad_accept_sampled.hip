@@ -1,0 +1,399 @@
+// Acceptance of drafted tokens under sampled decoding, from given random numbers.
+//
+// Row i of a sequence has scores x over the vocabulary, p = softmax(x / T), a drafted token d and the drafter's probabilities q (none: all on d).
+// d stands where u_i q(d) < p(d).  The first row i whose token does not stand takes another: r = max(p - q, 0) (a drafter without
+// probabilities: p without d; no token drafted: p), and the token is the least t with r(0) + .. + r(t) > v (r(0) + .. + r(V - 1)).
+// Tokens so accepted are distributed as p.
+//
+// A drawn number may lie next to the border between two tokens, so sums over the vocabulary and what goes into them have 64 bits:
+//   k_accept_stats   a workgroup per 4096 scores of a row: their maximum, and sum of exp2((x - max) log2(e) / T) (without d where q is none).  It reads everything
+//                    once and is bound by that; 64-bit exponentials cost 20 instructions a score.
+//   k_accept_rest    (q given) a workgroup per 4096 scores of each sequence's deciding row: sum of r
+//   k_accept_pick    a workgroup per sequence: the rows' tests, the piece of the deciding row that holds the wanted sum, the token in it
+#include <hip/hip_runtime.h>
+#include <math.h>
+
+#include <algorithm>
+
+#include "ad_accept.h"
+#include "ad_device.h"
+
+namespace ad {
+
+constexpr int kAcceptThreads = 256;
+constexpr int kAcceptPiece = 4096;                                  // scores of a workgroup
+constexpr int kAcceptEach = kAcceptPiece / kAcceptThreads;          // of a thread
+
+// 2^t for t <= 0 (NaN stays): nearest whole number and the Taylor series of 2^f, |f| <= 1/2, to f^11: 7e-15 relative
+__device__ __forceinline__ double exp2_down(double t) {
+  if (t < -1000.0) return 0.0;
+  const double n = rint(t), f = (t - n) * 0.69314718055994530942;
+  double p = 2.50521083854417187751e-8;   // 1 / 11!
+  p = fma(p, f, 2.75573192239858906526e-7);
+  p = fma(p, f, 2.75573192239858906526e-6);
+  p = fma(p, f, 2.48015873015873015873e-5);
+  p = fma(p, f, 1.98412698412698412698e-4);
+  p = fma(p, f, 1.38888888888888888889e-3);
+  p = fma(p, f, 8.33333333333333333333e-3);
+  p = fma(p, f, 4.16666666666666666667e-2);
+  p = fma(p, f, 1.66666666666666666667e-1);
+  p = fma(p, f, 0.5);
+  p = fma(p, f, 1.0);
+  p = fma(p, f, 1.0);
+  return ldexp(p, (int)n);
+}
+__device__ __forceinline__ double wave_sum_f64(double v) {
+#pragma unroll
+  for (int s = 1; s < 64; s *= 2) v += __shfl_xor(v, s);
+  return v;
+}
+
+template <typename T> struct AcceptRow {
+  const T* x;
+  int vocab, skew;   // skew: scores before the first 16-byte boundary
+  static constexpr int kVec = 16 / (int)sizeof(T);
+  __device__ __forceinline__ AcceptRow(const AcceptArgs& a, int row) {
+    x = (const T*)a.logits + (size_t)row * a.stride;
+    vocab = a.vocab;
+    skew = (int)((16 - ((uintptr_t)x & 15)) & 15) / (int)sizeof(T);
+  }
+  __device__ __forceinline__ float at(int i) const { return Store<T>::load(x + i); }
+  // Piece c holds the scores from skew + 4096 c on (and, the first one, the skew's): thread t's element j.
+  __device__ __forceinline__ int index(int c, int t, int j) const { return skew + c * kAcceptPiece + ((j / kVec) * kAcceptThreads + t) * kVec + j % kVec; }
+  __device__ __forceinline__ int heads(int c) const { return c == 0 ? min(skew, vocab) : 0; }
+  // (-inf past the end)
+  __device__ __forceinline__ void load(int c, int t, float (&v)[kAcceptEach]) const {
+#pragma unroll
+    for (int j = 0; j < kAcceptEach; j += kVec) {
+      const int i = index(c, t, j);
+      if (i + kVec <= vocab) {
+        const uint4 w = ldg16(x + i);
+        if constexpr (sizeof(T) == 4) {
+          v[j] = __uint_as_float(w.x); v[j + 1] = __uint_as_float(w.y); v[j + 2] = __uint_as_float(w.z); v[j + 3] = __uint_as_float(w.w);
+        } else {
+          v[j] = __uint_as_float(w.x << 16); v[j + 1] = __uint_as_float(w.x & 0xffff0000u);
+          v[j + 2] = __uint_as_float(w.y << 16); v[j + 3] = __uint_as_float(w.y & 0xffff0000u);
+          v[j + 4] = __uint_as_float(w.z << 16); v[j + 5] = __uint_as_float(w.z & 0xffff0000u);
+          v[j + 6] = __uint_as_float(w.w << 16); v[j + 7] = __uint_as_float(w.w & 0xffff0000u);
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) v[j + e] = i + e < vocab ? at(i + e) : -INFINITY;
+      }
+    }
+  }
+};
+
+struct AcceptSeq { int row0, n; };
+__device__ __forceinline__ AcceptSeq accept_seq(const AcceptArgs& a, int b) {
+  AcceptSeq s;
+  s.row0 = a.row_start[b];
+  s.n = min(min(a.row_start[b + 1] - s.row0, a.max_rows), a.rows - s.row0);
+  if (s.row0 < 0 || s.row0 > a.rows) s.n = 0;
+  return s;
+}
+// log2(e) / T; NaN where T is no positive number
+__device__ __forceinline__ double accept_rate(const AcceptArgs& a, int b) {
+  const float t = a.temperature ? a.temperature[b] : 1.f;
+  return t > 0.f && t < INFINITY ? 1.44269504088896340736 / (double)t : (double)NAN;
+}
+__device__ __forceinline__ bool accept_drafted(const AcceptArgs& a, int d) { return d >= 0 && d < a.vocab; }
+
+template <typename T>
+__global__ __launch_bounds__(kAcceptThreads) void k_accept_stats(AcceptArgs a) {
+  __shared__ float ms[kAcceptThreads / 64];
+  __shared__ double ss[kAcceptThreads / 64];
+  const int c = blockIdx.x, b = blockIdx.z, t = threadIdx.x;
+  const AcceptSeq sq = accept_seq(a, b);
+  if ((int)blockIdx.y >= sq.n) return;
+  const int row = sq.row0 + blockIdx.y;
+  const AcceptRow<T> x(a, row);
+  float v[kAcceptEach];
+  x.load(c, t, v);
+  const float head = t < x.heads(c) ? x.at(t) : -INFINITY;
+  const int skip = a.probs ? -1 : a.draft[row];   // (point mass: summed apart, so that what is left beside it is not a difference)
+  const double rate = accept_rate(a, b);
+  float m = head;
+#pragma unroll
+  for (int j = 0; j < kAcceptEach; ++j) m = fmaxf(m, v[j]);
+  m = wave_max(m);
+  if ((t & 63) == 0) ms[t >> 6] = m;
+  __syncthreads();
+  m = fmaxf(fmaxf(ms[0], ms[1]), fmaxf(ms[2], ms[3]));
+  double s = 0.0;
+  if (m > -INFINITY) {
+#pragma unroll
+    for (int j = 0; j < kAcceptEach; ++j) {
+      const double e = exp2_down(((double)v[j] - (double)m) * rate);
+      s += x.index(c, t, j) == skip ? 0.0 : e;
+    }
+    if (t < x.heads(c) && t != skip) s += exp2_down(((double)head - (double)m) * rate);
+  } else {
+    // nothing but -inf here, or a NaN that the maximum has passed over
+    bool nan = head != head;
+#pragma unroll
+    for (int j = 0; j < kAcceptEach; ++j) nan = nan || v[j] != v[j];
+    if (nan) s = (double)NAN;
+  }
+  s = wave_sum_f64(s);
+  if ((t & 63) == 0) ss[t >> 6] = s;
+  __syncthreads();
+  if (t == 0) {
+    a.piece_sum[(size_t)row * a.pieces + c] = (ss[0] + ss[1]) + (ss[2] + ss[3]);
+    a.piece_max[(size_t)row * a.pieces + c] = m;
+  }
+}
+
+// A row's maximum and the sum over its vocabulary relative to it (without the drafted token: wd), by one wave
+struct AcceptSums { float m; double z, wd; };
+template <typename T> __device__ __forceinline__ AcceptSums accept_sums(const AcceptArgs& a, int row, double rate) {
+  const int lane = threadIdx.x & 63;
+  AcceptSums r;
+  r.m = -INFINITY;
+  for (int c = lane; c < a.pieces; c += 64) r.m = fmaxf(r.m, a.piece_max[(size_t)row * a.pieces + c]);
+  r.m = wave_max(r.m);
+  double z = 0.0;
+  for (int c = lane; c < a.pieces; c += 64) {
+    const float mc = a.piece_max[(size_t)row * a.pieces + c];
+    const double s = a.piece_sum[(size_t)row * a.pieces + c];
+    z += mc > -INFINITY ? s * exp2_down(((double)mc - (double)r.m) * rate) : s;   // (s is 0 there, or NaN)
+  }
+  r.z = wave_sum_f64(z);
+  const int d = a.draft[row];
+  r.wd = 0.0;
+  if (accept_drafted(a, d)) r.wd = exp2_down(((double)AcceptRow<T>(a, row).at(d) - (double)r.m) * rate);
+  if (!a.probs) r.z += r.wd;
+  return r;
+}
+__device__ __forceinline__ bool accept_broken(double z) { return !(z > 0.0 && z < (double)INFINITY); }
+
+// The first row whose drafted token does not stand (n: all do), by the whole workgroup
+template <typename T> __device__ __forceinline__ int accept_first(const AcceptArgs& a, const AcceptSeq& sq, double rate, int* first) {
+  const int wave = threadIdx.x >> 6;
+  if (threadIdx.x == 0) *first = sq.n;
+  __syncthreads();
+  for (int i0 = 0; i0 < sq.n; i0 += kAcceptThreads / 64) {
+    const int i = i0 + wave;
+    if (i < sq.n) {
+      const int row = sq.row0 + i, d = a.draft[row];
+      bool stands = false;
+      if (accept_drafted(a, d)) {
+        const AcceptSums r = accept_sums<T>(a, row, rate);
+        const double q = a.probs ? (double)a.probs[(size_t)row * a.probs_stride + d] : 1.0;
+        stands = !accept_broken(r.z) && (double)a.accept_u[row] * q < r.wd / r.z;
+      }
+      if (!stands && (threadIdx.x & 63) == 0) atomicMin(first, i);
+    }
+    __syncthreads();
+    const int f = *first;
+    __syncthreads();
+    if (f < sq.n) break;
+  }
+  return *first;
+}
+
+// What a token of the deciding row weighs in the draw, relative to the row's maximum (q given: as a probability)
+template <typename T> struct AcceptWeight {
+  const float* q;   // null: none
+  int skip;
+  float m;
+  double rate, inv_z;
+  __device__ __forceinline__ AcceptWeight(const AcceptArgs& a, int row, const AcceptSums& s, double rate_) {
+    const int d = a.draft[row];
+    const bool drafted = accept_drafted(a, d);
+    q = a.probs && drafted ? a.probs + (size_t)row * a.probs_stride : nullptr;
+    skip = !a.probs && drafted ? d : -1;
+    m = s.m; rate = rate_; inv_z = 1.0 / s.z;
+  }
+  __device__ __forceinline__ double operator()(int i, float x) const {
+    const double e = exp2_down(((double)x - (double)m) * rate);
+    if (q) return fmax(e * inv_z - (double)q[i], 0.0);
+    return i == skip ? 0.0 : e;
+  }
+};
+
+template <typename T>
+__global__ __launch_bounds__(kAcceptThreads) void k_accept_rest(AcceptArgs a) {
+  __shared__ int first;
+  __shared__ double ss[kAcceptThreads / 64];
+  const int c = blockIdx.x, b = blockIdx.y, t = threadIdx.x;
+  const AcceptSeq sq = accept_seq(a, b);
+  if (sq.n <= 0) return;
+  const double rate = accept_rate(a, b);
+  const int i = accept_first<T>(a, sq, rate, &first);
+  if (i >= sq.n) return;
+  const int row = sq.row0 + i;
+  const AcceptSums sums = accept_sums<T>(a, row, rate);
+  const AcceptRow<T> x(a, row);
+  const AcceptWeight<T> w(a, row, sums, rate);
+  float v[kAcceptEach];
+  x.load(c, t, v);
+  double s = 0.0;
+#pragma unroll
+  for (int j = 0; j < kAcceptEach; ++j) {
+    const int at = x.index(c, t, j);
+    if (at < a.vocab) s += w(at, v[j]);
+  }
+  if (t < x.heads(c)) s += w(t, x.at(t));
+  s = wave_sum_f64(s);
+  if ((t & 63) == 0) ss[t >> 6] = s;
+  __syncthreads();
+  if (t == 0) a.rest_sum[(size_t)b * a.pieces + c] = (ss[0] + ss[1]) + (ss[2] + ss[3]);
+}
+
+template <typename T>
+__global__ __launch_bounds__(kAcceptThreads) void k_accept_pick(AcceptArgs a) {
+  constexpr int kVec = AcceptRow<T>::kVec, kSlots = kAcceptPiece / kVec, kLaneSlots = kSlots / 64;
+  __shared__ int first, token;
+  __shared__ double slot[kSlots];
+  const int b = blockIdx.x, t = threadIdx.x, lane = t & 63;
+  const AcceptSeq sq = accept_seq(a, b);
+  const double rate = accept_rate(a, b);
+  int i = 0;
+  if (sq.n > 0) {
+    i = accept_first<T>(a, sq, rate, &first);
+    if (t == 0) token = AD_NEVER;
+    __syncthreads();
+  }
+  if (i < sq.n) {
+    const int row = sq.row0 + i;
+    const AcceptSums sums = accept_sums<T>(a, row, rate);
+    if (!accept_broken(sums.z)) {
+      const AcceptRow<T> x(a, row);
+      const AcceptWeight<T> w(a, row, sums, rate);
+      // (the drafted token is left out of the pieces' sums where the drafter gave no probabilities)
+      auto piece = [&](int c) -> double {
+        if (a.probs) return a.rest_sum[(size_t)b * a.pieces + c];
+        const float mc = a.piece_max[(size_t)row * a.pieces + c];
+        return mc > -INFINITY ? a.piece_sum[(size_t)row * a.pieces + c] * exp2_down(((double)mc - (double)sums.m) * rate) : 0.0;
+      };
+      // the piece in which the sum passes the wanted part of the whole: every wave finds it by itself, 64 pieces at a time
+      double total = 0.0;
+      for (int c = lane; c < a.pieces; c += 64) total += piece(c);
+      total = wave_sum_f64(total);
+      if (total > 0.0) {
+        const double want = (double)a.pick_u[b] * total;
+        double before = 0.0, base = 0.0;
+        int at = -1, last = 0;
+        double last_base = 0.0;
+        for (int c0 = 0; c0 < a.pieces && at < 0; c0 += 64) {
+          const double own = c0 + lane < a.pieces ? piece(c0 + lane) : 0.0;
+          double upto = own;
+#pragma unroll
+          for (int s = 1; s < 64; s *= 2) {
+            const double o = __shfl_up(upto, s);
+            if (lane >= s) upto += o;
+          }
+          const unsigned long long some = __ballot(own > 0.0), over = __ballot(before + upto > want) & some;
+          if (over) {
+            const int l = __ffsll(over) - 1;
+            at = c0 + l;
+            base = before + __shfl(upto - own, l);
+          }
+          if (some) {
+            const int l = 63 - __clzll(some);
+            last = c0 + l;
+            last_base = before + __shfl(upto - own, l);
+          }
+          before += __shfl(upto, 63);
+        }
+        if (at < 0) { at = last; base = last_base; }   // (rounding: the last piece that holds anything)
+        // its weights, a slot of kVec scores a sum, in the order of their indices
+        float v[kAcceptEach];
+        x.load(at, t, v);
+#pragma unroll
+        for (int j = 0; j < kAcceptEach; j += kVec) {
+          double s = 0.0;
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) {
+            const int n = x.index(at, t, j + e);
+            if (n < a.vocab) s += w(n, v[j + e]);
+          }
+          slot[(j / kVec) * kAcceptThreads + t] = s;
+        }
+        __syncthreads();
+        if (t < 64) {
+          // the first token whose running sum passes `want`, else the last that weighs anything
+          int hit = -1, heavy = -1;
+          double run = base;
+          for (int n = 0; n < x.heads(at) && hit < 0; ++n) {
+            const double e = w(n, x.at(n));
+            run += e;
+            if (e > 0.0) heavy = n;
+            if (run > want) hit = n;
+          }
+          if (hit < 0) {
+            double own = 0.0;
+            for (int n = 0; n < kLaneSlots; ++n) own += slot[lane * kLaneSlots + n];
+            double upto = own;
+#pragma unroll
+            for (int s = 1; s < 64; s *= 2) {
+              const double o = __shfl_up(upto, s);
+              if (lane >= s) upto += o;
+            }
+            const unsigned long long some = __ballot(own > 0.0), over = __ballot(run + upto > want) & some;
+            if (over || some) {
+              const int l = over ? __ffsll(over) - 1 : 63 - __clzll(some);
+              run += __shfl(upto - own, l);
+              // (the slots of that lane, one by one; the whole wave does the same)
+              int in = -1;
+              double in_run = run;
+              for (int n = l * kLaneSlots; n < (l + 1) * kLaneSlots; ++n) {
+                const double e = slot[n];
+                if (e > 0.0) { in = n; in_run = run; }
+                run += e;
+                if (run > want && e > 0.0) break;
+              }
+              if (in >= 0) {
+                const int n0 = x.skew + at * kAcceptPiece + in * kVec;
+                run = in_run;
+                for (int e = 0; e < kVec && hit < 0 && n0 + e < a.vocab; ++e) {
+                  const double g = w(n0 + e, x.at(n0 + e));
+                  run += g;
+                  if (g > 0.0) {
+                    heavy = n0 + e;
+                    if (run > want) hit = n0 + e;
+                  }
+                }
+              }
+            }
+          }
+          if (lane == 0) token = hit >= 0 ? hit : heavy;
+        }
+      } else {
+        if (t == 0) token = a.draft[row];   // p and q alike: nothing is left over, the drafted token stands
+      }
+    }
+    __syncthreads();
+  }
+  const int tok = sq.n > 0 && i < sq.n ? token : AD_NEVER;
+  for (int n = t; n < sq.n; n += kAcceptThreads) {
+    const int to = n < i ? a.draft[sq.row0 + n] : n == i ? tok : AD_NEVER;
+    if (!a.keep || (n <= i && to >= 0)) a.tokens[sq.row0 + n] = to;
+  }
+  if (t == 0 && a.n_accept) a.n_accept[b] = max(sq.n, 0) == 0 ? 0 : i >= sq.n ? sq.n : tok >= 0 ? i + 1 : i;
+}
+
+int accept_pieces(int vocab) { return (vocab + kAcceptPiece - 1) / kAcceptPiece; }
+static size_t up256(size_t x) { return (x + 255) / 256 * 256; }
+size_t accept_bytes(int n_seq, int rows, int vocab) {
+  const size_t p = accept_pieces(vocab);
+  return up256(rows * p * 8) + up256(rows * p * 4) + up256((size_t)n_seq * p * 8);
+}
+void launch_accept_sampled(int dtype, AcceptArgs a, void* ws, hipStream_t s) {
+  a.pieces = accept_pieces(a.vocab);
+  char* w = (char*)ws;
+  a.piece_sum = (double*)w;
+  a.piece_max = (float*)(w + up256((size_t)a.rows * a.pieces * 8));
+  a.rest_sum = (double*)((char*)a.piece_max + up256((size_t)a.rows * a.pieces * 4));
+  auto go = [&](auto one) {
+    typedef decltype(one) T;
+    k_accept_stats<T><<<dim3(a.pieces, a.max_rows, a.n_seq), kAcceptThreads, 0, s>>>(a);
+    if (a.probs) k_accept_rest<T><<<dim3(a.pieces, a.n_seq), kAcceptThreads, 0, s>>>(a);
+    k_accept_pick<T><<<a.n_seq, kAcceptThreads, 0, s>>>(a);
+  };
+  if (dtype == AD_BF16) go(bf16_t{});
+  else go(float{});
+}
+
+}  // namespace ad

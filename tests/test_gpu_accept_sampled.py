@@ -1,0 +1,191 @@
+"""Acceptance of sampled blocks through the public entry point, against the plain 64-bit form.  Tokens are whole numbers: they have to be equal
+(a drawn number within 1e-12 of a border between two tokens, where 64 bits may fall either way, does not occur in these draws)."""
+import numpy as np
+import pytest
+
+import paper_2205_10350_amd as ad
+from kv8_reference import accept
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+NAN, INF = float("nan"), float("inf")
+
+
+def i32(x):
+    return torch.tensor(np.asarray(x, np.int32), device="cuda")
+
+
+def f32(x):
+    return torch.tensor(np.asarray(x, np.float32), device="cuda")
+
+
+def problem(seed, rows, vocab, probs, bf16=False, width=3.0):
+    rng = np.random.default_rng(seed)
+    n = sum(rows)
+    x = torch.tensor(rng.standard_normal((n, vocab)) * width, dtype=torch.float32)
+    if bf16:
+        x = x.to(torch.bfloat16)
+    q = torch.softmax(x.float() + 0.5 * torch.tensor(rng.standard_normal((n, vocab)), dtype=torch.float32), -1) if probs else None
+    d = np.array([rng.choice(vocab, p=(q[i] if probs else torch.softmax(x[i].float(), -1)).double().numpy() / float((q[i] if probs else torch.softmax(x[i].float(), -1)).double().sum()))
+                  for i in range(n)], np.int32)
+    return dict(x=x, q=q, d=d, u=rng.random(n).astype(np.float32) * (1.0 if probs else 0.5 / vocab ** 0.5), v=rng.random(len(rows)).astype(np.float32),
+                t=(0.5 + rng.random(len(rows))).astype(np.float32))
+
+
+def run(p, rows, **more):
+    start = i32(np.concatenate(([0], np.cumsum(rows))))
+    n, tok = ad.accept_sampled(p["x"].cuda(), i32(p["d"]), start, f32(p["u"]), f32(p["v"]), temperature=f32(p["t"]),
+                               draft_probs=None if p["q"] is None else p["q"].cuda(), **more)
+    return n.cpu().tolist(), tok.cpu().tolist()
+
+
+def check(p, rows, got):
+    at, (n, tok) = 0, got
+    for b, m in enumerate(rows):
+        s = slice(at, at + m)
+        want = accept(p["x"][s].float().numpy(), p["d"][s], None if p["q"] is None else p["q"][s].numpy(), p["t"][b], p["u"][s], p["v"][b])
+        assert n[b] == len(want) and tok[s] == want + [ad.AD_NEVER] * (m - len(want)), (b, n[b], tok[s], want)
+        at += m
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("probs", [False, True])
+@pytest.mark.parametrize("vocab", [1, 2, 7, 9, 257, 4095, 4096, 4097, 4104, 12301])
+def test_accepted_tokens(vocab, probs, bf16):
+    rows = [1, 0, 5, 3, 8, 1, 2, 0, 6]
+    for seed in range(3):
+        p = problem(100 * vocab + seed, rows, vocab, probs, bf16)
+        check(p, rows, run(p, rows))
+        assert run(p, rows) == run(p, rows, max_rows=8)
+
+
+@pytest.mark.parametrize("probs", [False, True])
+def test_a_large_vocabulary_of_more_than_64_pieces(probs):
+    rows = [3, 2]
+    for seed in range(4):
+        p = problem(seed, rows, 300007, probs, bf16=seed % 2 == 1, width=1.0)
+        check(p, rows, run(p, rows))
+
+
+@pytest.mark.parametrize("skew", range(8))
+@pytest.mark.parametrize("bf16", [False, True])
+def test_rows_at_every_alignment(skew, bf16):
+    """Rows out of a wider tensor, from any 2- or 4-byte boundary on."""
+    rows, vocab = [4, 3], 4100
+    p = problem(skew, rows, vocab, False, bf16)
+    wide = torch.full((sum(rows), vocab + 13), NAN, dtype=p["x"].dtype)
+    wide[:, skew:skew + vocab] = p["x"]
+    want = run(p, rows)
+    p["x"] = wide.cuda()[:, skew:skew + vocab]
+    assert run(p, rows) == want
+
+
+def test_random_numbers_at_their_ends():
+    rows, vocab = [4] * 6, 1000
+    p = problem(5, rows, vocab, False)
+    last = np.float32(1) - np.float32(2) ** -24
+    for u, v in ((0.0, 0.0), (last, 0.0), (last, last), (0.0, last)):
+        p["u"][:] = u
+        p["v"][:] = v
+        got = run(p, rows)
+        check(p, rows, got)
+        assert got[0] == [4 if u == 0 else 1] * 6
+
+
+def test_no_draft_draws_from_the_model():
+    rows, vocab = [3, 1, 2], 500
+    for probs in (False, True):
+        p = problem(6, rows, vocab, probs)
+        p["d"][[2, 3, 4]] = [ad.AD_NEVER, vocab, -7]
+        p["u"][:] = 0
+        got = run(p, rows)
+        check(p, rows, got)
+        assert got[0] == [3, 1, 1]
+
+
+def test_masked_scores_are_never_drawn():
+    rows, vocab = [1] * 200, 60
+    for probs in (False, True):
+        p = problem(7, rows, vocab, probs)
+        allowed = np.zeros(vocab, bool)
+        allowed[[3, 30, 59]] = True
+        p["x"][:, ~allowed] = -INF
+        p["u"][:] = 0.999
+        got = run(p, rows)
+        check(p, rows, got)
+        assert all(allowed[t] for t in got[1])
+        # the lowest score of the type is a score: it weighs nothing beside others, everything alone
+        p["x"][:, ~allowed] = torch.finfo(torch.float32).min
+        check(p, rows, run(p, rows))
+
+
+def test_a_block_ends_before_a_row_without_a_distribution():
+    rows, vocab = [3] * 6, 5000
+    p = problem(8, rows, vocab, False)
+    p["u"][:] = 0
+    p["x"][1] = -INF                  # sequence 0, row 1: no finite score
+    p["x"][3 + 2, 4999] = NAN         # sequence 1, row 2
+    p["x"][6, 17] = INF               # sequence 2, row 0
+    p["t"][3], p["t"][4] = 0.0, NAN
+    got = run(p, rows)
+    check(p, rows, got)
+    assert got[0] == [1, 2, 0, 0, 0, 3]
+    p["t"][:] = [-1, INF, 1, 1, 1, 1]
+    p["d"][:] = ad.AD_NEVER
+    got = run(p, rows)
+    check(p, rows, got)
+    assert got[0] == [0, 0, 0, 1, 1, 1]
+
+
+def test_a_drafter_that_says_what_the_model_says():
+    """q = p up to rounding: hardly anything is rejected, and what is leaves next to nothing over."""
+    rows, vocab = [40] * 8, 300
+    p = problem(9, rows, vocab, True)
+    p["t"][:] = 1
+    p["q"] = torch.softmax(p["x"].double(), -1).float()
+    got = run(p, rows)
+    check(p, rows, got)
+    assert sum(got[0]) >= 300
+
+
+def test_tokens_are_distributed_as_the_model_says():
+    """4,000 draws of one row: drafted from q and verified, they follow p.  A count of mean n p has a standard deviation below sqrt(n p): five of them."""
+    n, vocab = 4000, 12
+    rng = np.random.default_rng(10)
+    x = rng.standard_normal(vocab).astype(np.float32)
+    q = rng.dirichlet(np.ones(vocab)).astype(np.float32)
+    p = np.exp(x.astype(np.float64))
+    p /= p.sum()
+    rows = [1] * n
+    for probs in (True, False):
+        d = rng.choice(vocab, size=n, p=q.astype(np.float64) / q.astype(np.float64).sum()) if probs else np.full(n, 4)
+        got = run(dict(x=torch.tensor(x).expand(n, vocab).contiguous(), q=torch.tensor(q).expand(n, vocab).contiguous() if probs else None, d=d,
+                       u=rng.random(n).astype(np.float32), v=rng.random(n).astype(np.float32), t=np.ones(n, np.float32)), rows)[1]
+        count = np.bincount(got, minlength=vocab)
+        assert np.all(np.abs(count - n * p) <= 5 * np.sqrt(n * p) + 1), (count, n * p)
+
+
+def test_captured_and_replayed():
+    rows, vocab = [5, 2, 4], 6000
+    p = problem(11, rows, vocab, True)
+    x, q, d = p["x"].cuda(), p["q"].cuda(), i32(p["d"])
+    start, u, v = i32([0, 5, 7, 11]), f32(p["u"]), f32(p["v"])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        ad.accept_sampled(x, d, start, u, v, draft_probs=q, max_rows=5)
+    torch.cuda.current_stream().wait_stream(side)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = ad.accept_sampled(x, d, start, u, v, draft_probs=q, max_rows=5)
+    for seed in range(4):
+        r = problem(20 + seed, rows, vocab, True)
+        for to, key in ((x, "x"), (q, "q")):
+            to.copy_(r[key])
+        d.copy_(i32(r["d"])); u.copy_(f32(r["u"])); v.copy_(f32(r["v"]))
+        g.replay()
+        want = ad.accept_sampled(x, d, start, u, v, draft_probs=q, max_rows=5)
+        assert all(torch.equal(a, b) for a, b in zip(out, want))
+        r["t"][:] = 1
+        check(r, rows, (out[0].cpu().tolist(), out[1].cpu().tolist()))
