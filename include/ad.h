@@ -62,7 +62,9 @@ typedef struct {
                           bf16 GEMM/attention operands, fp32 accumulation, fp32 residual
                           stream, LayerNorm, softmax and logits; AD_BF16_KV_E4M3, AD_BF16_KV_I8:
                           AD_BF16 with the verifier's key/value caches (the decoder's own and the
-                          encoder memory's) in 8 bits, as ad_kv8_append holds them              */
+                          encoder memory's) in 8 bits, as ad_kv8_append holds them: head size
+                          32, 64 or 128; without a drafter max_len + k_max may exceed what
+                          attention over bf16 rows takes                               */
   int32_t tie_output;  /* 1: the embedding table is also the output projection        */
   int32_t debug_logits;/* 1: keep the last forward's full logits for ad_debug_logits  */
 } ad_config;
@@ -164,6 +166,15 @@ int ad_verify(ad_ctx* ctx, const int32_t* draft, const int32_t* k,
  * obtained on this device. */
 int ad_verify_static(ad_ctx* ctx, const int32_t* draft, const int32_t* k,
                      int32_t* n_accept, int32_t* next_token, int32_t* verified);
+
+/* ad_verify for sampled decoding: same block, same effect on the decode state, but a drafted token stands, and the token in the place of the
+ * first that does not is drawn, as ad_accept_sampled says (draft_probs = NULL: drafted tokens are certain, as a guide's or the block
+ * drafter's are), from the given random numbers.  So outputs are distributed as sampled from the model token by token, at
+ * temperature[b] (HOST [B], positive and finite; NULL: 1).  accept_u HOST [B, k_max] as draft, pick_u HOST [B]: in [0, 1).
+ * verified[b][i]: the accepted tokens, the drawn one, and behind it the rows' arg maxima.  AD_NEVER as the last draft draws that row's token.
+ * Needs cfg.debug_logits (AD_ESTATE otherwise: the scores it draws from are kept in the workspace) and beta = 1 (ad_set_gadpp). */
+int ad_verify_sampled(ad_ctx* ctx, const int32_t* draft, const int32_t* k, const float* accept_u, const float* pick_u,
+                      const float* temperature, int32_t* n_accept, int32_t* next_token, int32_t* verified);
 
 /* Block drafter (Section 3.2, draft paragraph; Section 3.2.1): decoder input
  * (o_0..o_j, [MASK] x k) at positions 0..j+k with bidirectional self-attention and

@@ -26,7 +26,7 @@ AD_NEVER = -1
 EXPORTS = [
     "ad_config_check", "ad_workspace_bytes", "ad_weights_count", "ad_weights_bytes", "ad_weights_entry",
     "ad_weights_pack",
-    "ad_create", "ad_destroy", "ad_last_error", "ad_encode", "ad_verify", "ad_verify_static", "ad_draft_nat", "ad_output",
+    "ad_create", "ad_destroy", "ad_last_error", "ad_encode", "ad_verify", "ad_verify_static", "ad_verify_sampled", "ad_draft_nat", "ad_output",
     "ad_decode_greedy", "ad_decode_iad", "ad_decode_gad", "ad_debug_logits", "ad_time_verify_forward",
     "ad_suffix_match", "ad_host_simulate", "ad_set_option", "ad_get_option", "ad_calibration_copy", "ad_set_gadpp", "ad_time_output_projection", "ad_calibration_mfma",
     "ad_kv8_check", "ad_kv8_bytes", "ad_kv8_append", "ad_kv8_read", "ad_kv8_attend_bytes", "ad_kv8_attend", "ad_accept_sampled_bytes", "ad_accept_sampled",
@@ -96,6 +96,8 @@ def lib():
     L.ad_encode.argtypes = [C.c_void_p, C.c_int, _I32P, _I32P, C.c_int, _I32P]; L.ad_encode.restype = C.c_int
     L.ad_verify.argtypes = [C.c_void_p, _I32P, _I32P, _I32P, _I32P, _I32P]; L.ad_verify.restype = C.c_int
     L.ad_verify_static.argtypes = [C.c_void_p, _I32P, _I32P, _I32P, _I32P, _I32P]; L.ad_verify_static.restype = C.c_int
+    fp = C.POINTER(C.c_float)
+    L.ad_verify_sampled.argtypes = [C.c_void_p, _I32P, _I32P, fp, fp, fp, _I32P, _I32P, _I32P]; L.ad_verify_sampled.restype = C.c_int
     L.ad_draft_nat.argtypes = [C.c_void_p, C.c_int, _I32P]; L.ad_draft_nat.restype = C.c_int
     L.ad_output.argtypes = [C.c_void_p, _I32P, _I32P]; L.ad_output.restype = C.c_int
     sp = C.POINTER(AdStats)
@@ -152,11 +154,14 @@ def _check(rc, ctx=None):
         raise AdError(rc, (lib().ad_last_error(ctx) or b"").decode())
 
 
+_DTYPES = {"bf16": AD_BF16, "fp32": AD_F32, "bf16_kv_e4m3": AD_BF16_KV_E4M3, "bf16_kv_i8": AD_BF16_KV_I8}
+
+
 def make_config(dims: dict, *, max_batch, max_src, max_len, k_max, dtype, special, tie_output=False,
                 debug_logits=False) -> AdConfig:
     return AdConfig(dims["enc_layers"], dims["dec_layers"], dims["d_model"], dims["n_heads"], dims["d_ffn"],
                     dims["vocab"], max_batch, max_src, max_len, k_max, special["bos"], special["pad"],
-                    special["eos"], special["mask"], AD_BF16 if dtype == "bf16" else AD_F32,
+                    special["eos"], special["mask"], _DTYPES.get(dtype, AD_F32),
                     int(tie_output), int(debug_logits))
 
 
@@ -335,6 +340,27 @@ class Context:
         ver = np.zeros((self.B, km), dtype=np.int32) if want_verified else None
         fn = self.L.ad_verify_static if static else self.L.ad_verify
         _check(fn(self.h, _p(d), _p(k), _p(n), _p(nx), _p(ver)), self.h)
+        return (n, nx, ver) if want_verified else (n, nx)
+
+    def verify_sampled(self, drafts, accept_u, pick_u, temperature=None, want_verified=False):
+        """verify() for sampled decoding (ad_verify_sampled).  accept_u: one number in [0, 1) per drafted token, as the drafts; pick_u: one per
+        sequence; temperature: per sequence, or one for all, or None (1)."""
+        km = self.cfg.k_max
+        d, k = self._pad_rows(drafts, km)
+        u = np.zeros((self.B, km), dtype=np.float32)
+        if len(accept_u) != len(drafts) or any(len(a) < len(b) for a, b in zip(accept_u, drafts)):
+            raise AdError(AD_EINVAL, "accept_u needs a number for every drafted token")
+        for b, a in enumerate(accept_u[:self.B]):
+            a = np.asarray(a, dtype=np.float32)[:km]
+            u[b, :len(a)] = a
+        v = np.ascontiguousarray(pick_u, dtype=np.float32)
+        t = None if temperature is None else np.ascontiguousarray(np.broadcast_to(np.asarray(temperature, dtype=np.float32), (self.B,)))
+        if len(drafts) != self.B or v.shape != (self.B,):
+            raise AdError(AD_EINVAL, "one draft and one pick_u per sequence of the batch")
+        n = np.zeros(self.B, dtype=np.int32); nx = np.zeros(self.B, dtype=np.int32)
+        ver = np.zeros((self.B, km), dtype=np.int32) if want_verified else None
+        f = lambda a: None if a is None else a.ctypes.data_as(C.POINTER(C.c_float))
+        _check(self.L.ad_verify_sampled(self.h, _p(d), _p(k), f(u), f(v), f(t), _p(n), _p(nx), _p(ver)), self.h)
         return (n, nx, ver) if want_verified else (n, nx)
 
     def draft_nat(self, k):

@@ -24,6 +24,10 @@ struct AcceptArgs {
   float* piece_max;
   double* rest_sum;
 };
+// The inputs of a verify call, host-visible and by sequence, as packed rows in device memory: draft, u [n_seq, k_max], v, t [n_seq] -> rows of
+// row_start (draft_out, u_out) and copies (v_out, t_out)
+void launch_accept_inputs(const int* draft, const float* u, const float* v, const float* t, int k_max, const int* row_start, int n_seq, int* draft_out,
+                          float* u_out, float* v_out, float* t_out, hipStream_t s);
 size_t accept_bytes(int n_seq, int rows, int vocab);
 void launch_accept_sampled(int dtype, AcceptArgs a, void* ws, hipStream_t s);
 

@@ -374,6 +374,21 @@ __global__ __launch_bounds__(kAcceptThreads) void k_accept_pick(AcceptArgs a) {
   if (t == 0 && a.n_accept) a.n_accept[b] = max(sq.n, 0) == 0 ? 0 : i >= sq.n ? sq.n : tok >= 0 ? i + 1 : i;
 }
 
+__global__ __launch_bounds__(64) void k_accept_inputs(const int* __restrict__ draft, const float* __restrict__ u, const float* __restrict__ v,
+                                                      const float* __restrict__ t, int k_max, const int* __restrict__ row_start, int* __restrict__ draft_out,
+                                                      float* __restrict__ u_out, float* __restrict__ v_out, float* __restrict__ t_out) {
+  const int b = blockIdx.x, r0 = row_start[b], n = min(row_start[b + 1] - r0, k_max);
+  for (int i = threadIdx.x; i < n; i += 64) {
+    draft_out[r0 + i] = draft[(size_t)b * k_max + i];
+    u_out[r0 + i] = u[(size_t)b * k_max + i];
+  }
+  if (threadIdx.x == 0) { v_out[b] = v[b]; t_out[b] = t[b]; }
+}
+void launch_accept_inputs(const int* draft, const float* u, const float* v, const float* t, int k_max, const int* row_start, int n_seq, int* draft_out,
+                          float* u_out, float* v_out, float* t_out, hipStream_t s) {
+  k_accept_inputs<<<n_seq, 64, 0, s>>>(draft, u, v, t, k_max, row_start, draft_out, u_out, v_out, t_out);
+}
+
 int accept_pieces(int vocab) { return (vocab + kAcceptPiece - 1) / kAcceptPiece; }
 static size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 size_t accept_bytes(int n_seq, int rows, int vocab) {

@@ -13,7 +13,9 @@
 #include <utility>
 #include <vector>
 
+#include "ad_accept.h"
 #include "ad_internal.h"
+#include "ad_kv8.h"
 #include "ad_team.h"
 
 namespace ad {
@@ -51,13 +53,19 @@ struct Plan {
   size_t cache_k, cache_v, cache_layer_stride;          // [NL][B*l_cap, d]
   size_t mem_k[2], mem_v[2], mem_layer_stride;          // per model: [NL][B*max_src, d]
   size_t row_tok, row_pos, row_seq, row_dst, row_dst2, row_start, self_desc, cross_desc;
+  // caches in 8 bits (kv8): per decoder layer one of the decoder's own and one of the verifier's memory; identity row table; attention's workspace
+  bool kv8 = false;
+  Kv8Dims kv8_self{}, kv8_mem{};
+  size_t kv8_self_at, kv8_mem_at, kv8_self_stride, kv8_mem_stride, row_id, kv8_ws;
+  size_t sd_draft, sd_u, sd_v, sd_t, sd_ws, sd_host;    // sampled acceptance: packed inputs, its workspace, the inputs' copy where they are not mapped
   size_t team_words[3];                                 // barrier state of the team launches: the encoders' (per model), the decoders'
   size_t len, pending, finished, max_out, src_len[2], out, result, k_dev, draft_dev, src_dev, draft_out;
 };
 
 static Plan make_plan(const ad_config& c, bool with_drafter) {
   Plan p;
-  p.esz = c.dtype == AD_BF16 ? 2 : 4;
+  p.esz = bf16_dtype(c.dtype) ? 2 : 4;
+  p.kv8 = kv8_dtype(c.dtype);
   const size_t B = c.max_batch, d = c.d_model;
   p.l_cap = c.max_len + c.k_max;
   p.mv_cap = (int)(B * c.k_max);
@@ -80,7 +88,7 @@ static Plan make_plan(const ad_config& c, bool with_drafter) {
   p.f = take(m * (size_t)c.d_ffn * p.esz);
   // what a team launch passes on: inside a layer, from layer to layer, keys and values that have no place in a cache
   const bool team32 = c.dtype == AD_F32 && team_f32_widths((int)d, c.n_heads, c.d_ffn);
-  const size_t team_layers = team32 || (c.dtype == AD_BF16 && d == kTeamD && c.d_ffn == kTeamF) ? std::max(c.enc_layers, c.dec_layers) : 0;
+  const size_t team_layers = team32 || (bf16_dtype(c.dtype) && d == kTeamD && c.d_ffn == kTeamF) ? std::max(c.enc_layers, c.dec_layers) : 0;
   p.team_slots = take(team32 ? team_layers * 8 * team_f32_slot_bytes((int)d) : team_layers ? 8 * TeamSlot::kBytes : 0);
   p.team_hop = take(team_layers * kTeamHopBytes);
   p.team_kv_stride = team32 ? kTeamXRows * d * 4 : kTeamKvBytes;
@@ -104,14 +112,30 @@ static Plan make_plan(const ad_config& c, bool with_drafter) {
   p.draft_lp = take((size_t)p.mv_cap * 4);
   p.draft_col = take((size_t)p.mv_cap * 4);
   p.logits = take(c.debug_logits ? (size_t)p.mv_cap * c.vocab * 4 : 0);
-  p.cache_layer_stride = align_up(B * p.l_cap * d * p.esz);
+  if (c.debug_logits) {
+    p.sd_draft = take((size_t)p.mv_cap * 4); p.sd_u = take((size_t)p.mv_cap * 4); p.sd_v = take(B * 4); p.sd_t = take(B * 4);
+    p.sd_ws = take(accept_bytes((int)B, p.mv_cap, c.vocab));
+    p.sd_host = take((B * c.k_max + 2 * B) * 4);
+  }
+  if (p.kv8) {
+    const int dh = c.d_model / c.n_heads, fmt = kv8_format(c.dtype);
+    p.kv8_self = kv8_dims(ad_kv8_config{c.max_batch, c.n_heads, dh, p.l_cap, c.k_max, fmt, 0});
+    p.kv8_mem = kv8_dims(ad_kv8_config{c.max_batch, c.n_heads, dh, c.max_src, 1, fmt, 1});
+    p.kv8_self_stride = align_up(p.kv8_self.bytes); p.kv8_mem_stride = align_up(p.kv8_mem.bytes);
+    p.kv8_self_at = take(p.kv8_self_stride * c.dec_layers);
+    p.kv8_mem_at = take(p.kv8_mem_stride * c.dec_layers);
+    p.row_id = take(m * 4);
+    p.kv8_ws = take(std::max(kv8_attend_bytes(p.kv8_self, c.n_heads, p.mv_cap, p.l_cap), kv8_attend_bytes(p.kv8_mem, c.n_heads, p.mv_cap, c.max_src)));
+  }
+  p.cache_layer_stride = p.kv8 ? 0 : align_up(B * p.l_cap * d * p.esz);
   p.cache_k = take(p.cache_layer_stride * c.dec_layers);
   p.cache_v = take(p.cache_layer_stride * c.dec_layers);
   p.mem_layer_stride = align_up(B * c.max_src * d * p.esz);
   for (int i = 0; i < 2; ++i) {
     const bool on = i == 0 || with_drafter;
-    p.mem_k[i] = take(on ? p.mem_layer_stride * c.dec_layers : 0);
-    p.mem_v[i] = take(on ? p.mem_layer_stride * c.dec_layers : 0);
+    const bool rows = on && !(i == 0 && p.kv8);   // (the drafter's memory stays in rows of bf16)
+    p.mem_k[i] = take(rows ? p.mem_layer_stride * c.dec_layers : 0);
+    p.mem_v[i] = take(rows ? p.mem_layer_stride * c.dec_layers : 0);
     p.src_len[i] = take(B * 4);
     p.kv_w[i] = take(on ? (size_t)c.dec_layers * 2 * d * d * p.esz : 0);
     p.kv_b[i] = take(on ? (size_t)c.dec_layers * 2 * d * 4 : 0);
@@ -139,6 +163,7 @@ struct PinLayout {
   size_t d_copy;                      // ad_draft_nat without the watch: draft_out[B, k_max]
   size_t enc[2];                      // ad_encode per model: src_len[B], max_out[B], src[B, max_src]
   size_t out;                         // ad_output: out[B, max_len]
+  size_t s_in;                        // ad_verify_sampled: accept_u[B, k_max], pick_u[B], temperature[B] (floats)
   size_t team_fail;                   // a team launch's fail word on its way to the host
   size_t total;
 };
@@ -154,6 +179,7 @@ static PinLayout make_pin_layout(const ad_config& c, const Plan& p) {
   l.d_copy = take(B * c.k_max);
   for (int i = 0; i < 2; ++i) l.enc[i] = take(B * (2 + (size_t)c.max_src));
   l.out = take(B * c.max_len);
+  l.s_in = take(c.debug_logits ? B * c.k_max + 2 * B : 0);
   l.team_fail = take(4);
   l.total = off;
   return l;
@@ -507,11 +533,33 @@ static void ffn_block(ad_ctx* c, const FfnW& f, const LnW& ln, int M) {
 // head_rows > 0: from the attention on, only the first head_rows packed rows are needed (they are
 // the queries of the first head_nseq descriptors, at most head_max_rows each): keys and values are
 // still projected from all M rows.
+// kv8: the layer's cache in 8 bits instead (Kl, Vl unused): rows to the packed temporaries, appended from there, and attended to.
+static Kv8Rows kv8_rows(const ad_ctx* c, const SeqDesc* desc, int M) {
+  static_assert(sizeof(SeqDesc) == 8 * sizeof(int), "the tables are read as ints");
+  return Kv8Rows{&desc->q_row0, &desc->nq, &desc->nk_base, 8, M, c->fw_max_rows, c->fw_nseq};
+}
+// Most keys a launch over a cache is made for: the next power of two from 256 on (part of a call shape's graph key).  Results do not depend on it.
+static int kv8_key_bound(int keys, int capacity) {
+  int n = 256;
+  while (n < keys) n *= 2;
+  return keys > 0 ? std::min(n, capacity) : capacity;
+}
 static void self_attn_block(ad_ctx* c, const AttnW& a, const LnW& ln, int M, void* Kl, void* Vl, int max_keys,
-                            int head_rows = 0, int head_nseq = 0, int head_max_rows = 0) {
+                            int head_rows = 0, int head_nseq = 0, int head_max_rows = 0, void* kv8 = nullptr) {
   const Plan& p = c->plan;
   const int d = c->cfg.d_model, H = c->cfg.n_heads;
   VerifyTables t = tables(c);
+  if (kv8) {
+    Epi e{};
+    e.mode = EPI_QKV; e.d = d; e.bias = a.bqkv; e.out0 = c->at<void>(p.q); e.out1 = c->at<void>(p.tk); e.out2 = c->at<void>(p.tv); e.row_dst = c->at<int>(p.row_id);
+    gemm_rows(c, a.wqkv, M, 3 * d, e);
+    const Kv8Rows rows = kv8_rows(c, t.self_desc, M);
+    launch_kv8_append(p.kv8_self, kv8, c->at<void>(p.tk), c->at<void>(p.tv), d, d, rows, c->stream);
+    launch_kv8_attend(p.kv8_self, kv8, c->at<void>(p.q), d, c->at<void>(p.att), d, H, rows, kv8_key_bound(c->fw_self_keys, p.l_cap),
+                      1.0f / sqrtf((float)(d / H)), c->at<void>(p.kv8_ws), c->stream);
+    gemm_resid_ln(c, c->at<void>(p.att), a.wo, a.bo, M, d, d, ln);
+    return;
+  }
   Epi e{};
   e.mode = EPI_QKV; e.d = d; e.bias = a.bqkv; e.out0 = c->at<void>(p.q); e.out1 = Kl; e.out2 = Vl; e.row_dst = t.row_dst;
   gemm_rows(c, a.wqkv, M, 3 * d, e);
@@ -523,10 +571,19 @@ static void self_attn_block(ad_ctx* c, const AttnW& a, const LnW& ln, int M, voi
   gemm_resid_ln(c, c->at<void>(p.att), a.wo, a.bo, M, d, d, ln);
 }
 
-static void cross_attn_block(ad_ctx* c, const AttnW& a, const LnW& ln, int M, const void* Km, const void* Vm) {
+static void cross_attn_block(ad_ctx* c, const AttnW& a, const LnW& ln, int M, const void* Km, const void* Vm, const void* kv8 = nullptr) {
   const Plan& p = c->plan;
   const int d = c->cfg.d_model, H = c->cfg.n_heads;
   VerifyTables t = tables(c);
+  if (kv8) {   // the layer's memory in 8 bits instead of (Km, Vm)
+    Epi e{};
+    e.mode = EPI_STORE; e.bias = a.bqkv; e.out0 = c->at<void>(p.q);
+    gemm_rows(c, a.wqkv, M, d, e);
+    launch_kv8_attend(p.kv8_mem, kv8, c->at<void>(p.q), d, c->at<void>(p.att), d, H, kv8_rows(c, t.cross_desc, M), kv8_key_bound(c->fw_cross_keys, c->cfg.max_src),
+                      1.0f / sqrtf((float)(d / H)), c->at<void>(p.kv8_ws), c->stream);
+    gemm_resid_ln(c, c->at<void>(p.att), a.wo, a.bo, M, d, d, ln);
+    return;
+  }
   // query projection (with the pending LayerNorm) and attention in one launch where the shape allows
   LnA la{};
   if (c->ln_pending) {
@@ -596,9 +653,9 @@ static int verify_forward(ad_ctx* c, int M, hipEvent_t ev_a = nullptr, hipEvent_
   } else for (int l = 0; l < c->cfg.dec_layers; ++l) {
     const DecLayerW& L = w.dec[l];
     self_attn_block(c, L.self, L.ln1, M, c->ws + p.cache_k + l * p.cache_layer_stride,
-                    c->ws + p.cache_v + l * p.cache_layer_stride, p.l_cap);
+                    c->ws + p.cache_v + l * p.cache_layer_stride, p.l_cap, 0, 0, 0, p.kv8 ? c->ws + p.kv8_self_at + l * p.kv8_self_stride : nullptr);
     cross_attn_block(c, L.cross, L.ln2, M, c->ws + p.mem_k[0] + l * p.mem_layer_stride,
-                     c->ws + p.mem_v[0] + l * p.mem_layer_stride);
+                     c->ws + p.mem_v[0] + l * p.mem_layer_stride, p.kv8 ? c->ws + p.kv8_mem_at + l * p.kv8_mem_stride : nullptr);
     ffn_block(c, L.ffn, L.ln3, M);
   }
   if (plain_rows) flush_ln(c, M);
@@ -650,13 +707,20 @@ static void write_out(ad_ctx* c, const LoopIO& io, int32_t* out, int32_t* out_le
   if (stats) { *stats = io.stats; stats->t_encode_us = t_enc; }
 }
 
+// a drafter attends over its prefix and masks as rows, whatever the verifier's caches are
+static int drafter_check(const ad_config& c, bool with_drafter) {
+  if (with_drafter && kv8_dtype(c.dtype) && !attention_keys_fit(c, c.max_len + c.k_max))
+    return fail(nullptr, AD_EINVAL, "max_len + k_max too large for a drafter: a head's keys and values must fit in 160 KB of LDS");
+  return AD_OK;
+}
+
 // =================================================================================================
 extern "C" {
 
 const char* ad_last_error(const ad_ctx* ctx) { return ctx ? ctx->err : ad::global_error(); }
 
 size_t ad_workspace_bytes(const ad_config* cfg, int with_drafter) {
-  if (ad_config_check(cfg) != AD_OK) return 0;
+  if (ad_config_check(cfg) != AD_OK || drafter_check(*cfg, with_drafter != 0) != AD_OK) return 0;
   return make_plan(*cfg, with_drafter != 0).total;
 }
 
@@ -669,12 +733,15 @@ int ad_create(const ad_config* cfg, const void* verifier_w, const void* drafter_
   if (!verifier_w || !workspace) return fail(nullptr, AD_EINVAL, "null verifier weights or workspace");
   if (((uintptr_t)verifier_w | (uintptr_t)drafter_w | (uintptr_t)workspace) & 255)
     return fail(nullptr, AD_EINVAL, "device pointers must be 256-byte aligned");
+  rc = drafter_check(*cfg, drafter_w != nullptr);
+  if (rc != AD_OK) return rc;
   Plan plan = make_plan(*cfg, drafter_w != nullptr);
   if (workspace_bytes < plan.total) return fail(nullptr, AD_ENOMEM, "workspace smaller than ad_workspace_bytes()");
   int ndev = 0;
   if (hipGetDeviceCount(&ndev) != hipSuccess || ndev < 1) return fail(nullptr, AD_EDEVICE, "no HIP device");
   ad_ctx* c = new ad_ctx();
   c->cfg = *cfg;
+  if (plan.kv8) c->cfg.dtype = AD_BF16;   // (what the weights and the arithmetic are; plan.kv8 has the rest)
   c->plan = plan;
   c->ws = (char*)workspace;
   c->stream = (hipStream_t)hip_stream;
@@ -748,6 +815,13 @@ int ad_create(const ad_config* cfg, const void* verifier_w, const void* drafter_
         return bail("hipMemcpyAsync(memory projections)", e);
     }
   }
+  if (plan.kv8) {
+    std::vector<int> id(plan.m_cap);
+    for (int i = 0; i < plan.m_cap; ++i) id[i] = i;
+    if ((e = hipMemcpyAsync(c->ws + plan.row_id, id.data(), id.size() * 4, hipMemcpyHostToDevice, c->stream)) != hipSuccess ||
+        (e = hipStreamSynchronize(c->stream)) != hipSuccess)
+      return bail("hipMemcpyAsync(row table)", e);
+  }
   for (int i = 0; i < 3; ++i)
     if ((e = hipMemsetAsync(c->ws + plan.team_words[i], 0, kTeamWords * 4, c->stream)) != hipSuccess) return bail("hipMemsetAsync", e);
   if ((e = hipStreamSynchronize(c->stream)) != hipSuccess) return bail("hipStreamSynchronize", e);
@@ -757,7 +831,7 @@ int ad_create(const ad_config* cfg, const void* verifier_w, const void* drafter_
     if (hipGetDevice(&dev) == hipSuccess && hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) == hipSuccess && cus == 8 * kTeamMembers &&
         (size_t)plan.m_cap * kTeamF * 2 < (1u << 31) && plan.cache_layer_stride < (1u << 31)) {   // (32-bit offsets in the kernel)
       for (int i = 0; i < (c->has_drafter ? 2 : 1); ++i)
-        for (int dec = 0; dec < 2; ++dec) c->can_team[i][dec] = team_layout_ok(*cfg, c->w[i], dec != 0) && (cfg->dtype == AD_F32 ? prepare_team_f32(cfg->d_model, dec != 0) : prepare_team(dec != 0));
+        for (int dec = 0; dec < 2; ++dec) c->can_team[i][dec] = !(plan.kv8 && i == AD_VERIFIER && dec) && team_layout_ok(c->cfg, c->w[i], dec != 0) && (cfg->dtype == AD_F32 ? prepare_team_f32(cfg->d_model, dec != 0) : prepare_team(dec != 0));
     } else {
       (void)hipGetLastError();
     }
@@ -878,7 +952,19 @@ static void encode_launches(ad_ctx* c, int model, const int* dev, int M, int B, 
   // cross-attention keys and values of every decoder layer: memory . [wk; wv]^T + [bk; bv], the
   // layers' matrices side by side (copied so at ad_create), the encoder's last LayerNorm applied
   // while the rows are staged
-  {
+  if (ver && p.kv8) {
+    // in 8 bits: layer by layer through the packed temporaries, so that no layer's rows need a place of their own
+    flush_ln(c, M);
+    const SeqDesc* desc = t.self_desc;
+    const Kv8Rows rows{&desc->q_row0, &desc->nq, nullptr, 8, M, c->fw_max_rows, B};
+    for (int l = 0; l < cf.dec_layers; ++l) {
+      Epi e{};
+      e.mode = EPI_KV; e.d = d; e.bias = c->at<float>(p.kv_b[model]) + (size_t)l * 2 * d;
+      e.out1 = c->at<void>(p.tk); e.out2 = c->at<void>(p.tv); e.layer_stride = 0; e.row_dst = c->at<int>(p.row_id);
+      gemm_rows(c, c->ws + p.kv_w[model] + (size_t)l * 2 * d * d * p.esz, M, 2 * d, e);
+      launch_kv8_append(p.kv8_mem, c->ws + p.kv8_mem_at + l * p.kv8_mem_stride, c->at<void>(p.tk), c->at<void>(p.tv), d, d, rows, c->stream);
+    }
+  } else {
     Epi e{};
     e.mode = EPI_KV; e.d = d; e.bias = c->at<float>(p.kv_b[model]);
     e.out1 = c->ws + p.mem_k[model]; e.out2 = c->ws + p.mem_v[model];
@@ -1031,6 +1117,7 @@ struct VerifyLaunch {
   int M, B;
   const TeamRun* team;               // the layers as one launch (null: launch by launch)
   TeamFail fail;
+  const float* sampled;              // ad_verify_sampled: accept_u[B, k_max], pick_u[B], temperature[B] as the device reads them (null: arg max)
 };
 // The launches of one verify call: row assembly + embedding, the forward, arg-max finish + acceptance.
 static void verify_launches(ad_ctx* c, const VerifyLaunch& v) {
@@ -1050,9 +1137,23 @@ static void verify_launches(ad_ctx* c, const VerifyLaunch& v) {
                                c->at<float>(p.pe), cf.d_model, sqrtf((float)cf.d_model), c->at<float>(p.x),
                                c->at<void>(p.xa), c->stream, v.team ? v.team->a.words : nullptr);
   PartialBuf pb{v.part_val, v.part_idx, v.part_stride};
-  if (!gadpp) {
+  if (!gadpp && !v.sampled) {
     const int n_part = verify_forward(c, v.M, nullptr, nullptr, false, false, true, &pb, v.team);
     accept(v.part_val, v.part_idx, v.part_stride, n_part, GadppIn{});
+    return;
+  }
+  if (v.sampled) {
+    // arg max as before (a row without a distribution keeps it); then the rows that the random numbers decide take their tokens, and acceptance finds
+    // the first one that is not the drafted one: a token drawn in its place is another (what is left over has nothing at the drafted token)
+    (void)verify_forward(c, v.M, nullptr, nullptr, true, false, true, &pb, v.team);
+    launch_accept_inputs(v.draft_src, v.sampled, v.sampled + (size_t)v.B * km, v.sampled + (size_t)v.B * km + v.B, km, t.row_start, v.B, c->at<int>(p.sd_draft),
+                         c->at<float>(p.sd_u), c->at<float>(p.sd_v), c->at<float>(p.sd_t), c->stream);
+    AcceptArgs a{};
+    a.logits = c->at<float>(p.logits); a.stride = cf.vocab; a.draft = c->at<int>(p.sd_draft); a.temperature = c->at<float>(p.sd_t);
+    a.accept_u = c->at<float>(p.sd_u); a.pick_u = c->at<float>(p.sd_v); a.row_start = t.row_start;
+    a.vocab = cf.vocab; a.n_seq = v.B; a.rows = v.M; a.max_rows = c->fw_max_rows; a.tokens = c->at<int>(p.o_hat); a.keep = 1;
+    launch_accept_sampled(AD_F32, a, c->at<void>(p.sd_ws), c->stream);
+    accept(c->at<float>(p.o_val), c->at<int>(p.o_hat), 1, 1, GadppIn{});
     return;
   }
   // GAD++ (Section 3.2.3): arg max as before; then the score of every row's drafted token,
@@ -1084,8 +1185,9 @@ static TeamFail team_fail_words(const ad_ctx* c, int model) {
 // ad_verify and its no-allocation variant.  static_scratch: the arg-max partials go to the
 // library's static device array, every launch is made eagerly (no graph is built or replayed) and
 // nothing on the way allocates.
+struct SampledIn { const float *accept_u, *pick_u, *temperature; };
 static int verify_call(ad_ctx* c, const int32_t* draft, const int32_t* k, int32_t* n_accept, int32_t* next_token,
-                       int32_t* verified, bool static_scratch) {
+                       int32_t* verified, bool static_scratch, const SampledIn* sampled = nullptr) {
   if (!c) return fail(nullptr, AD_EINVAL, "null context");
   if (!draft || !k || !n_accept || !next_token) return fail(c, AD_EINVAL, "null buffer");
   if (!c->encoded[AD_VERIFIER]) return fail(c, AD_ESTATE, "ad_verify before ad_encode(AD_VERIFIER)");
@@ -1104,6 +1206,17 @@ static int verify_call(ad_ctx* c, const int32_t* draft, const int32_t* k, int32_
     }
     M += k[b];
     max_rows = std::max(max_rows, (int)k[b]);
+  }
+  if (sampled) {
+    for (int b = 0; b < B; ++b) {
+      if (!k[b]) continue;
+      for (int i = 0; i < k[b]; ++i) {
+        const float u = sampled->accept_u[(size_t)b * km + i];
+        if (!(u >= 0.f && u < 1.f)) return fail(c, AD_EINVAL, "accept_u outside [0, 1)");
+      }
+      if (!(sampled->pick_u[b] >= 0.f && sampled->pick_u[b] < 1.f)) return fail(c, AD_EINVAL, "pick_u outside [0, 1)");
+      if (sampled->temperature && !(sampled->temperature[b] > 0.f && sampled->temperature[b] < INFINITY)) return fail(c, AD_EINVAL, "temperature must be positive and finite");
+    }
   }
   if (static_scratch) {
     if (!c->scratch_dev) return fail(c, AD_ESTATE, "the static scratch array is unavailable on this device");
@@ -1143,6 +1256,19 @@ static int verify_call(ad_ctx* c, const int32_t* draft, const int32_t* k, int32_
     HIP_TRY(c, hipMemcpyAsync(c->at<int>(p.k_dev), h + pl.k, (size_t)B * 4, hipMemcpyHostToDevice, c->stream));
     HIP_TRY(c, hipMemcpyAsync(c->at<int>(p.draft_dev), h + pl.draft, (size_t)B * km * 4, hipMemcpyHostToDevice, c->stream));
     v.k_src = c->at<int>(p.k_dev); v.draft_src = c->at<int>(p.draft_dev); v.result_dst = c->at<int>(p.result);
+  }
+  if (sampled) {
+    float* f = (float*)(h + pl.s_in);
+    memcpy(f, sampled->accept_u, (size_t)B * km * 4);
+    for (int b = 0; b < B; ++b) {
+      f[(size_t)B * km + b] = sampled->pick_u[b];
+      f[(size_t)B * km + B + b] = sampled->temperature ? sampled->temperature[b] : 1.f;
+    }
+    if (mapped) v.sampled = (const float*)(c->pin_dev + pl.s_in);
+    else {
+      HIP_TRY(c, hipMemcpyAsync(c->at<float>(p.sd_host), f, ((size_t)B * km + 2 * B) * 4, hipMemcpyHostToDevice, c->stream));
+      v.sampled = c->at<float>(p.sd_host);
+    }
   }
   if (static_scratch) {
     v.part_val = (float*)c->scratch_dev;
@@ -1196,11 +1322,13 @@ static int verify_call(ad_ctx* c, const int32_t* draft, const int32_t* k, int32_
     if (team) { c->last_run = run; ++c->team_launches; }
     bool launched = false;
     if (mapped && !static_scratch && (!team || B <= kTeamGraphBatch)) {
-      const unsigned long long key = shape_key(M, max_rows, B, (gadpp ? 1 : 0) | (watch ? 2 : 0) | (c->fuse_crossq ? 4 : 0) | (self_keys <= 64 ? 8 : 0) | (cross_keys <= 64 ? 16 : 0));
+      const unsigned long long key = shape_key(M, max_rows, B, (gadpp ? 1 : 0) | (watch ? 2 : 0) | (c->fuse_crossq ? 4 : 0) | (self_keys <= 64 ? 8 : 0) | (cross_keys <= 64 ? 16 : 0) | (sampled ? 32 : 0));
       unsigned tau_bits;
       memcpy(&tau_bits, &c->gadpp_tau, 4);
       const unsigned long long more = gadpp ? ((unsigned long long)c->gadpp_beta << 32) | tau_bits : 0;
-      launched = run_as_graph(c, c->stream, key, [&]() { verify_launches(c, v); }, more, team_part(v.team));
+      ad_ctx::TeamPart part = team_part(v.team);
+      if (p.kv8) { part[26] = kv8_key_bound(self_keys, p.l_cap); part[27] = kv8_key_bound(cross_keys, cf.max_src); }   // (places no team's deal uses)
+      launched = run_as_graph(c, c->stream, key, [&]() { verify_launches(c, v); }, more, part);
     }
     if (!launched) verify_launches(c, v);
     if (!mapped) HIP_TRY(c, hipMemcpyAsync(res, c->at<int>(p.result), (size_t)B * 8, hipMemcpyDeviceToHost, c->stream));
@@ -1268,6 +1396,16 @@ int ad_verify(ad_ctx* c, const int32_t* draft, const int32_t* k, int32_t* n_acce
 int ad_verify_static(ad_ctx* c, const int32_t* draft, const int32_t* k, int32_t* n_accept, int32_t* next_token,
                      int32_t* verified) {
   return verify_call(c, draft, k, n_accept, next_token, verified, true);
+}
+
+int ad_verify_sampled(ad_ctx* c, const int32_t* draft, const int32_t* k, const float* accept_u, const float* pick_u, const float* temperature,
+                      int32_t* n_accept, int32_t* next_token, int32_t* verified) {
+  if (!c) return fail(nullptr, AD_EINVAL, "null context");
+  if (!accept_u || !pick_u) return fail(c, AD_EINVAL, "null buffer");
+  if (!c->cfg.debug_logits) return fail(c, AD_ESTATE, "ad_verify_sampled needs a context with debug_logits (the scores it draws from are kept)");
+  if (c->gadpp_beta > 1) return fail(c, AD_ESTATE, "ad_verify_sampled under the relaxed verification (ad_set_gadpp): set beta to 1 first");
+  const SampledIn in{accept_u, pick_u, temperature};
+  return verify_call(c, draft, k, n_accept, next_token, verified, false, &in);
 }
 
 int ad_draft_nat(ad_ctx* c, int k, int32_t* draft_out) {

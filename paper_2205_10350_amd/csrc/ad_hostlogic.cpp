@@ -19,16 +19,22 @@ const char* global_error() { return g_error; }
 
 static size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
+// attention keeps one head's keys and values of a sequence in LDS (rows padded by a dword)
+bool attention_keys_fit(const ad_config& c, size_t keys) {
+  const size_t dh = c.d_model / c.n_heads, esz = bf16_dtype(c.dtype) ? 2 : 4;
+  return 2 * keys * (dh * esz / 4 + 1) * 4 + 64 * dh * 4 + 4 * keys * 4 <= 160 * 1024;
+}
+
 // ---------------------------------------------------------------------------------------------
 std::vector<WEntry> weight_layout(const ad_config& c, size_t* total_bytes) {
   std::vector<WEntry> v;
   size_t off = 0;
   const int d = c.d_model, f = c.d_ffn;
-  const int mb = c.dtype == AD_BF16 ? 2 : 4;   // matrix element bytes
+  const int mb = bf16_dtype(c.dtype) ? 2 : 4;   // matrix element bytes
   // bf16 matrices that feed a GEMM are stored as MFMA B-operand tiles (see ad.h); the embedding
   // table is gathered by row and stays row-major
   auto mat = [&](const std::string& n, int rows, int cols, bool gemm = true) {
-    v.push_back({n, off, rows, cols, mb, (gemm && c.dtype == AD_BF16) ? 1 : 0});
+    v.push_back({n, off, rows, cols, mb, (gemm && bf16_dtype(c.dtype)) ? 1 : 0});
     off += (size_t)rows * cols * mb;
   };
   auto vec = [&](const std::string& n, int cols) {
@@ -49,7 +55,7 @@ std::vector<WEntry> weight_layout(const ad_config& c, size_t* total_bytes) {
   };
   group(); mat("emb", c.vocab, d, false);
   // a tied output projection still gets its own (tiled) copy of the table in bf16 mode
-  if (!c.tie_output || c.dtype == AD_BF16) { group(); mat("out.w", c.vocab, d); }
+  if (!c.tie_output || bf16_dtype(c.dtype)) { group(); mat("out.w", c.vocab, d); }
   for (int l = 0; l < c.enc_layers; ++l) {
     std::string p = "enc." + std::to_string(l);
     attn(p + ".self"); ln(p + ".ln1"); ffn(p + ".ffn"); ln(p + ".ln2");
@@ -84,7 +90,7 @@ ModelW bind_weights(const ad_config& c, const void* blob) {
   };
   ModelW m;
   m.emb = find("emb");
-  m.out_w = (c.tie_output && c.dtype != AD_BF16) ? m.emb : find("out.w");
+  m.out_w = (c.tie_output && !bf16_dtype(c.dtype)) ? m.emb : find("out.w");
   for (int l = 0; l < c.enc_layers; ++l) {
     std::string p = "enc." + std::to_string(l);
     m.enc.push_back({attn(p + ".self"), ln(p + ".ln1"), ffn(p + ".ffn"), ln(p + ".ln2")});
@@ -261,22 +267,23 @@ extern "C" {
 int ad_config_check(const ad_config* c) {
   using ad::set_global_error;
   if (!c) { set_global_error("null config"); return AD_EINVAL; }
-  if (c->dtype != AD_F32 && c->dtype != AD_BF16) { set_global_error("dtype must be AD_F32 or AD_BF16"); return AD_EINVAL; }
+  const bool kv8 = ad::kv8_dtype(c->dtype);
+  if (c->dtype != AD_F32 && c->dtype != AD_BF16 && !kv8) { set_global_error("dtype must be AD_F32, AD_BF16, AD_BF16_KV_E4M3 or AD_BF16_KV_I8"); return AD_EINVAL; }
   if (c->d_model < 32 || c->d_model % 32 || c->d_model > 2048) { set_global_error("d_model must be a multiple of 32 in [32, 2048]"); return AD_EINVAL; }
   if (c->d_ffn < 32 || c->d_ffn % 32) { set_global_error("d_ffn must be a multiple of 32"); return AD_EINVAL; }
   if (c->n_heads < 1 || c->d_model % c->n_heads) { set_global_error("n_heads must divide d_model"); return AD_EINVAL; }
   const int dh = c->d_model / c->n_heads;
   if (dh != 16 && dh != 32 && dh != 64 && dh != 128) { set_global_error("head size must be 16, 32, 64 or 128"); return AD_EINVAL; }
+  if (kv8 && dh == 16) { set_global_error("caches in 8 bits need a head size of 32, 64 or 128"); return AD_EINVAL; }
+  if (kv8 && c->n_heads > 256) { set_global_error("caches in 8 bits have at most 256 heads"); return AD_EINVAL; }
   if (c->vocab < 16 || c->vocab % 16) { set_global_error("vocab must be a multiple of 16"); return AD_EINVAL; }
   if (c->enc_layers < 1 || c->dec_layers < 1) { set_global_error("need at least one encoder and one decoder layer"); return AD_EINVAL; }
   if (c->max_batch < 1 || c->max_src < 1 || c->max_len < 1 || c->k_max < 1) { set_global_error("capacities must be >= 1"); return AD_EINVAL; }
   if (c->max_batch > 4096 || c->max_src > 8192 || c->max_len > 8192 || c->k_max > 8192) { set_global_error("capacity too large"); return AD_EINVAL; }
-  {
-    // attention keeps one head's keys and values of a sequence in LDS (rows padded by a dword)
-    const size_t nk = (size_t)std::max(c->max_src, c->max_len + c->k_max);
-    const size_t esz = c->dtype == AD_BF16 ? 2 : 4;
-    const size_t need = 2 * nk * ((size_t)dh * esz / 4 + 1) * 4 + 64 * (size_t)dh * 4 + 4 * nk * 4;
-    if (need > 160 * 1024) { set_global_error("max_src / max_len + k_max too large: a head's keys and values must fit in 160 KB of LDS"); return AD_EINVAL; }
+  // (caches in 8 bits are not kept in LDS: there the encoder's own keys are all that has to fit)
+  if (!ad::attention_keys_fit(*c, kv8 ? c->max_src : std::max(c->max_src, c->max_len + c->k_max))) {
+    set_global_error("max_src / max_len + k_max too large: a head's keys and values must fit in 160 KB of LDS");
+    return AD_EINVAL;
   }
   const int32_t ids[4] = {c->bos, c->pad, c->eos, c->mask};
   for (int i = 0; i < 4; ++i)

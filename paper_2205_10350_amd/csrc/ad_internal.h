@@ -13,6 +13,13 @@
 
 namespace ad {
 
+// dtypes with bf16 weights and arithmetic; those with caches in 8 bits, and their format
+inline bool bf16_dtype(int dtype) { return dtype != AD_F32; }
+inline bool kv8_dtype(int dtype) { return dtype == AD_BF16_KV_E4M3 || dtype == AD_BF16_KV_I8; }
+inline int kv8_format(int dtype) { return dtype == AD_BF16_KV_E4M3 ? AD_KV_E4M3 : AD_KV_I8; }
+// most keys of a (sequence, head) that attention over bf16 / fp32 rows takes
+bool attention_keys_fit(const ad_config& c, size_t keys);
+
 // ---- weight layout ---------------------------------------------------------------------
 struct WEntry {
   std::string name;

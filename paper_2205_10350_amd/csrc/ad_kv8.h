@@ -41,11 +41,12 @@ inline Kv8Dims kv8_dims(const ad_kv8_config& c) {
   return d;
 }
 
-// Which packed rows a sequence has in a call and how many tokens it had before: entries `stride` ints apart, count == nullptr: start[b + 1] - start[b].
+// Which packed rows each of n_seq sequences has in a call and how many tokens it had before: entries `stride` ints apart; count == nullptr:
+// start[b + 1] - start[b], base == nullptr: 0.
 // What the tables say is held to [0, rows) packed rows, max_rows rows a sequence and the capacity, so that a wrong table cannot reach past a buffer.
 struct Kv8Rows {
   const int *start, *count, *base;
-  int stride, rows, max_rows;
+  int stride, rows, max_rows, n_seq;
 };
 
 // Keys and values of the rows (bf16, [rows, heads, width] with row strides in elements) behind base[b] tokens.

@@ -232,14 +232,14 @@ static void append_for(const Kv8Dims& d, unsigned char* cache, const bf16_t* k, 
   else k_kv8_append<DH, FMT, false><<<grid, 4 * DH, 0, s>>>(cache, k, v, ks, vs, r, d);
 }
 void launch_kv8_append(const Kv8Dims& d, void* cache, const void* k, const void* v, size_t k_stride, size_t v_stride, const Kv8Rows& r, hipStream_t s) {
-  const dim3 grid((r.max_rows + kKv8Block - 2) / kKv8Block + 1, d.heads, d.n_seq);
+  const dim3 grid((r.max_rows + kKv8Block - 2) / kKv8Block + 1, d.heads, r.n_seq);
   kv8_dispatch(d, [&](auto width, auto fmt) {
     append_for<width.value, fmt.value>(d, (unsigned char*)cache, (const bf16_t*)k, (const bf16_t*)v, k_stride, v_stride, r, grid, s);
   });
 }
 
 void launch_kv8_read(const Kv8Dims& d, const void* cache, const Kv8Rows& r, const int* length, int dtype, void* k_out, void* v_out, hipStream_t s) {
-  const dim3 grid((r.max_rows + kKv8Block - 2) / kKv8Block + 1, d.heads, d.n_seq);
+  const dim3 grid((r.max_rows + kKv8Block - 2) / kKv8Block + 1, d.heads, r.n_seq);
   kv8_dispatch(d, [&](auto width, auto fmt) {
     if (dtype == AD_BF16)
       k_kv8_read<width.value, fmt.value, bf16_t><<<grid, 4 * width.value, 0, s>>>((const unsigned char*)cache, r, length, (bf16_t*)k_out, (bf16_t*)v_out, d);

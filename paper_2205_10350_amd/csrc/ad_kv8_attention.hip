@@ -130,7 +130,7 @@ __global__ __launch_bounds__(256) void k_kv8_attend(const unsigned char* __restr
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // workgroup -> ((split, row tile), (sequence, head)): those of one (sequence, head) lie a multiple of n_seq * heads apart, on one XCD where that is
   // a multiple of 8, so that row tiles read the keys from one L2
-  const int pairs = dm.n_seq * dm.heads;
+  const int pairs = a.rows.n_seq * dm.heads;
   const int pair = blockIdx.x % pairs, rest = blockIdx.x / pairs;
   const int tile = rest % a.row_tiles, split = rest / a.row_tiles;
   const int b = pair / dm.heads, h = pair % dm.heads;
@@ -326,7 +326,7 @@ static void attend_for(const Kv8Dims& d, const unsigned char* cache, Kv8Attend& 
   const int m = a.rows.max_rows * a.group;
   auto go = [&](auto r, auto closed) {
     a.row_tiles = (m + 16 * r.value - 1) / (16 * r.value);
-    k_kv8_attend<DH, r.value, FMT, closed.value><<<(unsigned)((size_t)d.n_seq * d.heads * a.row_tiles * a.n_split), 256, 0, s>>>(cache, a, d);
+    k_kv8_attend<DH, r.value, FMT, closed.value><<<(unsigned)((size_t)a.rows.n_seq * d.heads * a.row_tiles * a.n_split), 256, 0, s>>>(cache, a, d);
   };
   auto by_rows = [&](auto closed) {
     // as few passes over the keys as the rows allow: up to 64 rows of a wave (width 128: 32, more would not fit the registers of two waves)
@@ -336,7 +336,7 @@ static void attend_for(const Kv8Dims& d, const unsigned char* cache, Kv8Attend& 
   };
   if (d.closed) by_rows(std::true_type{});
   else by_rows(std::false_type{});
-  if (a.n_split > 1) k_kv8_join<DH><<<dim3((a.rows.max_rows * d.heads * a.group + 3) / 4, d.n_seq), 256, 0, s>>>(a, d);
+  if (a.n_split > 1) k_kv8_join<DH><<<dim3((a.rows.max_rows * d.heads * a.group + 3) / 4, a.rows.n_seq), 256, 0, s>>>(a, d);
 }
 void launch_kv8_attend(const Kv8Dims& d, const void* cache, const void* q, size_t q_stride, void* out, size_t out_stride, int q_heads,
                        const Kv8Rows& r, int max_keys, float scale, void* ws, hipStream_t s) {

@@ -14,7 +14,7 @@ __device__ __forceinline__ Kv8Seq kv8_seq(const Kv8Rows& t, int b, int capacity,
   Kv8Seq s;
   s.row0 = t.start[at];
   s.n = t.count ? t.count[at] : t.start[at + t.stride] - s.row0;
-  s.base = t.base[at];
+  s.base = t.base ? t.base[at] : 0;
   if (s.row0 < 0 || s.row0 > t.rows || s.base < 0) s.n = 0;
   s.base = min(max(s.base, 0), capacity);
   s.n = min(min(s.n, t.max_rows), t.rows - s.row0);

@@ -60,7 +60,7 @@ int ad_kv8_append(const ad_kv8_config* c, void* cache, const void* k, int64_t k_
     return refuse("ad_kv8_append: k and v must be 16-byte aligned, their row strides multiples of 8 and at least n_heads * head_width");
   const Kv8Dims d = kv8_dims(*c);
   if (max_rows > d.k_max) return refuse(c->closed ? "ad_kv8_append: max_rows above the capacity" : "ad_kv8_append: max_rows above k_max");
-  launch_kv8_append(d, cache, k, v, (size_t)k_stride, (size_t)v_stride, Kv8Rows{row_start, nullptr, length, 1, rows, max_rows}, (hipStream_t)hip_stream);
+  launch_kv8_append(d, cache, k, v, (size_t)k_stride, (size_t)v_stride, Kv8Rows{row_start, nullptr, length, 1, rows, max_rows, c->n_seq}, (hipStream_t)hip_stream);
   return launched("ad_kv8_append");
 }
 
@@ -73,7 +73,7 @@ int ad_kv8_read(const ad_kv8_config* c, const void* cache, const int32_t* row_st
   if (!length || !k_out || !v_out) return refuse("ad_kv8_read: null buffer");
   if (((uintptr_t)k_out | (uintptr_t)v_out) & 15) return refuse("ad_kv8_read: outputs must be 16-byte aligned");
   const Kv8Dims d = kv8_dims(*c);
-  launch_kv8_read(d, cache, Kv8Rows{row_start, nullptr, begin, 1, rows, std::min(max_rows, d.capacity)}, length, dtype, k_out, v_out, (hipStream_t)hip_stream);
+  launch_kv8_read(d, cache, Kv8Rows{row_start, nullptr, begin, 1, rows, std::min(max_rows, d.capacity), c->n_seq}, length, dtype, k_out, v_out, (hipStream_t)hip_stream);
   return launched("ad_kv8_read");
 }
 
@@ -101,7 +101,7 @@ int ad_kv8_attend(const ad_kv8_config* c, const void* cache, const void* q, int6
   if (need && (!workspace || ((uintptr_t)workspace & 255))) return refuse("ad_kv8_attend: the workspace must be 256-byte aligned device memory");
   if (workspace_bytes < need) { set_global_error("ad_kv8_attend: workspace smaller than ad_kv8_attend_bytes()"); return AD_ENOMEM; }
   if (!kv8_attend_fits(d, q_heads, max_rows, max_keys)) return refuse("ad_kv8_attend: more workgroups than a launch takes (sequences x heads x rows x keys)");
-  launch_kv8_attend(d, cache, q, (size_t)q_stride, out, (size_t)out_stride, q_heads, Kv8Rows{row_start, nullptr, length, 1, rows, max_rows},
+  launch_kv8_attend(d, cache, q, (size_t)q_stride, out, (size_t)out_stride, q_heads, Kv8Rows{row_start, nullptr, length, 1, rows, max_rows, c->n_seq},
                     max_keys, scale, workspace, (hipStream_t)hip_stream);
   return launched("ad_kv8_attend");
 }

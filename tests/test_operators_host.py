@@ -125,3 +125,33 @@ def test_plain_forms():
     q = np.array([[0.25, 0.5, 0.25]])
     assert accept(p, [1], q, 1.0, [0.49], 0.0) == [1] and accept(p, [1], q, 1.0, [0.51], 0.9) == [0]
     assert accept(p, [ad.AD_NEVER], None, 1.0, [0.0], 0.6) == [1]
+
+
+def config(name="tiny", dtype="bf16_kv_i8", **kw):
+    from ad_inputs import SPECIAL, model_dims
+    a = dict(max_batch=2, max_src=24, max_len=32, k_max=8, special=SPECIAL)
+    a.update(kw)
+    return ad.make_config(model_dims(name) if isinstance(name, str) else name, dtype=dtype, **a)
+
+
+def test_contexts_with_caches_in_8_bits():
+    """Same weights as bf16; smaller workspaces once outputs are long; longer outputs than bf16 rows allow, but not beside a drafter."""
+    for dtype in ("bf16_kv_e4m3", "bf16_kv_i8"):
+        assert ad.config_check(config(dtype=dtype)) == ad.AD_OK
+        assert ad.weights_layout(config(dtype=dtype)) == ad.weights_layout(config(dtype="bf16"))
+        assert ad.weights_layout(config(dtype=dtype, tie_output=True)) == ad.weights_layout(config(dtype="bf16", tie_output=True))
+        big = dict(max_batch=32, max_src=500, max_len=400, k_max=16)
+        small, wide = (ad.workspace_bytes(config("big", dtype=t, **big), False) for t in (dtype, "bf16"))
+        caches = 6 * 2 * 32 * (500 + 416) * 1024 * 2
+        assert wide - small > 0.4 * caches
+        assert ad.config_check(config("base", dtype=dtype, max_len=8000)) == ad.AD_OK
+        assert ad.config_check(config("base", dtype="bf16", max_len=8000)) == ad.AD_EINVAL
+        assert ad.workspace_bytes(config("base", dtype=dtype, max_len=8000), False) > 0
+        assert ad.workspace_bytes(config("base", dtype=dtype, max_len=8000), True) == 0 and "drafter" in message()
+        assert ad.workspace_bytes(config("base", dtype=dtype), True) > 0
+        assert ad.config_check(config("micro", dtype=dtype)) == ad.AD_EINVAL and "head size" in message()      # heads of 16
+        assert ad.config_check(config("base", dtype=dtype, max_src=8000)) == ad.AD_EINVAL                       # the encoder's own attention
+
+
+def test_verify_sampled_without_a_context():
+    assert ad.lib().ad_verify_sampled(None, None, None, None, None, None, None, None, None) == ad.AD_EINVAL
