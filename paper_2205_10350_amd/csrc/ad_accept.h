@@ -19,11 +19,13 @@ struct AcceptArgs {
   int* tokens;                   // [rows]
   int keep;                      // 1: rows without a decided token keep what `tokens` holds
   // the launcher's: per row and piece of the vocabulary, per sequence and piece
-  int pieces;
+  int pieces, rest;              // rest: the deciding rows' sums are taken apart (rest_sum)
   double* piece_sum;
   float* piece_max;
   double* rest_sum;
+  struct AcceptRowInfo* row_info;   // [rows]
 };
+struct AcceptRowInfo { double z; float m; int stands; };
 // The inputs of a verify call, host-visible and by sequence, as packed rows in device memory: draft, u [n_seq, k_max], v, t [n_seq] -> rows of
 // row_start (draft_out, u_out) and copies (v_out, t_out)
 void launch_accept_inputs(const int* draft, const float* u, const float* v, const float* t, int k_max, const int* row_start, int n_seq, int* draft_out,

@@ -22,7 +22,11 @@ namespace ad {
 
 constexpr int kAcceptThreads = 256;
 constexpr int kAcceptPiece = 4096;                                  // scores of a workgroup
+constexpr int kDecideThreads = 1024;                                // where a sequence's rows are tested, a wave a row
 constexpr int kAcceptEach = kAcceptPiece / kAcceptThreads;          // of a thread
+
+// What weighs less than this beside the row's most likely token weighs nothing: a piece counts only if one of its tokens will (exp2_down ends at 2^-1000).
+constexpr double kNothing = 0x1p-900;
 
 // 2^t for t <= 0 (NaN stays): nearest whole number and the Taylor series of 2^f, |f| <= 1/2, to f^11: 7e-15 relative
 __device__ __forceinline__ double exp2_down(double t) {
@@ -42,10 +46,43 @@ __device__ __forceinline__ double exp2_down(double t) {
   p = fma(p, f, 1.0);
   return ldexp(p, (int)n);
 }
+// The same for the bulk of the scores, 16 instructions: t = fma(x, rate, off) held to [-1020, ..] (what is smaller weighs nothing beside the 1 of the maximum; a NaN is
+// the caller's to see), the whole part through the low word of t + 1.5 * 2^52 straight into the exponent, and 2^f to f^9 (7e-12 relative: a drawn number falls
+// between this and the exact border once in 10^11 / vocab draws).
+__device__ __forceinline__ double exp2_bulk(float x, double rate, double off) {
+  const double t = fmax(fma((double)x, rate, off), -1020.0);
+  const double big = t + 6755399441055744.0, f = t - (big - 6755399441055744.0);
+  double p = 1.01780860092396997275e-7;    // ln(2)^k / k!, k = 9 .. 0
+  p = fma(p, f, 1.32154867901443094884e-6);
+  p = fma(p, f, 1.52527338040598402800e-5);
+  p = fma(p, f, 1.54035303933816099544e-4);
+  p = fma(p, f, 1.33335581464284434234e-3);
+  p = fma(p, f, 9.61812910762847716197e-3);
+  p = fma(p, f, 5.55041086648215799532e-2);
+  p = fma(p, f, 2.40226506959100712334e-1);
+  p = fma(p, f, 6.93147180559945309417e-1);
+  p = fma(p, f, 1.0);
+  const long long bits = __builtin_bit_cast(long long, p);
+  const unsigned hi = (unsigned)(bits >> 32) + ((unsigned)__builtin_bit_cast(long long, big) << 20);
+  return __builtin_bit_cast(double, (long long)((unsigned long long)hi << 32 | (unsigned)bits));
+}
+// sum over the wave, the same in every lane: lane moves as wave_sum's
+template <int CTRL> __device__ __forceinline__ double dpp_move_f64(double v) {
+  const long long b = __builtin_bit_cast(long long, v);
+  const unsigned lo = (unsigned)__builtin_amdgcn_update_dpp(0, (int)b, CTRL, 0xf, 0xf, true), hi = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(b >> 32), CTRL, 0xf, 0xf, true);
+  return __builtin_bit_cast(double, (long long)((unsigned long long)hi << 32 | lo));
+}
+__device__ __forceinline__ double lane_f64(double v, int lane) {
+  const long long b = __builtin_bit_cast(long long, v);
+  const unsigned lo = (unsigned)__builtin_amdgcn_readlane((int)b, lane), hi = (unsigned)__builtin_amdgcn_readlane((int)(b >> 32), lane);
+  return __builtin_bit_cast(double, (long long)((unsigned long long)hi << 32 | lo));
+}
 __device__ __forceinline__ double wave_sum_f64(double v) {
-#pragma unroll
-  for (int s = 1; s < 64; s *= 2) v += __shfl_xor(v, s);
-  return v;
+  v += dpp_move_f64<0xB1>(v);
+  v += dpp_move_f64<0x4E>(v);
+  v += dpp_move_f64<0x141>(v);
+  v += dpp_move_f64<0x140>(v);
+  return (lane_f64(v, 0) + lane_f64(v, 16)) + (lane_f64(v, 32) + lane_f64(v, 48));
 }
 
 template <typename T> struct AcceptRow {
@@ -99,7 +136,7 @@ __device__ __forceinline__ double accept_rate(const AcceptArgs& a, int b) {
 }
 __device__ __forceinline__ bool accept_drafted(const AcceptArgs& a, int d) { return d >= 0 && d < a.vocab; }
 
-template <typename T>
+template <typename T, bool WIDE>
 __global__ __launch_bounds__(kAcceptThreads) void k_accept_stats(AcceptArgs a) {
   __shared__ float ms[kAcceptThreads / 64];
   __shared__ double ss[kAcceptThreads / 64];
@@ -115,31 +152,50 @@ __global__ __launch_bounds__(kAcceptThreads) void k_accept_stats(AcceptArgs a) {
   const double rate = accept_rate(a, b);
   float m = head;
 #pragma unroll
-  for (int j = 0; j < kAcceptEach; ++j) m = fmaxf(m, v[j]);
+  for (int j = 0; j < kAcceptEach; ++j) m = __builtin_amdgcn_fmed3f(m, v[j], INFINITY);   // (the larger; fmaxf would quiet NaN first)
   m = wave_max(m);
   if ((t & 63) == 0) ms[t >> 6] = m;
   __syncthreads();
   m = fmaxf(fmaxf(ms[0], ms[1]), fmaxf(ms[2], ms[3]));
   double s = 0.0;
+  bool nan = head != head || !(m < INFINITY) || rate != rate;   // (no distribution)
   if (m > -INFINITY) {
+    const bool here = t < x.heads(c) && t != skip;
+    // (the drafted token's is one thread's: there, and only there, it is taken out)
+    constexpr int kVec = AcceptRow<T>::kVec;
+    const int in = skip - x.index(c, t, 0);
+    if (skip >= 0 && in >= 0 && in % (kAcceptThreads * kVec) < kVec && in / (kAcceptThreads * kVec) < kAcceptEach / kVec) {
 #pragma unroll
-    for (int j = 0; j < kAcceptEach; ++j) {
-      const double e = exp2_down(((double)v[j] - (double)m) * rate);
-      s += x.index(c, t, j) == skip ? 0.0 : e;
+      for (int j = 0; j < kAcceptEach; ++j)
+        if (x.index(c, t, j) == skip) { nan = nan || v[j] != v[j]; v[j] = -INFINITY; }
     }
-    if (t < x.heads(c) && t != skip) s += exp2_down(((double)head - (double)m) * rate);
+    if constexpr (WIDE) {
+      const double off = -(double)m * rate;
+#pragma unroll
+      for (int j = 0; j < kAcceptEach; ++j) {
+        nan = nan || v[j] != v[j];
+        s += exp2_bulk(v[j], rate, off);
+      }
+      if (here) s += exp2_bulk(head, rate, off);
+    } else {
+      // (a row's test alone rests on these sums: 2^-24 of a probability is where a drawn number of 24 bits may fall either way)
+      const float r = (float)rate;
+      float e[4] = {here ? __builtin_amdgcn_exp2f((head - m) * r) : 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < kAcceptEach; ++j) e[j % 4] += __builtin_amdgcn_exp2f((v[j] - m) * r);
+      s = (double)((e[0] + e[1]) + (e[2] + e[3]));
+    }
   } else {
-    // nothing but -inf here, or a NaN that the maximum has passed over
-    bool nan = head != head;
 #pragma unroll
     for (int j = 0; j < kAcceptEach; ++j) nan = nan || v[j] != v[j];
-    if (nan) s = (double)NAN;
   }
+  if (nan) s = (double)NAN;
   s = wave_sum_f64(s);
   if ((t & 63) == 0) ss[t >> 6] = s;
   __syncthreads();
   if (t == 0) {
-    a.piece_sum[(size_t)row * a.pieces + c] = (ss[0] + ss[1]) + (ss[2] + ss[3]);
+    const double sum = (ss[0] + ss[1]) + (ss[2] + ss[3]);
+    a.piece_sum[(size_t)row * a.pieces + c] = sum < kNothing ? 0.0 : sum;
     a.piece_max[(size_t)row * a.pieces + c] = m;
   }
 }
@@ -148,40 +204,43 @@ __global__ __launch_bounds__(kAcceptThreads) void k_accept_stats(AcceptArgs a) {
 struct AcceptSums { float m; double z, wd; };
 template <typename T> __device__ __forceinline__ AcceptSums accept_sums(const AcceptArgs& a, int row, double rate) {
   const int lane = threadIdx.x & 63;
-  AcceptSums r;
-  r.m = -INFINITY;
-  for (int c = lane; c < a.pieces; c += 64) r.m = fmaxf(r.m, a.piece_max[(size_t)row * a.pieces + c]);
-  r.m = wave_max(r.m);
-  double z = 0.0;
-  for (int c = lane; c < a.pieces; c += 64) {
-    const float mc = a.piece_max[(size_t)row * a.pieces + c];
-    const double s = a.piece_sum[(size_t)row * a.pieces + c];
-    z += mc > -INFINITY ? s * exp2_down(((double)mc - (double)r.m) * rate) : s;   // (s is 0 there, or NaN)
-  }
-  r.z = wave_sum_f64(z);
+  const float* pm = a.piece_max + (size_t)row * a.pieces;
+  const double* ps = a.piece_sum + (size_t)row * a.pieces;
+  // (what the row needs is requested at once: the drafted token's score behind its id, the first 64 pieces beside them)
   const int d = a.draft[row];
-  r.wd = 0.0;
-  if (accept_drafted(a, d)) r.wd = exp2_down(((double)AcceptRow<T>(a, row).at(d) - (double)r.m) * rate);
+  const float m0 = lane < a.pieces ? pm[lane] : -INFINITY;
+  const double s0 = lane < a.pieces ? ps[lane] : 0.0;
+  const float xd = accept_drafted(a, d) ? AcceptRow<T>(a, row).at(d) : -INFINITY;
+  AcceptSums r;
+  r.m = m0;
+  for (int c = lane + 64; c < a.pieces; c += 64) r.m = fmaxf(r.m, pm[c]);
+  r.m = wave_max(r.m);
+  auto part = [&](float mc, double s) { return mc > -INFINITY ? s * exp2_down(((double)mc - (double)r.m) * rate) : s; };   // (s is 0 there, or NaN)
+  double z = part(m0, s0);
+  for (int c = lane + 64; c < a.pieces; c += 64) z += part(pm[c], ps[c]);
+  r.z = wave_sum_f64(z);
+  r.wd = accept_drafted(a, d) ? exp2_down(((double)xd - (double)r.m) * rate) : 0.0;
   if (!a.probs) r.z += r.wd;
   return r;
 }
 __device__ __forceinline__ bool accept_broken(double z) { return !(z > 0.0 && z < (double)INFINITY); }
 
+// A row's test, by one wave
+template <typename T> __device__ __forceinline__ AcceptRowInfo accept_decide(const AcceptArgs& a, int row, double rate) {
+  const int d = a.draft[row];
+  const float u = a.accept_u[row], q = !a.probs ? 1.f : accept_drafted(a, d) ? a.probs[(size_t)row * a.probs_stride + d] : 0.f;
+  const AcceptSums r = accept_sums<T>(a, row, rate);
+  return AcceptRowInfo{r.z, r.m, accept_drafted(a, d) && !accept_broken(r.z) && (double)u * (double)q < r.wd / r.z};
+}
 // The first row whose drafted token does not stand (n: all do), by the whole workgroup
 template <typename T> __device__ __forceinline__ int accept_first(const AcceptArgs& a, const AcceptSeq& sq, double rate, int* first) {
   const int wave = threadIdx.x >> 6;
   if (threadIdx.x == 0) *first = sq.n;
   __syncthreads();
-  for (int i0 = 0; i0 < sq.n; i0 += kAcceptThreads / 64) {
+  for (int i0 = 0; i0 < sq.n; i0 += kDecideThreads / 64) {
     const int i = i0 + wave;
     if (i < sq.n) {
-      const int row = sq.row0 + i, d = a.draft[row];
-      bool stands = false;
-      if (accept_drafted(a, d)) {
-        const AcceptSums r = accept_sums<T>(a, row, rate);
-        const double q = a.probs ? (double)a.probs[(size_t)row * a.probs_stride + d] : 1.0;
-        stands = !accept_broken(r.z) && (double)a.accept_u[row] * q < r.wd / r.z;
-      }
+      const bool stands = accept_decide<T>(a, sq.row0 + i, rate).stands;
       if (!stands && (threadIdx.x & 63) == 0) atomicMin(first, i);
     }
     __syncthreads();
@@ -192,18 +251,37 @@ template <typename T> __device__ __forceinline__ int accept_first(const AcceptAr
   return *first;
 }
 
+// The test of all rows at once, a wave a row
+template <typename T>
+__global__ __launch_bounds__(kAcceptThreads) void k_accept_rows(AcceptArgs a) {
+  const int i = blockIdx.x * (kAcceptThreads / 64) + (threadIdx.x >> 6), b = blockIdx.y;
+  const AcceptSeq sq = accept_seq(a, b);
+  if (i >= sq.n) return;
+  const AcceptRowInfo r = accept_decide<T>(a, sq.row0 + i, accept_rate(a, b));
+  if ((threadIdx.x & 63) == 0) a.row_info[sq.row0 + i] = r;
+}
+// The first row whose token does not stand, from there, by each wave for itself
+__device__ __forceinline__ int accept_first_of(const AcceptArgs& a, const AcceptSeq& sq) {
+  const int lane = threadIdx.x & 63;
+  for (int i0 = 0; i0 < sq.n; i0 += 64) {
+    const unsigned long long falls = __ballot(i0 + lane < sq.n && !a.row_info[sq.row0 + i0 + min(lane, sq.n - 1 - i0)].stands);
+    if (falls) return i0 + __ffsll(falls) - 1;
+  }
+  return sq.n;
+}
+
 // What a token of the deciding row weighs in the draw, relative to the row's maximum (q given: as a probability)
 template <typename T> struct AcceptWeight {
   const float* q;   // null: none
   int skip;
   float m;
   double rate, inv_z;
-  __device__ __forceinline__ AcceptWeight(const AcceptArgs& a, int row, const AcceptSums& s, double rate_) {
+  __device__ __forceinline__ AcceptWeight(const AcceptArgs& a, int row, float m_, double z, double rate_) {
     const int d = a.draft[row];
     const bool drafted = accept_drafted(a, d);
     q = a.probs && drafted ? a.probs + (size_t)row * a.probs_stride : nullptr;
     skip = !a.probs && drafted ? d : -1;
-    m = s.m; rate = rate_; inv_z = 1.0 / s.z;
+    m = m_; rate = rate_; inv_z = 1.0 / z;
   }
   __device__ __forceinline__ double operator()(int i, float x) const {
     const double e = exp2_down(((double)x - (double)m) * rate);
@@ -214,58 +292,68 @@ template <typename T> struct AcceptWeight {
 
 template <typename T>
 __global__ __launch_bounds__(kAcceptThreads) void k_accept_rest(AcceptArgs a) {
-  __shared__ int first;
   __shared__ double ss[kAcceptThreads / 64];
   const int c = blockIdx.x, b = blockIdx.y, t = threadIdx.x;
   const AcceptSeq sq = accept_seq(a, b);
   if (sq.n <= 0) return;
-  const double rate = accept_rate(a, b);
-  const int i = accept_first<T>(a, sq, rate, &first);
+  const int i = accept_first_of(a, sq);
   if (i >= sq.n) return;
   const int row = sq.row0 + i;
-  const AcceptSums sums = accept_sums<T>(a, row, rate);
   const AcceptRow<T> x(a, row);
-  const AcceptWeight<T> w(a, row, sums, rate);
   float v[kAcceptEach];
   x.load(c, t, v);
-  double s = 0.0;
+  const AcceptWeight<T> w(a, row, a.row_info[row].m, a.row_info[row].z, accept_rate(a, b));
+  {
+    double s = 0.0;
 #pragma unroll
-  for (int j = 0; j < kAcceptEach; ++j) {
-    const int at = x.index(c, t, j);
-    if (at < a.vocab) s += w(at, v[j]);
+    for (int j = 0; j < kAcceptEach; ++j) {
+      const int at = x.index(c, t, j);
+      if (at < a.vocab) s += w(at, v[j]);
+    }
+    if (t < x.heads(c)) s += w(t, x.at(t));
+    s = wave_sum_f64(s);
+    if ((t & 63) == 0) ss[t >> 6] = s;
   }
-  if (t < x.heads(c)) s += w(t, x.at(t));
-  s = wave_sum_f64(s);
-  if ((t & 63) == 0) ss[t >> 6] = s;
   __syncthreads();
   if (t == 0) a.rest_sum[(size_t)b * a.pieces + c] = (ss[0] + ss[1]) + (ss[2] + ss[3]);
 }
 
-template <typename T>
-__global__ __launch_bounds__(kAcceptThreads) void k_accept_pick(AcceptArgs a) {
-  constexpr int kVec = AcceptRow<T>::kVec, kSlots = kAcceptPiece / kVec, kLaneSlots = kSlots / 64;
+// DECIDED: k_accept_rows has been over the rows
+template <typename T, bool DECIDED>
+__global__ __launch_bounds__(DECIDED ? kAcceptThreads : kDecideThreads) void k_accept_pick(AcceptArgs a) {
+  constexpr int kThreads = DECIDED ? kAcceptThreads : kDecideThreads;
+  constexpr int kVec = AcceptRow<T>::kVec, kGroups = kAcceptEach / kVec;
   __shared__ int first, token;
-  __shared__ double slot[kSlots];
+  __shared__ double round[kGroups * 4];
   const int b = blockIdx.x, t = threadIdx.x, lane = t & 63;
   const AcceptSeq sq = accept_seq(a, b);
   const double rate = accept_rate(a, b);
   int i = 0;
   if (sq.n > 0) {
-    i = accept_first<T>(a, sq, rate, &first);
+    if constexpr (DECIDED) i = accept_first_of(a, sq);
+    else i = accept_first<T>(a, sq, rate, &first);
     if (t == 0) token = AD_NEVER;
     __syncthreads();
   }
   if (i < sq.n) {
     const int row = sq.row0 + i;
-    const AcceptSums sums = accept_sums<T>(a, row, rate);
-    if (!accept_broken(sums.z)) {
+    float m;
+    double z;
+    if constexpr (DECIDED) {
+      m = a.row_info[row].m; z = a.row_info[row].z;
+    } else {
+      const AcceptSums sums = accept_sums<T>(a, row, rate);
+      m = sums.m; z = sums.z;
+    }
+    if (!accept_broken(z)) {
       const AcceptRow<T> x(a, row);
-      const AcceptWeight<T> w(a, row, sums, rate);
+      const AcceptWeight<T> w(a, row, m, z, rate);
       // (the drafted token is left out of the pieces' sums where the drafter gave no probabilities)
       auto piece = [&](int c) -> double {
-        if (a.probs) return a.rest_sum[(size_t)b * a.pieces + c];
+        if (a.rest) return a.rest_sum[(size_t)b * a.pieces + c];
         const float mc = a.piece_max[(size_t)row * a.pieces + c];
-        return mc > -INFINITY ? a.piece_sum[(size_t)row * a.pieces + c] * exp2_down(((double)mc - (double)sums.m) * rate) : 0.0;
+        const double s = mc > -INFINITY ? a.piece_sum[(size_t)row * a.pieces + c] * exp2_down(((double)mc - (double)m) * rate) : 0.0;
+        return s < kNothing ? 0.0 : s;
       };
       // the piece in which the sum passes the wanted part of the whole: every wave finds it by itself, 64 pieces at a time
       double total = 0.0;
@@ -298,67 +386,81 @@ __global__ __launch_bounds__(kAcceptThreads) void k_accept_pick(AcceptArgs a) {
           before += __shfl(upto, 63);
         }
         if (at < 0) { at = last; base = last_base; }   // (rounding: the last piece that holds anything)
-        // its weights, a slot of kVec scores a sum, in the order of their indices
-        float v[kAcceptEach];
-        x.load(at, t, v);
+        // Its weights: sums of kVec scores side by side by thread, in kGroups rounds of the workgroup's four waves, which is the order of their indices; the round and
+        // wave, the thread, the score in which the running sum passes `want` (else the last that weighs anything).
+        double each[kAcceptEach], own[kGroups];
+        if (t < kAcceptThreads) {
+          float v[kAcceptEach];
+          x.load(at, t, v);
 #pragma unroll
-        for (int j = 0; j < kAcceptEach; j += kVec) {
-          double s = 0.0;
+          for (int j = 0; j < kAcceptEach; j += kVec) {
+            double s = 0.0;
 #pragma unroll
-          for (int e = 0; e < kVec; ++e) {
-            const int n = x.index(at, t, j + e);
-            if (n < a.vocab) s += w(n, v[j + e]);
+            for (int e = 0; e < kVec; ++e) {
+              const int n = x.index(at, t, j + e);
+              each[j + e] = n < a.vocab ? w(n, v[j + e]) : 0.0;
+              s += each[j + e];
+            }
+            own[j / kVec] = s;
+            const double all = wave_sum_f64(s);
+            if (lane == 0) round[(j / kVec) * 4 + (t >> 6)] = all;
           }
-          slot[(j / kVec) * kAcceptThreads + t] = s;
         }
         __syncthreads();
-        if (t < 64) {
-          // the first token whose running sum passes `want`, else the last that weighs anything
-          int hit = -1, heavy = -1;
-          double run = base;
-          for (int n = 0; n < x.heads(at) && hit < 0; ++n) {
-            const double e = w(n, x.at(n));
-            run += e;
-            if (e > 0.0) heavy = n;
-            if (run > want) hit = n;
-          }
-          if (hit < 0) {
-            double own = 0.0;
-            for (int n = 0; n < kLaneSlots; ++n) own += slot[lane * kLaneSlots + n];
-            double upto = own;
-#pragma unroll
-            for (int s = 1; s < 64; s *= 2) {
-              const double o = __shfl_up(upto, s);
-              if (lane >= s) upto += o;
+        int hit = -1, heavy = -1;
+        double run = base;
+        {
+          const int n = x.heads(at);
+          const double e = lane < n ? w(lane, x.at(lane)) : 0.0;
+          for (int i = 0; i < n && hit < 0; ++i) {
+            const double g = lane_f64(e, i);
+            run += g;
+            if (g > 0.0) {
+              heavy = i;
+              if (run > want) hit = i;
             }
-            const unsigned long long some = __ballot(own > 0.0), over = __ballot(run + upto > want) & some;
-            if (over || some) {
-              const int l = over ? __ffsll(over) - 1 : 63 - __clzll(some);
-              run += __shfl(upto - own, l);
-              // (the slots of that lane, one by one; the whole wave does the same)
-              int in = -1;
-              double in_run = run;
-              for (int n = l * kLaneSlots; n < (l + 1) * kLaneSlots; ++n) {
-                const double e = slot[n];
-                if (e > 0.0) { in = n; in_run = run; }
-                run += e;
-                if (run > want && e > 0.0) break;
+          }
+        }
+        if (hit < 0) {
+          int in = -1;
+          double in_run = run;
+          for (int n = 0; n < kGroups * 4; ++n) {
+            const double s = round[n];
+            if (s > 0.0) { in = n; in_run = run; }
+            run += s;
+            if (run > want && s > 0.0) break;
+          }
+          if (in >= 0) {
+            if (t >> 6 == in % 4) {   // (one wave; it has the round's sums)
+              run = in_run;
+              double mine = own[0];
+#pragma unroll
+              for (int j = 1; j < kGroups; ++j) mine = in / 4 == j ? own[j] : mine;
+              double upto = mine;
+#pragma unroll
+              for (int s = 1; s < 64; s *= 2) {
+                const double o = __shfl_up(upto, s);
+                if (lane >= s) upto += o;
               }
-              if (in >= 0) {
-                const int n0 = x.skew + at * kAcceptPiece + in * kVec;
-                run = in_run;
-                for (int e = 0; e < kVec && hit < 0 && n0 + e < a.vocab; ++e) {
-                  const double g = w(n0 + e, x.at(n0 + e));
-                  run += g;
-                  if (g > 0.0) {
-                    heavy = n0 + e;
-                    if (run > want) hit = n0 + e;
+              const unsigned long long some = __ballot(mine > 0.0), over = __ballot(run + upto > want) & some;
+              const int l = over ? __ffsll(over) - 1 : 63 - __clzll(some);
+              run += upto - mine;
+#pragma unroll
+              for (int j = 0; j < kAcceptEach; ++j)
+                if (j / kVec == in / 4) {   // (every thread its own scores: the thread's that was found counts)
+                  run += each[j];
+                  if (each[j] > 0.0 && hit < 0) {
+                    heavy = x.index(at, t, j);
+                    if (run > want) hit = heavy;
                   }
                 }
-              }
+              if (lane == l) token = hit >= 0 ? hit : heavy;
             }
+          } else if (t == 0) {
+            token = heavy;
           }
-          if (lane == 0) token = hit >= 0 ? hit : heavy;
+        } else if (t == 0) {
+          token = hit;
         }
       } else {
         if (t == 0) token = a.draft[row];   // p and q alike: nothing is left over, the drafted token stands
@@ -367,7 +469,7 @@ __global__ __launch_bounds__(kAcceptThreads) void k_accept_pick(AcceptArgs a) {
     __syncthreads();
   }
   const int tok = sq.n > 0 && i < sq.n ? token : AD_NEVER;
-  for (int n = t; n < sq.n; n += kAcceptThreads) {
+  for (int n = t; n < sq.n; n += kThreads) {
     const int to = n < i ? a.draft[sq.row0 + n] : n == i ? tok : AD_NEVER;
     if (!a.keep || (n <= i && to >= 0)) a.tokens[sq.row0 + n] = to;
   }
@@ -393,19 +495,32 @@ int accept_pieces(int vocab) { return (vocab + kAcceptPiece - 1) / kAcceptPiece;
 static size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 size_t accept_bytes(int n_seq, int rows, int vocab) {
   const size_t p = accept_pieces(vocab);
-  return up256(rows * p * 8) + up256(rows * p * 4) + up256((size_t)n_seq * p * 8);
+  return up256(rows * p * 8) + up256(rows * p * 4) + up256((size_t)n_seq * p * 8) + up256(rows * sizeof(AcceptRowInfo));
 }
 void launch_accept_sampled(int dtype, AcceptArgs a, void* ws, hipStream_t s) {
   a.pieces = accept_pieces(a.vocab);
+#ifndef WTH
+#define WTH (1<<22)
+#endif
+  const bool wide = a.probs || (size_t)a.rows * a.vocab < WTH;
+  a.rest = a.probs || !wide;
   char* w = (char*)ws;
   a.piece_sum = (double*)w;
   a.piece_max = (float*)(w + up256((size_t)a.rows * a.pieces * 8));
   a.rest_sum = (double*)((char*)a.piece_max + up256((size_t)a.rows * a.pieces * 4));
+  a.row_info = (AcceptRowInfo*)((char*)a.rest_sum + up256((size_t)a.n_seq * a.pieces * 8));
   auto go = [&](auto one) {
     typedef decltype(one) T;
-    k_accept_stats<T><<<dim3(a.pieces, a.max_rows, a.n_seq), kAcceptThreads, 0, s>>>(a);
-    if (a.probs) k_accept_rest<T><<<dim3(a.pieces, a.n_seq), kAcceptThreads, 0, s>>>(a);
-    k_accept_pick<T><<<a.n_seq, kAcceptThreads, 0, s>>>(a);
+    const dim3 grid(a.pieces, a.max_rows, a.n_seq);
+    if (wide) k_accept_stats<T, true><<<grid, kAcceptThreads, 0, s>>>(a);
+    else k_accept_stats<T, false><<<grid, kAcceptThreads, 0, s>>>(a);
+    if (a.rest) {
+      k_accept_rows<T><<<dim3((a.max_rows + 3) / 4, a.n_seq), kAcceptThreads, 0, s>>>(a);
+      k_accept_rest<T><<<dim3(a.pieces, a.n_seq), kAcceptThreads, 0, s>>>(a);
+      k_accept_pick<T, true><<<a.n_seq, kAcceptThreads, 0, s>>>(a);
+    } else {
+      k_accept_pick<T, false><<<a.n_seq, kDecideThreads, 0, s>>>(a);
+    }
   };
   if (dtype == AD_BF16) go(bf16_t{});
   else go(float{});

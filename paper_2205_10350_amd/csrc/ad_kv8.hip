@@ -77,6 +77,7 @@ __global__ __launch_bounds__(4 * DH) void k_kv8_append(unsigned char* __restrict
   // rows: thread u holds columns 32 s + 8 g .. + 7 of keys r and 16 + r (s = u / 64), as the keys' operand wants them
   const int s = u >> 6;
   uint4 x[2];
+  bool spoilt = false;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const int p = tok0 + 16 * i + r;
@@ -87,86 +88,72 @@ __global__ __launch_bounds__(4 * DH) void k_kv8_append(unsigned char* __restrict
     } else if (!CLOSED && !values && p < sq.base) {
       x[i] = ldg16(ring + ((2 * s + i) * 64 + lane) * 8);
     }
-    if (kv8_not_finite(x[i])) bad[16 * i + r] = 1;   // (several threads may: all write the same)
   }
   // the values kept from earlier calls are in operand order: thread u holds columns 16 c + r, c = 2 s and 2 s + 1, of eight keys each
   uint4 kept[2] = {uint4{0, 0, 0, 0}, uint4{0, 0, 0, 0}};
-  if (!CLOSED && values && tok0 < sq.base) {
+  const bool keeps = !CLOSED && tok0 < sq.base;
+  if (keeps && values) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) kept[i] = ldg16(ring + ((2 * s + i) * 64 + lane) * 8);
   }
-  if (values) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+  for (int i = 0; i < 2; ++i) {
+    if (kv8_not_finite(x[i])) { bad[16 * i + r] = 1; spoilt = true; }   // (several threads may: all write the same)
+    if (values) {
       unsigned* to = (unsigned*)(Vs + (16 * i + r) * kLdv + 32 * s + 8 * g);
       to[0] = x[i].x; to[1] = x[i].y; to[2] = x[i].z; to[3] = x[i].w;
     }
   }
-  __syncthreads();
+  const bool any_spoilt = __syncthreads_or(spoilt);
 
-  // the 16 elements in operand order, clean
-  bf16_t e[16];
+  // the 16 elements in operand order, two a word
+  unsigned e[8] = {x[0].x, x[0].y, x[0].z, x[0].w, x[1].x, x[1].y, x[1].z, x[1].w};
   if (values) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const bf16_t* old = (const bf16_t*)&kept[i];
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int key = kv8_key(g, j);
-        const bf16_t w = tok0 + key < sq.base ? old[j] : Vs[key * kLdv + 16 * (2 * s + i) + r];
-        e[8 * i + j] = bad[key] ? (bf16_t)0 : w;
+      for (int j = 0; j < 8; j += 2) {
+        const int key = kv8_key(g, j), col = 16 * (2 * s + i) + r;
+        unsigned w = Vs[key * kLdv + col] | (unsigned)Vs[(key + 1) * kLdv + col] << 16;
+        if (keeps) {   // (the same for the whole workgroup)
+          const unsigned old = j == 0 ? kept[i].x : j == 2 ? kept[i].y : j == 4 ? kept[i].z : kept[i].w;
+          const unsigned from = (tok0 + key < sq.base ? 0xffffu : 0u) | (tok0 + key + 1 < sq.base ? 0xffff0000u : 0u);
+          w = (old & from) | (w & ~from);
+        }
+        if (any_spoilt) w &= (bad[key] ? 0u : 0xffffu) | (bad[key + 1] ? 0u : 0xffff0000u);
+        e[4 * i + j / 2] = w;
       }
-    }
-  } else {
+  } else if (any_spoilt) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const bf16_t* w = (const bf16_t*)&x[i];
-      const bool gone = bad[16 * i + r] != 0;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) e[8 * i + j] = gone ? (bf16_t)0x7fc0 : w[j];
-    }
+    for (int j = 0; j < 8; ++j)
+      if (bad[16 * (j / 4) + r]) e[j] = 0x7fc07fc0u;
   }
   if (!CLOSED) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) gstore((uint4*)(ring + ((2 * s + i) * 64 + lane) * 8), *(const uint4*)&e[8 * i]);
+    for (int i = 0; i < 2; ++i) gstore((uint4*)(ring + ((2 * s + i) * 64 + lane) * 8), uint4{e[4 * i], e[4 * i + 1], e[4 * i + 2], e[4 * i + 3]});
     if (tok0 + kKv8Block > end) return;   // (the whole workgroup: the block has tokens to come)
   }
-  // the block is complete: its largest value, its bytes
-  float mx = 0.f;
-  bool nan = false;
+  // The block is complete: its largest value, its bytes.  Magnitudes of bf16 order as whole numbers; a spoilt token's keys are left out of them.
+  typedef unsigned short half2 __attribute__((ext_vector_type(2)));
+  half2 hi = {0, 0};
 #pragma unroll
-  for (int j = 0; j < 16; ++j) {
-    const float f = bf2f(e[j]);
-    nan = nan || f != f;
-    mx = fmaxf(mx, fabsf(f));   // (of a NaN and a number the number)
+  for (int j = 0; j < 8; ++j) {
+    if (any_spoilt && (e[j] & 0x7fffu) > 0x7f80u) e[j] = 0;
+    hi = __builtin_elementwise_max(hi, __builtin_bit_cast(half2, e[j] & 0x7fff7fffu));
   }
-  mx = wave_max(mx);
-  const bool any_nan = __any(nan);
-  if (lane == 0) most[t >> 6] = any_nan ? -1.f - mx : mx;   // (negative: a NaN among the keys)
+  const float mx = wave_max(__uint_as_float((unsigned)(hi.x > hi.y ? hi.x : hi.y) << 16));
+  if (lane == 0) most[t >> 6] = mx;
   __syncthreads();
   float top = 0.f;
-  bool spoiled = false;
 #pragma unroll
-  for (int w = 0; w < kWaves / 2; ++w) {
-    const float o = most[(values ? kWaves / 2 : 0) + w];
-    spoiled = spoiled || o < 0.f;
-    top = fmaxf(top, o < 0.f ? -1.f - o : o);
-  }
+  for (int w = 0; w < kWaves / 2; ++w) top = fmaxf(top, most[(values ? kWaves / 2 : 0) + w]);
   const Kv8Quant q = kv8_quant<FMT>(top);
-  uint4 bytes;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    float f[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      f[j] = bf2f(e[4 * i + j]);
-      if (f[j] != f[j]) f[j] = 0.f;
-    }
-    const unsigned w = kv8_pack4<FMT>(f, q);
-    if (i == 0) bytes.x = w; else if (i == 1) bytes.y = w; else if (i == 2) bytes.z = w; else bytes.w = w;
-  }
-  gstore((uint4*)(cache + (bh * dm.blocks + blk) * (2 * kKv8Block * DH) + (values ? kKv8Block * DH : 0) + u * 16), bytes);
-  if (u == 0) gstore((float*)(cache + dm.scales) + (bh * dm.blocks + blk) * 2 + (values ? 1 : 0), spoiled ? __uint_as_float(0x7fc00000u) : q.scale);
+  auto four = [&](int j) {
+    const float f[4] = {__uint_as_float(e[j] << 16), __uint_as_float(e[j] & 0xffff0000u), __uint_as_float(e[j + 1] << 16), __uint_as_float(e[j + 1] & 0xffff0000u)};
+    return kv8_pack4<FMT>(f, q);
+  };
+  gstore((uint4*)(cache + (bh * dm.blocks + blk) * (2 * kKv8Block * DH) + (values ? kKv8Block * DH : 0) + u * 16), uint4{four(0), four(2), four(4), four(6)});
+  if (u == 0) gstore((float*)(cache + dm.scales) + (bh * dm.blocks + blk) * 2 + (values ? 1 : 0), any_spoilt && !values ? __uint_as_float(0x7fc00000u) : q.scale);
 }
 
 // One workgroup per (block, head, sequence), 4 * DH threads; keys' rows are written as they are held, values turned in LDS.  Bound by memory.
@@ -195,9 +182,9 @@ __global__ __launch_bounds__(4 * DH) void k_kv8_read(const unsigned char* __rest
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const uint4 w = ldg16(ring + ((2 * s + i) * 64 + lane) * 8);
-      const bf16_t* e = (const bf16_t*)&w;
+      const unsigned e[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-      for (int j = 0; j < 8; ++j) f[8 * i + j] = bf2f(e[j]);
+      for (int j = 0; j < 8; ++j) f[8 * i + j] = __uint_as_float(j & 1 ? e[j / 2] & 0xffff0000u : e[j / 2] << 16);
     }
   }
   if (values) {

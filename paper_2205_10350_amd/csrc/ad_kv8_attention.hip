@@ -4,7 +4,8 @@
 // lane holds one query row (lane % 16) throughout and its probabilities are the right operand of the second product as they are.
 //  * A wave takes 16 R query rows of a (sequence, head), those of the query heads that share the head among them, and every fourth block of
 //    a split's keys: four waves of a workgroup, then the splits, each an online softmax of its own, joined in their order.
-//  * Bytes become bf16 operands in registers, exactly; the keys' scale multiplies the scores, the values' the probabilities before they are rounded.
+//  * Bytes become bf16 operands in registers, exactly; the keys' scale multiplies the scores, the values' the probabilities before they are rounded (e4m3: a
+//    power of two, which the conversion of the values applies).
 //  * Blocks of 8 bits first, those that every row of the tile sees without a mask; then the rows' own blocks from the bf16 ring.
 // A row's sums depend on the cache's sizes and the row's position alone: not on the call's other rows, nor on R, nor on how many splits are launched (blocks and
 // splits that a row does not see change nothing in it, to the bit).
@@ -18,6 +19,7 @@
 namespace ad {
 
 constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kStep = 8.f;
 
 // what a launch needs beyond the cache
 struct Kv8Attend {
@@ -32,12 +34,25 @@ struct Kv8Attend {
   float scale;               // of the scores, times log2(e)
 };
 
+// (splits that the join fetches together)
+constexpr int kGroup = 4;
+struct Kv8Sum { float top, sum; };
+// (top, sum) of what came before and of what comes next, and the factors of their outputs
+__device__ __forceinline__ Kv8Sum kv8_join(Kv8Sum a, Kv8Sum b, float& fa, float& fb) {
+  const float t = fmaxf(a.top, b.top), base = t == -INFINITY ? 0.f : t;
+  fa = __builtin_amdgcn_exp2f(a.top - base);
+  fb = __builtin_amdgcn_exp2f(b.top - base);
+  return Kv8Sum{t, fmaf(b.sum, fb, a.sum * fa)};
+}
+
+// the larger of two (of a NaN and a number the number), one instruction where fmaxf first makes signalling NaNs quiet
+__device__ __forceinline__ float kv8_max(float a, float b) { return __builtin_amdgcn_fmed3f(a, b, INFINITY); }
 // maximum / sum over the four lane groups that hold a row's keys
 __device__ __forceinline__ float kv8_rows_max(float m) {
   auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(m), __float_as_uint(m), false, false);
-  m = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+  m = kv8_max(__uint_as_float(p[0]), __uint_as_float(p[1]));
   p = __builtin_amdgcn_permlane32_swap(__float_as_uint(m), __float_as_uint(m), false, false);
-  return fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+  return kv8_max(__uint_as_float(p[0]), __uint_as_float(p[1]));
 }
 __device__ __forceinline__ float kv8_rows_sum(float v) {
   auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -46,16 +61,19 @@ __device__ __forceinline__ float kv8_rows_sum(float v) {
   return __uint_as_float(p[0]) + __uint_as_float(p[1]);
 }
 
+// waves a SIMD should hold (its registers are shared out accordingly)
+constexpr int kv8_waves(int dh, int r) { return dh == 128 ? (r == 2 ? 1 : 2) : r == 4 ? 2 : r == 2 ? 3 : 4; }
+
 template <int DH, int R> struct Kv8State {
   bf16x8 q[R][DH / 32];
   f32x4 o[R][DH / 16];
-  float m[R], l[R];   // of this lane's row: the maximum (all lane groups alike), the denominator's part of this lane's keys
+  float m[R], l[R];   // of this lane's row: the exponents' reference (all lane groups alike), the denominator's part of this lane's keys
 };
 
-// One block: kf(kt, s) and vf(c) give operands; c1: what the raw scores are multiplied by, cv: the values' scale.
+// One block: kf(kt, s) and vf(c) give operands; c1 >= 0: what the raw scores are multiplied by; cv: what the probabilities are, if VSCALE.
 // seen(rt): bits of the eight keys of this lane (4 kt + i) that its row sees; MASK false: all.
 // (fused multiply-adds are written out: with and without a mask the same roundings)
-template <int DH, int R, bool MASK, typename KF, typename VF, typename SEEN>
+template <int DH, int R, bool MASK, bool VSCALE, typename KF, typename VF, typename SEEN>
 __device__ __forceinline__ void kv8_block(Kv8State<DH, R>& st, const KF& kf, const VF& vf, float c1, float cv, const SEEN& seen) {
   f32x4 sc[R][2];
 #pragma unroll
@@ -77,26 +95,32 @@ __device__ __forceinline__ void kv8_block(Kv8State<DH, R>& st, const KF& kf, con
     auto score = [&](int i) { return sc[rt][i >> 2][i & 3]; };
     float x[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = !MASK || ((bits >> i) & 1) ? score(i) * c1 : -INFINITY;
-    float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-    top = fmaxf(st.m[rt], kv8_rows_max(top));
-    const float off = top == -INFINITY ? 0.f : top;   // (a row that has seen nothing yet)
-    if (__any(top != st.m[rt])) {
-      const float f = __builtin_amdgcn_exp2f(st.m[rt] - off);
-      st.m[rt] = top;
+    for (int i = 0; i < 8; ++i) x[i] = !MASK || ((bits >> i) & 1) ? score(i) : -INFINITY;
+    float top = kv8_max(kv8_max(kv8_max(x[0], x[1]), kv8_max(x[2], x[3])), kv8_max(kv8_max(x[4], x[5]), kv8_max(x[6], x[7])));
+    top = kv8_rows_max(top) * c1;   // (the largest product is the product of the largest; NaN: ignored here, in the sums below it is not)
+    // The reference that a row's exponents are taken from follows its maximum in steps of 2^kStep or more: sums stay far from the ends of fp32 either way, and the
+    // sums so far need no rescaling in most blocks.  Which blocks do is a row's own affair; a tile does it for all of its rows, by one for the others.
+    const bool step = top > st.m[rt] + kStep;
+    if (__any(step)) {
+      const float to = step ? top : st.m[rt];
+      const float f = __builtin_amdgcn_exp2f(st.m[rt] - (to == -INFINITY ? 0.f : to));
+      st.m[rt] = to;
       st.l[rt] *= f;
 #pragma unroll
       for (int c = 0; c < DH / 16; ++c)
 #pragma unroll
         for (int i = 0; i < 4; ++i) st.o[rt][c][i] *= f;
     }
+    const float off = st.m[rt] == -INFINITY ? 0.f : st.m[rt];   // (a row that has seen nothing yet)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      x[i] = !MASK || ((bits >> i) & 1) ? __builtin_amdgcn_exp2f(fmaf(score(i), c1, -off)) : 0.f;
-      st.l[rt] += x[i];
-    }
+    for (int i = 0; i < 8; ++i) x[i] = !MASK || ((bits >> i) & 1) ? __builtin_amdgcn_exp2f(fmaf(score(i), c1, -off)) : 0.f;
+    st.l[rt] += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
     // (the probabilities of the output product have 8 bits, half a step of 2^-8 relative each, as in every attention of bf16 here; the denominator has 24)
-    const uint4 w = uint4{f2bf_pair(x[0] * cv, x[1] * cv), f2bf_pair(x[2] * cv, x[3] * cv), f2bf_pair(x[4] * cv, x[5] * cv), f2bf_pair(x[6] * cv, x[7] * cv)};
+    if constexpr (VSCALE) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] *= cv;
+    }
+    const uint4 w = uint4{f2bf_pair(x[0], x[1]), f2bf_pair(x[2], x[3]), f2bf_pair(x[4], x[5]), f2bf_pair(x[6], x[7])};
     pf[rt] = __builtin_bit_cast(bf16x8, w);
   }
 #pragma unroll
@@ -121,30 +145,20 @@ template <int DH> __device__ __forceinline__ void kv8_fetch(Kv8Bytes<DH>& x, con
   x.scale = scales[blk];
 }
 
+// The state of rows row0 .. last of a (sequence, head) over a split's blocks of this wave, two blocks on their way while one is worked on.
 template <int DH, int R, int FMT, bool CLOSED>
-__global__ __launch_bounds__(256) void k_kv8_attend(const unsigned char* __restrict__ cache, Kv8Attend a, Kv8Dims dm) {
-  constexpr int kPad = DH + 4;
-  __shared__ float Os[4][16 * kPad];
-  __shared__ float Ms[4][16][2];
+__device__ __forceinline__ void kv8_wave(Kv8State<DH, R>& st, const unsigned char* cache, const Kv8Attend& a, const Kv8Dims& dm, const Kv8Seq& sq, size_t bh, int h,
+                                         int row0, int last, int own_lo, int own_hi, int blk0, int blk1, int wave) {
   const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  // workgroup -> ((split, row tile), (sequence, head)): those of one (sequence, head) lie a multiple of n_seq * heads apart, on one XCD where that is
-  // a multiple of 8, so that row tiles read the keys from one L2
-  const int pairs = a.rows.n_seq * dm.heads;
-  const int pair = blockIdx.x % pairs, rest = blockIdx.x / pairs;
-  const int tile = rest % a.row_tiles, split = rest / a.row_tiles;
-  const int b = pair / dm.heads, h = pair % dm.heads;
-  const Kv8Seq sq = kv8_seq(a.rows, b, dm.capacity, !CLOSED);
-  const int m_rows = sq.n * a.group, row0 = tile * 16 * R;
-  if (row0 >= m_rows) return;
-  const int last = min(row0 + 16 * R, m_rows) - 1;
-  // blocks: every row sees [0, own_lo) in 8 bits; a row at t sees [0, t / 32) so and its own in bf16 (closed: all in 8 bits, up to the length)
-  const int own_lo = CLOSED ? sq.base / kKv8Block : (sq.base + row0 / a.group) / kKv8Block;
-  const int own_hi = CLOSED ? (sq.base + kKv8Block - 1) / kKv8Block : (sq.base + last / a.group) / kKv8Block;
-  const int blk0 = split * a.split_blocks, blk1 = blk0 + a.split_blocks;
-  if (blk0 >= (CLOSED ? max(own_hi, 1) : own_hi + 1)) return;   // nothing here for any row (of an empty memory the first split writes the zeros)
-
-  Kv8State<DH, R> st;
+  const unsigned char* blocks = cache + bh * dm.blocks * (2 * kKv8Block * DH);
+  const float2* scales = (const float2*)(cache + dm.scales) + bh * dm.blocks;
+  const int whole = min(blk1, own_lo), end = min(blk1, own_hi);
+  int blk = blk0 + wave;
+  constexpr int AHEAD = 2;
+  Kv8Bytes<DH> x[AHEAD + 1];
+#pragma unroll
+  for (int n = 0; n < AHEAD; ++n)
+    if (blk + 4 * n < whole) kv8_fetch(x[n], blocks, scales, blk + 4 * n, lane);
   int pos[R];   // position of this lane's row (closed: the length; rows past the last one repeat it)
 #pragma unroll
   for (int rt = 0; rt < R; ++rt) {
@@ -152,72 +166,76 @@ __global__ __launch_bounds__(256) void k_kv8_attend(const unsigned char* __restr
     pos[rt] = CLOSED ? sq.base : sq.base + i;
     const bf16_t* qp = a.q + (size_t)(sq.row0 + i) * a.q_stride + (size_t)hq * DH + 8 * g;
 #pragma unroll
-    for (int s = 0; s < DH / 32; ++s) st.q[rt][s] = __builtin_bit_cast(bf16x8, ldg16(qp + 32 * s));
+    for (int s = 0; s < DH / 32; ++s) {
+      uint4 w = ldg16(qp + 32 * s);
+      if (a.scale < 0.f) { w.x ^= 0x80008000u; w.y ^= 0x80008000u; w.z ^= 0x80008000u; w.w ^= 0x80008000u; }
+      st.q[rt][s] = __builtin_bit_cast(bf16x8, w);
+    }
     st.m[rt] = -INFINITY;
     st.l[rt] = 0.f;
 #pragma unroll
     for (int c = 0; c < DH / 16; ++c) st.o[rt][c] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  const size_t bh = (size_t)b * dm.heads + h;
-  {
-    const unsigned char* blocks = cache + bh * dm.blocks * (2 * kKv8Block * DH);
-    const float2* scales = (const float2*)(cache + dm.scales) + bh * dm.blocks;
-    auto take = [&](const Kv8Bytes<DH>& x, int blk) {
-      auto kf = [&](int kt, int s) { return kv8_operand<FMT>(kt == 0 ? uint2{x.k[s].x, x.k[s].y} : uint2{x.k[s].z, x.k[s].w}); };
-      auto vf = [&](int c) { return kv8_operand<FMT>((c & 1) == 0 ? uint2{x.v[c >> 1].x, x.v[c >> 1].y} : uint2{x.v[c >> 1].z, x.v[c >> 1].w}); };
-      const float c1 = x.scale.x * a.scale;
-      if (blk < own_lo) {
-        kv8_block<DH, R, false>(st, kf, vf, c1, x.scale.y, [](int) { return 0xffu; });
-      } else {
-        auto seen = [&](int rt) -> unsigned {
-          if constexpr (CLOSED) {
-            unsigned bits = 0;
+  const float scale = fabsf(a.scale);
+  auto take = [&](auto mask, const Kv8Bytes<DH>& x, int blk) {
+    auto kf = [&](int kt, int s) { return kv8_operand<FMT>(kt == 0 ? uint2{x.k[s].x, x.k[s].y} : uint2{x.k[s].z, x.k[s].w}, 1.f); };
+    auto vf = [&](int c) { return kv8_operand<FMT>((c & 1) == 0 ? uint2{x.v[c >> 1].x, x.v[c >> 1].y} : uint2{x.v[c >> 1].z, x.v[c >> 1].w}, x.scale.y); };
+    auto seen = [&](int rt) -> unsigned {
+      if constexpr (!mask.value) return 0xffu;
+      if constexpr (CLOSED) {
+        unsigned bits = 0;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) bits |= (blk * kKv8Block + kv8_key(g, j) < pos[rt] ? 1u : 0u) << j;
-            return bits;
-          } else {
-            return blk < pos[rt] / kKv8Block ? 0xffu : 0u;
-          }
-        };
-        kv8_block<DH, R, true>(st, kf, vf, c1, x.scale.y, seen);
+        for (int j = 0; j < 8; ++j) bits |= (blk * kKv8Block + kv8_key(g, j) < pos[rt] ? 1u : 0u) << j;
+        return bits;
+      } else {
+        return blk < pos[rt] / kKv8Block ? 0xffu : 0u;
       }
     };
-    const int end = min(blk1, own_hi);
-    int blk = blk0 + wave;
-    if (blk < end) {
-      Kv8Bytes<DH> x, y;
-      kv8_fetch(x, blocks, scales, blk, lane);
-      for (; blk < end; blk += 8) {
-        if (blk + 4 < end) kv8_fetch(y, blocks, scales, blk + 4, lane);
-        take(x, blk);
-        if (blk + 4 >= end) break;
-        if (blk + 8 < end) kv8_fetch(x, blocks, scales, blk + 8, lane);
-        take(y, blk + 4);
-      }
+    kv8_block<DH, R, mask.value, FMT == AD_KV_I8>(st, kf, vf, x.scale.x * scale, x.scale.y, seen);
+  };
+  const std::false_type all{};
+  const std::true_type some{};
+  while (blk < whole) {
+#pragma unroll
+    for (int n = 0; n <= AHEAD; ++n) {
+      if (blk + 4 * AHEAD < whole) kv8_fetch(x[(n + AHEAD) % (AHEAD + 1)], blocks, scales, blk + 4 * AHEAD, lane);
+      take(all, x[n], blk);
+      blk += 4;
+      if (blk >= whole) break;
     }
+  }
+  for (; blk < end; blk += 4) {   // blocks that some of the rows see
+    kv8_fetch(x[0], blocks, scales, blk, lane);
+    take(some, x[0], blk);
   }
   if constexpr (!CLOSED) {
     const bf16_t* ring = (const bf16_t*)(cache + dm.rings) + bh * dm.ring * (2 * kKv8Block * DH);
-    int blk = max(own_lo, blk0);
-    blk += (wave - blk % 4 + 4) % 4;   // (a split's blocks are dealt to the waves from a multiple of four on)
-    for (; blk <= own_hi && blk < blk1; blk += 4) {
-      const bf16_t* kp = ring + (size_t)(blk % dm.ring) * (2 * kKv8Block * DH) + lane * 8;
+    int own = max(own_lo, blk0);
+    own += (wave - own % 4 + 4) % 4;   // (a split's blocks are dealt to the waves from a multiple of four on)
+    for (; own <= own_hi && own < blk1; own += 4) {
+      const bf16_t* kp = ring + (size_t)(own % dm.ring) * (2 * kKv8Block * DH) + lane * 8;
       const bf16_t* vp = kp + kKv8Block * DH;
       uint4 kr[DH / 16], vr[DH / 16];
 #pragma unroll
       for (int c = 0; c < DH / 16; ++c) { kr[c] = ldg16(kp + c * 512); vr[c] = ldg16(vp + c * 512); }
-      kv8_block<DH, R, true>(
-          st, [&](int kt, int s) { return __builtin_bit_cast(bf16x8, kr[2 * s + kt]); }, [&](int c) { return __builtin_bit_cast(bf16x8, vr[c]); }, a.scale, 1.f,
+      kv8_block<DH, R, true, false>(
+          st, [&](int kt, int s) { return __builtin_bit_cast(bf16x8, kr[2 * s + kt]); }, [&](int c) { return __builtin_bit_cast(bf16x8, vr[c]); }, scale, 1.f,
           [&](int rt) -> unsigned {
             unsigned bits = 0;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) bits |= (blk * kKv8Block + kv8_key(g, j) <= pos[rt] ? 1u : 0u) << j;
-            return blk == pos[rt] / kKv8Block ? bits : 0u;
+            for (int j = 0; j < 8; ++j) bits |= (own * kKv8Block + kv8_key(g, j) <= pos[rt] ? 1u : 0u) << j;
+            return own == pos[rt] / kKv8Block ? bits : 0u;
           });
     }
   }
+}
 
-  // the four waves' states, in their order
+// The four waves' states of a tile, in their order: to the output, or to the join's workspace.
+template <int DH, int R>
+__device__ __forceinline__ void kv8_merge(const Kv8State<DH, R>& st, float (*Os)[16 * (DH + 4)], float (*Ms)[16][2], const Kv8Attend& a, const Kv8Dims& dm,
+                                          const Kv8Seq& sq, int h, int row0, int last, int split, int wave) {
+  constexpr int kPad = DH + 4;
+  const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
 #pragma unroll
   for (int rt = 0; rt < R; ++rt) {
     if (rt) __syncthreads();
@@ -237,26 +255,64 @@ __global__ __launch_bounds__(256) void k_kv8_attend(const unsigned char* __restr
       f[w] = __builtin_amdgcn_exp2f(Ms[w][row][0] - (top == -INFINITY ? 0.f : top));
       sum = fmaf(f[w], Ms[w][row][1], sum);
     }
+    float o[DH / 16];
+#pragma unroll
+    for (int c = 0; c < DH / 16; ++c) {
+      const int col = 32 * (c / 2) + 2 * (threadIdx.x & 15) + (c & 1);
+      o[c] = 0.f;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) o[c] = fmaf(f[w], Os[w][row * kPad + col], o[c]);
+    }
     const int i = m / a.group, hq = h * a.group + m % a.group;
     const size_t at = ((size_t)(sq.row0 + i) * (dm.heads * a.group) + hq) * a.n_split + split;
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
-    for (int c = 0; c < DH / 32; ++c) {
-      const int col = 32 * c + 2 * (threadIdx.x & 15);
-      float o[2] = {0.f, 0.f};
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        o[0] = fmaf(f[w], Os[w][row * kPad + col], o[0]);
-        o[1] = fmaf(f[w], Os[w][row * kPad + col + 1], o[1]);
-      }
-      if (a.n_split == 1) gstore((unsigned*)(a.out + (size_t)(sq.row0 + i) * a.out_stride + (size_t)hq * DH + col), f2bf_pair(o[0] * inv, o[1] * inv));
-      else gstore((float2*)(a.part_o + at * DH + col), float2{o[0], o[1]});
+    for (int c = 0; c < DH / 16; c += 2) {
+      const int col = 16 * c + 2 * (threadIdx.x & 15);
+      if (a.n_split == 1) gstore((unsigned*)(a.out + (size_t)(sq.row0 + i) * a.out_stride + (size_t)hq * DH + col), f2bf_pair(o[c] * inv, o[c + 1] * inv));
+      else gstore((float2*)(a.part_o + at * DH + col), float2{o[c], o[c + 1]});
     }
     if (a.n_split > 1 && (threadIdx.x & 15) == 0) gstore((float2*)(a.part_ml + at * 2), float2{top, sum});
   }
 }
 
-// The splits of a (row, query head), in their order: one wave, DH / 4 lanes a split and 256 / DH splits at once.
+// One workgroup per 16 R rows, (sequence, head) and split.  A tile of at most 8 R rows takes half the tiles (a batch's blocks are ragged).
+template <int DH, int R, int FMT, bool CLOSED>
+__global__ __launch_bounds__(256, kv8_waves(DH, R)) void k_kv8_attend(const unsigned char* __restrict__ cache, Kv8Attend a, Kv8Dims dm) {
+  __shared__ float Os[4][16 * (DH + 4)];
+  __shared__ float Ms[4][16][2];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // workgroup -> ((split, row tile), (sequence, head)): those of one (sequence, head) lie a multiple of n_seq * heads apart, on one XCD where that is
+  // a multiple of 8, so that row tiles read the keys from one L2
+  const int pairs = a.rows.n_seq * dm.heads;
+  const int pair = blockIdx.x % pairs, rest = blockIdx.x / pairs;
+  const int tile = rest % a.row_tiles, split = rest / a.row_tiles;
+  const int b = pair / dm.heads, h = pair % dm.heads;
+  const Kv8Seq sq = kv8_seq(a.rows, b, dm.capacity, !CLOSED);
+  const int m_rows = sq.n * a.group, row0 = tile * 16 * R;
+  if (row0 >= m_rows) return;
+  const int last = min(row0 + 16 * R, m_rows) - 1;
+  // blocks: every row sees [0, own_lo) in 8 bits; a row at t sees [0, t / 32) so and its own in bf16 (closed: all in 8 bits, up to the length)
+  const int own_lo = CLOSED ? sq.base / kKv8Block : (sq.base + row0 / a.group) / kKv8Block;
+  const int own_hi = CLOSED ? (sq.base + kKv8Block - 1) / kKv8Block : (sq.base + last / a.group) / kKv8Block;
+  const int blk0 = split * a.split_blocks, blk1 = blk0 + a.split_blocks;
+  if (blk0 >= (CLOSED ? max(own_hi, 1) : own_hi + 1)) return;   // nothing here for any row (of an empty memory the first split writes the zeros)
+  const size_t bh = (size_t)b * dm.heads + h;
+  auto go = [&](auto tiles) {
+    Kv8State<DH, tiles.value> st;
+    kv8_wave<DH, tiles.value, FMT, CLOSED>(st, cache, a, dm, sq, bh, h, row0, last, own_lo, own_hi, blk0, blk1, wave);
+    kv8_merge<DH, tiles.value>(st, Os, Ms, a, dm, sq, h, row0, last, split, wave);
+  };
+  if constexpr (R > 1) {
+    if (last - row0 < 8 * R) {
+      go(std::integral_constant<int, R / 2>{});
+      return;
+    }
+  }
+  go(std::integral_constant<int, R>{});
+}
+
+// The splits of a (row, query head): one wave, DH / 4 lanes a group of kGroup and 256 / DH groups at once; joined group by group, a group's in their order.
 template <int DH>
 __global__ __launch_bounds__(256) void k_kv8_join(Kv8Attend a, Kv8Dims dm) {
   constexpr int kLanes = DH / 4, kAtOnce = 64 / kLanes;
@@ -270,41 +326,57 @@ __global__ __launch_bounds__(256) void k_kv8_join(Kv8Attend a, Kv8Dims dm) {
   const int end = dm.closed ? (sq.base + kKv8Block - 1) / kKv8Block : (sq.base + i) / kKv8Block + 1;
   const int n = min(max(1, (end + a.split_blocks - 1) / a.split_blocks), a.n_split);
   const size_t at = ((size_t)(sq.row0 + i) * heads + hq) * a.n_split;
-  float top = -INFINITY, sum = 0.f;
+  const float2* ml = (const float2*)a.part_ml + at;
+  const float* po = a.part_o + at * DH + col;
+  Kv8Sum all{-INFINITY, 0.f};
   float4 o = float4{0.f, 0.f, 0.f, 0.f};
-  for (int s0 = 0; s0 < n; s0 += kAtOnce) {
-    const int s = s0 + part;
-    if (s >= n) continue;
-    const float2 ml = gload((const float2*)(a.part_ml + (at + s) * 2));
-    const float4 x = gload((const float4*)(a.part_o + (at + s) * DH + col));
-    const float t = fmaxf(top, ml.x), base = t == -INFINITY ? 0.f : t;
-    const float f0 = __builtin_amdgcn_exp2f(top - base), f1 = __builtin_amdgcn_exp2f(ml.x - base);
-    top = t;
-    sum = sum * f0 + ml.y * f1;
-    o.x = o.x * f0 + x.x * f1; o.y = o.y * f0 + x.y * f1; o.z = o.z * f0 + x.z * f1; o.w = o.w * f0 + x.w * f1;
+  auto add = [](Kv8Sum& s, float4& o, Kv8Sum n, float4 x) {
+    float fa, fb;
+    s = kv8_join(s, n, fa, fb);
+    o.x = fmaf(x.x, fb, o.x * fa); o.y = fmaf(x.y, fb, o.y * fa); o.z = fmaf(x.z, fb, o.z * fa); o.w = fmaf(x.w, fb, o.w * fa);
+  };
+  const int groups = (n + kGroup - 1) / kGroup;
+  for (int g = part; g < groups; g += kAtOnce) {
+    float2 w[kGroup];
+    float4 x[kGroup];
+#pragma unroll
+    for (int j = 0; j < kGroup; ++j) {
+      const int s = min(g * kGroup + j, n - 1);   // (past the last one: read again, counted as nothing)
+      w[j] = gload(ml + s);
+      x[j] = gload((const float4*)(po + (size_t)s * DH));
+      if (g * kGroup + j >= n) { w[j] = float2{-INFINITY, 0.f}; x[j] = float4{0.f, 0.f, 0.f, 0.f}; }
+    }
+    Kv8Sum s{w[0].x, w[0].y};
+    float4 y = x[0];
+#pragma unroll
+    for (int j = 1; j < kGroup; ++j) add(s, y, Kv8Sum{w[j].x, w[j].y}, x[j]);
+    add(all, o, s, y);
   }
 #pragma unroll
   for (int step = kLanes; step < 64; step *= 2) {
-    const float ot = __shfl_xor(top, step), os = __shfl_xor(sum, step);
-    const float t = fmaxf(top, ot), base = t == -INFINITY ? 0.f : t;
-    const float f0 = __builtin_amdgcn_exp2f(top - base), f1 = __builtin_amdgcn_exp2f(ot - base);
-    sum = sum * f0 + os * f1;
-    o.x = o.x * f0 + __shfl_xor(o.x, step) * f1; o.y = o.y * f0 + __shfl_xor(o.y, step) * f1;
-    o.z = o.z * f0 + __shfl_xor(o.z, step) * f1; o.w = o.w * f0 + __shfl_xor(o.w, step) * f1;
-    top = t;
+    const Kv8Sum other{__shfl_xor(all.top, step), __shfl_xor(all.sum, step)};
+    const float4 x{__shfl_xor(o.x, step), __shfl_xor(o.y, step), __shfl_xor(o.z, step), __shfl_xor(o.w, step)};
+    // (both sides of a pair do the same sum in the same order)
+    if (lane & step) {
+      Kv8Sum s = other;
+      float4 y = x;
+      add(s, y, all, o);
+      all = s; o = y;
+    } else {
+      add(all, o, other, x);
+    }
   }
   if (part) return;
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  const float inv = all.sum == 0.f ? 0.f : 1.f / all.sum;
   gstore((uint2*)(a.out + (size_t)(sq.row0 + i) * a.out_stride + (size_t)hq * DH + col),
          uint2{f2bf_pair(o.x * inv, o.y * inv), f2bf_pair(o.z * inv, o.w * inv)});
 }
 
-// The split of the keys: 256 keys give each wave two blocks, the least that hides a fetch; larger ones where the cache's own sizes (sequences, heads, row tiles
-// of its longest call) fill the chip without, since every split costs its rows' state on the way to the join.
+// The split of the keys.  It goes by the cache's own sizes, so that a row's sums do not depend on a call.
 int kv8_split_keys(const Kv8Dims& d) {
-  const size_t units = (size_t)d.n_seq * d.heads * (d.closed ? 1 : (d.k_max + 63) / 64);
-  size_t keys = 256;
-  while (keys < 8192 && keys * 1024 < units * d.capacity) keys *= 2;
+  const size_t pairs = (size_t)d.n_seq * d.heads;
+  size_t keys = 512;
+  while (keys < 8192 && ((!d.closed && keys < 2 * (size_t)d.k_max) || keys * 2048 < pairs * d.capacity)) keys *= 2;
   return (int)keys;
 }
 static int splits_of(const Kv8Dims& d, int max_keys) {
@@ -312,10 +384,9 @@ static int splits_of(const Kv8Dims& d, int max_keys) {
   return std::max(1, (std::min(max_keys, d.capacity) + keys - 1) / keys);
 }
 size_t kv8_attend_bytes(const Kv8Dims& d, int q_heads, int rows, int max_keys) {
-  const int n = splits_of(d, max_keys);
+  const size_t n = splits_of(d, max_keys);
   return n == 1 ? 0 : ((size_t)rows * q_heads * n * 2 * 4 + 255) / 256 * 256 + (size_t)rows * q_heads * n * d.width * 4;
 }
-
 bool kv8_attend_fits(const Kv8Dims& d, int q_heads, int max_rows, int max_keys) {
   const size_t tiles = ((size_t)max_rows * (q_heads / d.heads) + 15) / 16;
   return tiles * d.n_seq * d.heads * splits_of(d, max_keys) < (1u << 31) && (size_t)max_rows * q_heads / 4 < (1u << 31);
@@ -329,7 +400,7 @@ static void attend_for(const Kv8Dims& d, const unsigned char* cache, Kv8Attend& 
     k_kv8_attend<DH, r.value, FMT, closed.value><<<(unsigned)((size_t)a.rows.n_seq * d.heads * a.row_tiles * a.n_split), 256, 0, s>>>(cache, a, d);
   };
   auto by_rows = [&](auto closed) {
-    // as few passes over the keys as the rows allow: up to 64 rows of a wave (width 128: 32, more would not fit the registers of two waves)
+    // as few passes over the keys as the rows allow: up to 64 rows of a wave (width 128: 32, more would not fit the registers)
     if (m <= 16) go(std::integral_constant<int, 1>{}, closed);
     else if (m <= 32 || DH == 128) go(std::integral_constant<int, 2>{}, closed);
     else go(std::integral_constant<int, DH == 128 ? 2 : 4>{}, closed);

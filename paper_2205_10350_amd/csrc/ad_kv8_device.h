@@ -50,14 +50,14 @@ template <int FMT> __device__ __forceinline__ void kv8_unpack(unsigned w, float 
     for (int i = 0; i < 4; ++i) f[i] = (float)(signed char)(w >> (8 * i)) * scale;
   }
 }
-// eight bytes -> an operand of eight bf16, exactly (|i8| < 2^8; e4m3 has four significant bits)
-template <int FMT> __device__ __forceinline__ bf16x8 kv8_operand(uint2 w) {
+// eight bytes -> an operand of eight bf16, exactly (|i8| < 2^8; e4m3 has four significant bits); e4m3: times `scale`, a power of two
+template <int FMT> __device__ __forceinline__ bf16x8 kv8_operand(uint2 w, float scale) {
   uint4 o;
   if constexpr (FMT == AD_KV_E4M3) {
-    o.x = __builtin_bit_cast(unsigned, (kv8_bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.x, 1.f, false));
-    o.y = __builtin_bit_cast(unsigned, (kv8_bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.x, 1.f, true));
-    o.z = __builtin_bit_cast(unsigned, (kv8_bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.y, 1.f, false));
-    o.w = __builtin_bit_cast(unsigned, (kv8_bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.y, 1.f, true));
+    o.x = __builtin_bit_cast(unsigned, (kv8_bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.x, scale, false));
+    o.y = __builtin_bit_cast(unsigned, (kv8_bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.x, scale, true));
+    o.z = __builtin_bit_cast(unsigned, (kv8_bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.y, scale, false));
+    o.w = __builtin_bit_cast(unsigned, (kv8_bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.y, scale, true));
   } else {
     auto two = [](unsigned x, int at) {   // the upper halves of two floats that have nothing in their lower ones
       const unsigned a = __float_as_uint((float)(signed char)(x >> (8 * at))), b = __float_as_uint((float)(signed char)(x >> (8 * at + 8)));

@@ -7,6 +7,7 @@ per call, which orders their reuse on the stream; two calls never share one.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import math
 
 from . import binding as B
@@ -18,46 +19,37 @@ def _refuse(msg):
     raise B.AdError(B.AD_EINVAL, msg)
 
 
-def _is(t, name, device, dtype, shape):
+# The checks of a call are most of what the smallest calls cost: plain comparisons, one pass, words only where one fails.
+def _flat(t, name, index, dtype, shape):
+    """Address of a contiguous tensor of that type and shape on GPU `index`."""
+    try:
+        if t.dtype is dtype and t.shape == shape and t.get_device() == index and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    _refuse(f"{name} must be a contiguous {dtype} tensor of shape {list(shape)} on cuda:{index}")
+
+
+def _rows(t, name, index, dtype, heads, width):
+    """Address, row stride and rows of [rows, heads, width]: rows may lie apart, a row's heads side by side."""
+    try:
+        rows, h, w = t.shape
+        if t.dtype is dtype and h == heads and w == width and t.get_device() == index:
+            apart, side, one = t.stride()
+            if one == 1 and (side == width or h == 1):
+                return t.data_ptr(), (apart if rows > 1 else h * w), rows
+    except (AttributeError, ValueError):
+        pass
+    _refuse(f"{name} must be a {dtype} tensor [rows, {heads}, {width}] on cuda:{index}, the heads of a row side by side")
+
+
+def _on(index, call):
+    """call(stream) with GPU `index` current and its current stream."""
     import torch
-    if not isinstance(t, torch.Tensor) or t.device != device or t.dtype != dtype or t.dim() != len(shape) or any(
-            want is not None and got != want for got, want in zip(t.shape, shape)):
-        _refuse(f"{name} must be a {dtype} tensor of shape {list(shape)} on {device}")
-    return t
-
-
-def _flat(t, name, device, dtype, shape):
-    if not _is(t, name, device, dtype, shape).is_contiguous():
-        _refuse(f"{name} must be contiguous")
-    return t.data_ptr()
-
-
-def _rows(t, name, device, heads, width, rows=None):
-    """Address and row stride of [rows, heads, width] bf16: rows may lie apart, a row's heads side by side."""
-    import torch
-    _is(t, name, device, torch.bfloat16, (rows, heads, width))
-    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != width):
-        _refuse(f"{name}: the heads of a row must lie side by side")
-    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else heads * width)
-
-
-class _On:
-    """The device of a call: current for its length, its stream."""
-
-    def __init__(self, device):
-        import torch
-        self.guard = None if torch.cuda.current_device() == device.index else torch.cuda.device(device)
-
-    def __enter__(self):
-        import torch
-        if self.guard is not None:
-            self.guard.__enter__()
-        return torch.cuda.current_stream().cuda_stream
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
-        return False
+    if torch._C._cuda_getDevice() == index:
+        return call(torch._C._cuda_getCurrentRawStream(index))
+    with torch.cuda.device(index):
+        return call(torch._C._cuda_getCurrentRawStream(index))
 
 
 class Kv8Cache:
@@ -83,24 +75,27 @@ class Kv8Cache:
         B._check(self.L.ad_kv8_check(self._cfg))
         self.most_rows = capacity if closed else k_max
         device = torch.device(device)
-        self.device = torch.device("cuda", torch.cuda.current_device()) if device.index is None else device
+        self.index = torch.cuda.current_device() if device.index is None else device.index
+        self.device = torch.device("cuda", self.index)
         self.memory = torch.empty(self.L.ad_kv8_bytes(self._cfg), dtype=torch.uint8, device=self.device)
-
-    def _tables(self, row_start, length, name="length"):
-        import torch
-        n = self.cfg.n_seq
-        return (_flat(row_start, "row_start", self.device, torch.int32, (n + 1,)), _flat(length, name, self.device, torch.int32, (n,)))
+        self._at = self.memory.data_ptr()
+        self._start, self._len = (n_seq + 1,), (n_seq,)
+        self._i32, self._bf16 = torch.int32, torch.bfloat16
+        self._scale = 1.0 / math.sqrt(head_width)
+        self._need = {}
 
     def append(self, k, v, row_start, length, max_rows=None):
         """Rows k, v [rows, n_heads, head_width] bf16 become the tokens from length[b] on."""
-        c = self.cfg
-        kp, ks = _rows(k, "k", self.device, c.n_heads, c.head_width)
-        vp, vs = _rows(v, "v", self.device, c.n_heads, c.head_width, k.shape[0])
-        start, at = self._tables(row_start, length)
-        rows = k.shape[0]
-        with _On(self.device) as stream:
-            B._check(self.L.ad_kv8_append(self._cfg, self.memory.data_ptr(), kp, ks, vp, vs, start, at, rows,
-                                          min(rows, self.most_rows) if max_rows is None else max_rows, stream))
+        c, i = self.cfg, self.index
+        kp, ks, rows = _rows(k, "k", i, self._bf16, c.n_heads, c.head_width)
+        vp, vs, vrows = _rows(v, "v", i, self._bf16, c.n_heads, c.head_width)
+        if vrows != rows:
+            _refuse("k and v must have as many rows")
+        start, at = _flat(row_start, "row_start", i, self._i32, self._start), _flat(length, "length", i, self._i32, self._len)
+        most = min(rows, self.most_rows) if max_rows is None else max_rows
+        rc = _on(i, lambda stream: self.L.ad_kv8_append(self._cfg, self._at, kp, ks, vp, vs, start, at, rows, most, stream))
+        if rc:
+            B._check(rc)
 
     def read(self, row_start, begin, length, rows, max_rows=None, dtype=None):
         """The values the cache stands for, (k, v) [rows, n_heads, head_width]: tokens begin[b] .. of sequence b, as the row at position
@@ -109,36 +104,48 @@ class Kv8Cache:
         dtype = torch.bfloat16 if dtype is None else dtype
         if dtype not in (torch.bfloat16, torch.float32):
             _refuse("dtype must be bfloat16 or float32")
-        start, first = self._tables(row_start, begin, "begin")
-        at = self._tables(row_start, length)[1]
-        c = self.cfg
-        with _On(self.device) as stream:
-            k, v = (torch.empty((rows, c.n_heads, c.head_width), dtype=dtype, device=self.device) for _ in range(2))
-            B._check(self.L.ad_kv8_read(self._cfg, self.memory.data_ptr(), start, first, at, rows, rows if max_rows is None else max_rows,
-                                        B.AD_F32 if dtype == torch.float32 else B.AD_BF16, k.data_ptr(), v.data_ptr(), stream))
+        c, i = self.cfg, self.index
+        start, first = _flat(row_start, "row_start", i, self._i32, self._start), _flat(begin, "begin", i, self._i32, self._len)
+        at = _flat(length, "length", i, self._i32, self._len)
+        k, v = (torch.empty((rows, c.n_heads, c.head_width), dtype=dtype, device=self.device) for _ in range(2))
+        kp, vp = k.data_ptr(), v.data_ptr()
+        rc = _on(i, lambda stream: self.L.ad_kv8_read(self._cfg, self._at, start, first, at, rows, rows if max_rows is None else max_rows,
+                                                      B.AD_F32 if dtype is torch.float32 else B.AD_BF16, kp, vp, stream))
+        if rc:
+            B._check(rc)
         return k, v
 
     def attend(self, q, row_start, length, max_rows=None, max_keys=None, scale=None, out=None):
         """softmax(scale q k^T) v of rows q [rows, q_heads, head_width] bf16 (appended before: at positions length[b] ..; closed: over length[b]
         tokens).  q_heads: a multiple of n_heads, neighbours share a head.  scale: 1 / sqrt(head_width) by default."""
         import torch
-        c = self.cfg
-        if not isinstance(q, torch.Tensor) or q.dim() != 3:
-            _refuse("q must be a tensor [rows, q_heads, head_width]")
-        rows, heads = q.shape[0], q.shape[1]
-        qp, qs = _rows(q, "q", self.device, heads, c.head_width)
-        start, at = self._tables(row_start, length)
-        most = rows if c.closed else min(rows, c.k_max)
+        c, i = self.cfg, self.index
+        heads = q.shape[1] if isinstance(q, torch.Tensor) and q.dim() == 3 else 0
+        qp, qs, rows = _rows(q, "q", i, self._bf16, heads, c.head_width)
+        start, at = _flat(row_start, "row_start", i, self._i32, self._start), _flat(length, "length", i, self._i32, self._len)
+        most = (rows if c.closed else min(rows, c.k_max)) if max_rows is None else max_rows
         keys = c.capacity if max_keys is None else max_keys
-        with _On(self.device) as stream:
+        scale = self._scale if scale is None else scale
+
+        def call(stream):
+            nonlocal out
             if out is None:
-                out = torch.empty((rows, heads, c.head_width), dtype=torch.bfloat16, device=self.device)
-            op, os = _rows(out, "out", self.device, heads, c.head_width, rows)
-            need = self.L.ad_kv8_attend_bytes(self._cfg, heads, rows, keys)
+                out = torch.empty((rows, heads, c.head_width), dtype=self._bf16, device=self.device)
+            op, os, orows = _rows(out, "out", i, self._bf16, heads, c.head_width)
+            if orows != rows:
+                _refuse("out must have as many rows as q")
+            need = self._need.get((heads, rows, keys))
+            if need is None:
+                if len(self._need) >= 4096:
+                    self._need.clear()
+                need = self._need[heads, rows, keys] = self.L.ad_kv8_attend_bytes(self._cfg, heads, rows, keys)
+            # (held until the kernels are enqueued; whatever gets it from the allocator afterwards comes behind them on this stream)
             ws = torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
-            B._check(self.L.ad_kv8_attend(self._cfg, self.memory.data_ptr(), qp, qs, heads, start, at, rows, most if max_rows is None else max_rows,
-                                          keys, 1.0 / math.sqrt(c.head_width) if scale is None else scale, op, os,
-                                          ws.data_ptr() if ws is not None else None, need, stream))
+            return self.L.ad_kv8_attend(self._cfg, self._at, qp, qs, heads, start, at, rows, most, keys, scale, op, os,
+                                        None if ws is None else ws.data_ptr(), need, stream)
+        rc = _on(i, call)
+        if rc:
+            B._check(rc)
         return out
 
 
@@ -148,32 +155,40 @@ def accept_sampled(logits, draft, row_start, accept_u, pick_u, temperature=None,
     logits [rows, vocab] fp32 or bf16 (rows may lie apart), draft [rows] int32 (AD_NEVER: none), row_start [n_seq + 1] int32, accept_u [rows] and pick_u [n_seq]
     fp32 uniform in [0, 1), temperature [n_seq] fp32 or None (1), draft_probs [rows, vocab] fp32 or None (drafted tokens are certain)."""
     import torch
-    if not isinstance(logits, torch.Tensor) or logits.dim() != 2 or logits.dtype not in (torch.float32, torch.bfloat16) or logits.device.type != "cuda":
-        _refuse("logits must be a float32 or bfloat16 tensor [rows, vocab] on a GPU")
-    dev, (rows, vocab) = logits.device, logits.shape
-    if vocab > 1 and logits.stride(1) != 1:
-        _refuse("logits: a row's scores must lie side by side")
     f32, i32 = torch.float32, torch.int32
-    if not isinstance(pick_u, torch.Tensor):
-        _refuse("pick_u must be a tensor")
-    n_seq = pick_u.shape[0] if pick_u.dim() == 1 else -1
+    if not isinstance(logits, torch.Tensor) or logits.dim() != 2 or logits.dtype not in (f32, torch.bfloat16) or not logits.is_cuda:
+        _refuse("logits must be a float32 or bfloat16 tensor [rows, vocab] on a GPU")
+    i, (rows, vocab), (stride, one) = logits.get_device(), logits.shape, logits.stride()
+    if vocab > 1 and one != 1:
+        _refuse("logits: a row's scores must lie side by side")
+    n_seq = pick_u.shape[0] if isinstance(pick_u, torch.Tensor) and pick_u.dim() == 1 else -1
     probs, probs_stride = None, 0
     if draft_probs is not None:
-        _is(draft_probs, "draft_probs", dev, f32, (rows, vocab))
-        if vocab > 1 and draft_probs.stride(1) != 1:
+        if not isinstance(draft_probs, torch.Tensor) or draft_probs.dtype is not f32 or draft_probs.shape != logits.shape or draft_probs.get_device() != i:
+            _refuse(f"draft_probs must be a float32 tensor {[rows, vocab]} on cuda:{i}")
+        probs, (probs_stride, one) = draft_probs.data_ptr(), draft_probs.stride()
+        if vocab > 1 and one != 1:
             _refuse("draft_probs: a row's probabilities must lie side by side")
-        probs, probs_stride = draft_probs.data_ptr(), draft_probs.stride(0) if rows > 1 else vocab
-    args = (_flat(accept_u, "accept_u", dev, f32, (rows,)), _flat(pick_u, "pick_u", dev, f32, (n_seq,)),
-            _flat(row_start, "row_start", dev, i32, (n_seq + 1,)))
-    drafted = _flat(draft, "draft", dev, i32, (rows,))
-    temp = None if temperature is None else _flat(temperature, "temperature", dev, f32, (n_seq,))
-    L = B.lib()
-    with _On(dev) as stream:
-        n_accept = torch.empty(n_seq, dtype=i32, device=dev)
-        tokens = torch.empty(rows, dtype=i32, device=dev)
-        need = L.ad_accept_sampled_bytes(n_seq, rows, vocab)
-        ws = torch.empty(max(need, 1), dtype=torch.uint8, device=dev)
-        B._check(L.ad_accept_sampled(logits.data_ptr(), B.AD_F32 if logits.dtype == f32 else B.AD_BF16, logits.stride(0) if rows > 1 else vocab, vocab,
-                                     drafted, probs, probs_stride, temp, *args, n_seq, rows, rows if max_rows is None else max_rows,
-                                     n_accept.data_ptr(), tokens.data_ptr(), ws.data_ptr(), need, stream))
+    drafted = _flat(draft, "draft", i, i32, (rows,))
+    u, v = _flat(accept_u, "accept_u", i, f32, (rows,)), _flat(pick_u, "pick_u", i, f32, (n_seq,))
+    start = _flat(row_start, "row_start", i, i32, (n_seq + 1,))
+    temp = None if temperature is None else _flat(temperature, "temperature", i, f32, (n_seq,))
+    n_accept = torch.empty(n_seq, dtype=i32, device=logits.device)
+    tokens = torch.empty(rows, dtype=i32, device=logits.device)
+    need = _accept_bytes(n_seq, rows, vocab)
+
+    def call(stream):
+        # (held until the kernels are enqueued; whatever gets it from the allocator afterwards comes behind them on this stream)
+        ws = torch.empty(max(need, 1), dtype=torch.uint8, device=logits.device)
+        return B.lib().ad_accept_sampled(logits.data_ptr(), B.AD_F32 if logits.dtype is f32 else B.AD_BF16, stride if rows > 1 else vocab, vocab,
+                                         drafted, probs, probs_stride if rows > 1 else vocab, temp, u, v, start, n_seq, rows,
+                                         rows if max_rows is None else max_rows, n_accept.data_ptr(), tokens.data_ptr(), ws.data_ptr(), need, stream)
+    rc = _on(i, call)
+    if rc:
+        B._check(rc)
     return n_accept, tokens
+
+
+@functools.lru_cache(maxsize=4096)
+def _accept_bytes(n_seq, rows, vocab):
+    return B.lib().ad_accept_sampled_bytes(n_seq, rows, vocab)
