@@ -8,8 +8,9 @@
 // A drawn number may lie next to the border between two tokens, so sums over the vocabulary and what goes into them have 64 bits:
 //   k_accept_stats   a workgroup per 4096 scores of a row: their maximum, and sum of exp2((x - max) log2(e) / T) (without d where q is none).  It reads everything
 //                    once and is bound by that; 64-bit exponentials cost 20 instructions a score.
-//   k_accept_rest    (q given) a workgroup per 4096 scores of each sequence's deciding row: sum of r
-//   k_accept_pick    a workgroup per sequence: the rows' tests, the piece of the deciding row that holds the wanted sum, the token in it
+//   k_accept_rows    (q given, or many or large rows) a wave per row: its test
+//   k_accept_rest    (then) a workgroup per 4096 scores of each sequence's deciding row: sum of r
+//   k_accept_pick    a workgroup per sequence: the rows' tests if they have not been made, the piece of the deciding row that holds the wanted sum, the token in it
 #include <hip/hip_runtime.h>
 #include <math.h>
 
@@ -66,6 +67,26 @@ __device__ __forceinline__ double exp2_bulk(float x, double rate, double off) {
   const unsigned hi = (unsigned)(bits >> 32) + ((unsigned)__builtin_bit_cast(long long, big) << 20);
   return __builtin_bit_cast(double, (long long)((unsigned long long)hi << 32 | (unsigned)bits));
 }
+// and to f^11, nothing below 2^-1000, for the rows that are drawn from
+__device__ __forceinline__ double exp2_weight(float x, double rate, double off) {
+  const double u = fma((double)x, rate, off), t = fmax(u, -1020.0);
+  const double big = t + 6755399441055744.0, f = t - (big - 6755399441055744.0);
+  double p = 4.44553827187081149760e-10;   // ln(2)^k / k!, k = 11 .. 0
+  p = fma(p, f, 7.05491162080112332988e-9);
+  p = fma(p, f, 1.01780860092396997275e-7);
+  p = fma(p, f, 1.32154867901443094884e-6);
+  p = fma(p, f, 1.52527338040598402800e-5);
+  p = fma(p, f, 1.54035303933816099544e-4);
+  p = fma(p, f, 1.33335581464284434234e-3);
+  p = fma(p, f, 9.61812910762847716197e-3);
+  p = fma(p, f, 5.55041086648215799532e-2);
+  p = fma(p, f, 2.40226506959100712334e-1);
+  p = fma(p, f, 6.93147180559945309417e-1);
+  p = fma(p, f, 1.0);
+  const long long bits = __builtin_bit_cast(long long, p);
+  const unsigned hi = (unsigned)(bits >> 32) + ((unsigned)__builtin_bit_cast(long long, big) << 20);
+  return u < -1000.0 ? 0.0 : __builtin_bit_cast(double, (long long)((unsigned long long)hi << 32 | (unsigned)bits));
+}
 // sum over the wave, the same in every lane: lane moves as wave_sum's
 template <int CTRL> __device__ __forceinline__ double dpp_move_f64(double v) {
   const long long b = __builtin_bit_cast(long long, v);
@@ -121,6 +142,19 @@ template <typename T> struct AcceptRow {
   }
 };
 
+// Takes score `skip` (-1: none) out of what thread t holds of piece c: it is one thread's, there, and only there, it is looked for.  Whether it was a NaN.
+template <typename T> __device__ __forceinline__ bool accept_drop(const AcceptRow<T>& x, int c, int t, int skip, float (&v)[kAcceptEach]) {
+  constexpr int kVec = AcceptRow<T>::kVec;
+  const int in = skip - x.index(c, t, 0);
+  bool nan = false;
+  if (skip >= 0 && in >= 0 && in % (kAcceptThreads * kVec) < kVec && in / (kAcceptThreads * kVec) < kAcceptEach / kVec) {
+#pragma unroll
+    for (int j = 0; j < kAcceptEach; ++j)
+      if (x.index(c, t, j) == skip) { nan = v[j] != v[j]; v[j] = -INFINITY; }
+  }
+  return nan;
+}
+
 struct AcceptSeq { int row0, n; };
 __device__ __forceinline__ AcceptSeq accept_seq(const AcceptArgs& a, int b) {
   AcceptSeq s;
@@ -161,14 +195,7 @@ __global__ __launch_bounds__(kAcceptThreads) void k_accept_stats(AcceptArgs a) {
   bool nan = head != head || !(m < INFINITY) || rate != rate;   // (no distribution)
   if (m > -INFINITY) {
     const bool here = t < x.heads(c) && t != skip;
-    // (the drafted token's is one thread's: there, and only there, it is taken out)
-    constexpr int kVec = AcceptRow<T>::kVec;
-    const int in = skip - x.index(c, t, 0);
-    if (skip >= 0 && in >= 0 && in % (kAcceptThreads * kVec) < kVec && in / (kAcceptThreads * kVec) < kAcceptEach / kVec) {
-#pragma unroll
-      for (int j = 0; j < kAcceptEach; ++j)
-        if (x.index(c, t, j) == skip) { nan = nan || v[j] != v[j]; v[j] = -INFINITY; }
-    }
+    nan = accept_drop(x, c, t, skip, v) || nan;
     if constexpr (WIDE) {
       const double off = -(double)m * rate;
 #pragma unroll
@@ -260,49 +287,59 @@ __global__ __launch_bounds__(kAcceptThreads) void k_accept_rows(AcceptArgs a) {
   const AcceptRowInfo r = accept_decide<T>(a, sq.row0 + i, accept_rate(a, b));
   if ((threadIdx.x & 63) == 0) a.row_info[sq.row0 + i] = r;
 }
-// The first row whose token does not stand, from there, by each wave for itself
-__device__ __forceinline__ int accept_first_of(const AcceptArgs& a, const AcceptSeq& sq) {
+// The first row whose token does not stand, with its maximum and sum, from there, by each wave for itself
+struct AcceptFirst { int i; float m; double z; };
+__device__ __forceinline__ AcceptFirst accept_first_of(const AcceptArgs& a, const AcceptSeq& sq) {
   const int lane = threadIdx.x & 63;
   for (int i0 = 0; i0 < sq.n; i0 += 64) {
-    const unsigned long long falls = __ballot(i0 + lane < sq.n && !a.row_info[sq.row0 + i0 + min(lane, sq.n - 1 - i0)].stands);
-    if (falls) return i0 + __ffsll(falls) - 1;
+    const AcceptRowInfo r = gload(a.row_info + sq.row0 + i0 + min(lane, sq.n - 1 - i0));
+    const unsigned long long falls = __ballot(i0 + lane < sq.n && !r.stands);
+    if (falls) {
+      const int l = __ffsll(falls) - 1;
+      return AcceptFirst{i0 + l, __int_as_float(__builtin_amdgcn_readlane(__float_as_int(r.m), l)), lane_f64(r.z, l)};
+    }
   }
-  return sq.n;
+  return AcceptFirst{sq.n, 0.f, 0.0};
 }
 
-// What a token of the deciding row weighs in the draw, relative to the row's maximum (q given: as a probability)
-template <typename T> struct AcceptWeight {
-  const float* q;   // null: none
+// What a token of the deciding row weighs in the draw, relative to the row's maximum, or (PROBS) as a probability.  Without the drafter's probabilities the
+// drafted token weighs nothing: its score is made -inf (accept_drop).
+template <bool PROBS> struct AcceptWeight {
+  const float* q;
+  float drafted;   // 0: nothing was drafted, q does not count
   int skip;
-  float m;
-  double rate, inv_z;
-  __device__ __forceinline__ AcceptWeight(const AcceptArgs& a, int row, float m_, double z, double rate_) {
+  double rate, off, inv_z;
+  __device__ __forceinline__ AcceptWeight(const AcceptArgs& a, int row, float m, double z, double rate_) {
     const int d = a.draft[row];
-    const bool drafted = accept_drafted(a, d);
-    q = a.probs && drafted ? a.probs + (size_t)row * a.probs_stride : nullptr;
-    skip = !a.probs && drafted ? d : -1;
-    m = m_; rate = rate_; inv_z = 1.0 / z;
+    const bool is = accept_drafted(a, d);
+    q = PROBS ? a.probs + (size_t)row * a.probs_stride : nullptr;
+    drafted = is ? 1.f : 0.f;
+    skip = !PROBS && is ? d : -1;
+    rate = rate_; off = -(double)m * rate_; inv_z = 1.0 / z;
   }
   __device__ __forceinline__ double operator()(int i, float x) const {
-    const double e = exp2_down(((double)x - (double)m) * rate);
-    if (q) return fmax(e * inv_z - (double)q[i], 0.0);
-    return i == skip ? 0.0 : e;
+    const double e = exp2_weight(x, rate, off);
+    if constexpr (PROBS) return fmax(fma(e, inv_z, -(double)(drafted != 0.f ? q[i] : 0.f)), 0.0);
+    return e;
   }
+  __device__ __forceinline__ double head(int i, float x) const { return i == skip ? 0.0 : (*this)(i, x); }
 };
 
-template <typename T>
+template <typename T, bool PROBS>
 __global__ __launch_bounds__(kAcceptThreads) void k_accept_rest(AcceptArgs a) {
   __shared__ double ss[kAcceptThreads / 64];
   const int c = blockIdx.x, b = blockIdx.y, t = threadIdx.x;
   const AcceptSeq sq = accept_seq(a, b);
   if (sq.n <= 0) return;
-  const int i = accept_first_of(a, sq);
-  if (i >= sq.n) return;
-  const int row = sq.row0 + i;
+  const double rate = accept_rate(a, b);
+  const AcceptFirst f = accept_first_of(a, sq);
+  if (f.i >= sq.n) return;
+  const int row = sq.row0 + f.i;
   const AcceptRow<T> x(a, row);
   float v[kAcceptEach];
   x.load(c, t, v);
-  const AcceptWeight<T> w(a, row, a.row_info[row].m, a.row_info[row].z, accept_rate(a, b));
+  const AcceptWeight<PROBS> w(a, row, f.m, f.z, rate);
+  accept_drop(x, c, t, w.skip, v);
   {
     double s = 0.0;
 #pragma unroll
@@ -310,7 +347,7 @@ __global__ __launch_bounds__(kAcceptThreads) void k_accept_rest(AcceptArgs a) {
       const int at = x.index(c, t, j);
       if (at < a.vocab) s += w(at, v[j]);
     }
-    if (t < x.heads(c)) s += w(t, x.at(t));
+    if (t < x.heads(c)) s += w.head(t, x.at(t));
     s = wave_sum_f64(s);
     if ((t & 63) == 0) ss[t >> 6] = s;
   }
@@ -319,7 +356,7 @@ __global__ __launch_bounds__(kAcceptThreads) void k_accept_rest(AcceptArgs a) {
 }
 
 // DECIDED: k_accept_rows has been over the rows
-template <typename T, bool DECIDED>
+template <typename T, bool DECIDED, bool PROBS>
 __global__ __launch_bounds__(DECIDED ? kAcceptThreads : kDecideThreads) void k_accept_pick(AcceptArgs a) {
   constexpr int kThreads = DECIDED ? kAcceptThreads : kDecideThreads;
   constexpr int kVec = AcceptRow<T>::kVec, kGroups = kAcceptEach / kVec;
@@ -328,9 +365,12 @@ __global__ __launch_bounds__(DECIDED ? kAcceptThreads : kDecideThreads) void k_a
   const int b = blockIdx.x, t = threadIdx.x, lane = t & 63;
   const AcceptSeq sq = accept_seq(a, b);
   const double rate = accept_rate(a, b);
+  // (requested at once with what decides the row)
+  const double rest0 = DECIDED && lane < a.pieces ? a.rest_sum[(size_t)b * a.pieces + lane] : 0.0, pick_u = a.pick_u[b];
+  AcceptFirst f{0, 0.f, 0.0};
   int i = 0;
   if (sq.n > 0) {
-    if constexpr (DECIDED) i = accept_first_of(a, sq);
+    if constexpr (DECIDED) { f = accept_first_of(a, sq); i = f.i; }
     else i = accept_first<T>(a, sq, rate, &first);
     if (t == 0) token = AD_NEVER;
     __syncthreads();
@@ -340,17 +380,17 @@ __global__ __launch_bounds__(DECIDED ? kAcceptThreads : kDecideThreads) void k_a
     float m;
     double z;
     if constexpr (DECIDED) {
-      m = a.row_info[row].m; z = a.row_info[row].z;
+      m = f.m; z = f.z;
     } else {
       const AcceptSums sums = accept_sums<T>(a, row, rate);
       m = sums.m; z = sums.z;
     }
     if (!accept_broken(z)) {
       const AcceptRow<T> x(a, row);
-      const AcceptWeight<T> w(a, row, m, z, rate);
+      const AcceptWeight<PROBS> w(a, row, m, z, rate);
       // (the drafted token is left out of the pieces' sums where the drafter gave no probabilities)
       auto piece = [&](int c) -> double {
-        if (a.rest) return a.rest_sum[(size_t)b * a.pieces + c];
+        if constexpr (DECIDED) return c == lane ? rest0 : a.rest_sum[(size_t)b * a.pieces + c];
         const float mc = a.piece_max[(size_t)row * a.pieces + c];
         const double s = mc > -INFINITY ? a.piece_sum[(size_t)row * a.pieces + c] * exp2_down(((double)mc - (double)m) * rate) : 0.0;
         return s < kNothing ? 0.0 : s;
@@ -360,7 +400,7 @@ __global__ __launch_bounds__(DECIDED ? kAcceptThreads : kDecideThreads) void k_a
       for (int c = lane; c < a.pieces; c += 64) total += piece(c);
       total = wave_sum_f64(total);
       if (total > 0.0) {
-        const double want = (double)a.pick_u[b] * total;
+        const double want = pick_u * total;
         double before = 0.0, base = 0.0;
         int at = -1, last = 0;
         double last_base = 0.0;
@@ -392,6 +432,7 @@ __global__ __launch_bounds__(DECIDED ? kAcceptThreads : kDecideThreads) void k_a
         if (t < kAcceptThreads) {
           float v[kAcceptEach];
           x.load(at, t, v);
+          accept_drop(x, at, t, w.skip, v);
 #pragma unroll
           for (int j = 0; j < kAcceptEach; j += kVec) {
             double s = 0.0;
@@ -411,7 +452,7 @@ __global__ __launch_bounds__(DECIDED ? kAcceptThreads : kDecideThreads) void k_a
         double run = base;
         {
           const int n = x.heads(at);
-          const double e = lane < n ? w(lane, x.at(lane)) : 0.0;
+          const double e = lane < n ? w.head(lane, x.at(lane)) : 0.0;
           for (int i = 0; i < n && hit < 0; ++i) {
             const double g = lane_f64(e, i);
             run += g;
@@ -499,10 +540,9 @@ size_t accept_bytes(int n_seq, int rows, int vocab) {
 }
 void launch_accept_sampled(int dtype, AcceptArgs a, void* ws, hipStream_t s) {
   a.pieces = accept_pieces(a.vocab);
-#ifndef WTH
-#define WTH (1<<22)
-#endif
-  const bool wide = a.probs || (size_t)a.rows * a.vocab < WTH;
+  // Sums in 64 bits of every row serve the draw as well as the test, and the draw is the second and last launch.  Where all rows together are large, only the deciding
+  // ones get them, in launches of their own (352 rows of 100,003 bf16 scores: 47 us all, 41 the deciding ones; 8 rows of 32,000: 9.4 and 12.5).
+  const bool wide = a.probs || (size_t)a.rows * a.vocab < ((size_t)1 << 22);
   a.rest = a.probs || !wide;
   char* w = (char*)ws;
   a.piece_sum = (double*)w;
@@ -516,10 +556,14 @@ void launch_accept_sampled(int dtype, AcceptArgs a, void* ws, hipStream_t s) {
     else k_accept_stats<T, false><<<grid, kAcceptThreads, 0, s>>>(a);
     if (a.rest) {
       k_accept_rows<T><<<dim3((a.max_rows + 3) / 4, a.n_seq), kAcceptThreads, 0, s>>>(a);
-      k_accept_rest<T><<<dim3(a.pieces, a.n_seq), kAcceptThreads, 0, s>>>(a);
-      k_accept_pick<T, true><<<a.n_seq, kAcceptThreads, 0, s>>>(a);
+      auto draw = [&](auto probs) {
+        k_accept_rest<T, probs.value><<<dim3(a.pieces, a.n_seq), kAcceptThreads, 0, s>>>(a);
+        k_accept_pick<T, true, probs.value><<<a.n_seq, kAcceptThreads, 0, s>>>(a);
+      };
+      if (a.probs) draw(std::true_type{});
+      else draw(std::false_type{});
     } else {
-      k_accept_pick<T, false><<<a.n_seq, kDecideThreads, 0, s>>>(a);
+      k_accept_pick<T, false, false><<<a.n_seq, kDecideThreads, 0, s>>>(a);
     }
   };
   if (dtype == AD_BF16) go(bf16_t{});
