@@ -107,7 +107,8 @@ class Kv8Cache:
         c, i = self.cfg, self.index
         start, first = _flat(row_start, "row_start", i, self._i32, self._start), _flat(begin, "begin", i, self._i32, self._len)
         at = _flat(length, "length", i, self._i32, self._len)
-        k, v = (torch.empty((rows, c.n_heads, c.head_width), dtype=dtype, device=self.device) for _ in range(2))
+        k = torch.empty((rows, c.n_heads, c.head_width), dtype=dtype, device=self.device)
+        v = torch.empty_like(k)
         kp, vp = k.data_ptr(), v.data_ptr()
         rc = _on(i, lambda stream: self.L.ad_kv8_read(self._cfg, self._at, start, first, at, rows, rows if max_rows is None else max_rows,
                                                       B.AD_F32 if dtype is torch.float32 else B.AD_BF16, kp, vp, stream))
@@ -129,11 +130,15 @@ class Kv8Cache:
 
         def call(stream):
             nonlocal out
-            if out is None:
-                out = torch.empty((rows, heads, c.head_width), dtype=self._bf16, device=self.device)
-            op, os, orows = _rows(out, "out", i, self._bf16, heads, c.head_width)
-            if orows != rows:
-                _refuse("out must have as many rows as q")
+            if out is None and qs == heads * c.head_width:
+                out = torch.empty_like(q)
+                op, os = out.data_ptr(), qs
+            else:
+                if out is None:
+                    out = torch.empty((rows, heads, c.head_width), dtype=self._bf16, device=self.device)
+                op, os, orows = _rows(out, "out", i, self._bf16, heads, c.head_width)
+                if orows != rows:
+                    _refuse("out must have as many rows as q")
             need = self._need.get((heads, rows, keys))
             if need is None:
                 if len(self._need) >= 4096:
@@ -173,8 +178,7 @@ def accept_sampled(logits, draft, row_start, accept_u, pick_u, temperature=None,
     u, v = _flat(accept_u, "accept_u", i, f32, (rows,)), _flat(pick_u, "pick_u", i, f32, (n_seq,))
     start = _flat(row_start, "row_start", i, i32, (n_seq + 1,))
     temp = None if temperature is None else _flat(temperature, "temperature", i, f32, (n_seq,))
-    n_accept = torch.empty(n_seq, dtype=i32, device=logits.device)
-    tokens = torch.empty(rows, dtype=i32, device=logits.device)
+    n_accept, tokens = torch.empty_like(pick_u, dtype=i32), torch.empty_like(draft)
     need = _accept_bytes(n_seq, rows, vocab)
 
     def call(stream):
