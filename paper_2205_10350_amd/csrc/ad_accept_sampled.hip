@@ -6,10 +6,10 @@
 // Tokens so accepted are distributed as p.
 //
 // A drawn number may lie next to the border between two tokens, so sums over the vocabulary and what goes into them have 64 bits:
-//   k_accept_stats   a workgroup per 4096 scores of a row: their maximum, and sum of exp2((x - max) log2(e) / T) (without d where q is none).  It reads everything
+//   k_accept_stats   a workgroup per 8 KB of scores of a row: their maximum, and sum of exp2((x - max) log2(e) / T) (without d where q is none).  It reads everything
 //                    once and is bound by that; 64-bit exponentials cost 20 instructions a score.
 //   k_accept_rows    (q given, or many or large rows) a wave per row: its test
-//   k_accept_rest    (then) a workgroup per 4096 scores of each sequence's deciding row: sum of r
+//   k_accept_rest    (then) a workgroup per 8 KB of scores of each sequence's deciding row: sum of r
 //   k_accept_pick    a workgroup per sequence: the rows' tests if they have not been made, the piece of the deciding row that holds the wanted sum, the token in it
 #include <hip/hip_runtime.h>
 #include <math.h>
@@ -22,9 +22,10 @@
 namespace ad {
 
 constexpr int kAcceptThreads = 256;
-constexpr int kAcceptPiece = 4096;                                  // scores of a workgroup
 constexpr int kDecideThreads = 1024;                                // where a sequence's rows are tested, a wave a row
-constexpr int kAcceptEach = kAcceptPiece / kAcceptThreads;          // of a thread
+// scores of a workgroup (8 KB: 32 blocks with the drafter's probabilities 39 us with 16 KB, 35 with 8; 64 of bf16 41 with 4 KB, 39 with 8) and of a thread
+template <typename T> constexpr int kPiece = 8192 / (int)sizeof(T);
+template <typename T> constexpr int kEach = kPiece<T> / kAcceptThreads;
 
 // What weighs less than this beside the row's most likely token weighs nothing: a piece counts only if one of its tokens will (exp2_down ends at 2^-1000).
 constexpr double kNothing = 0x1p-900;
@@ -116,13 +117,13 @@ template <typename T> struct AcceptRow {
     skew = (int)((16 - ((uintptr_t)x & 15)) & 15) / (int)sizeof(T);
   }
   __device__ __forceinline__ float at(int i) const { return Store<T>::load(x + i); }
-  // Piece c holds the scores from skew + 4096 c on (and, the first one, the skew's): thread t's element j.
-  __device__ __forceinline__ int index(int c, int t, int j) const { return skew + c * kAcceptPiece + ((j / kVec) * kAcceptThreads + t) * kVec + j % kVec; }
+  // Piece c holds the scores from skew + kPiece c on (and, the first one, the skew's): thread t's element j.
+  __device__ __forceinline__ int index(int c, int t, int j) const { return skew + c * kPiece<T> + ((j / kVec) * kAcceptThreads + t) * kVec + j % kVec; }
   __device__ __forceinline__ int heads(int c) const { return c == 0 ? min(skew, vocab) : 0; }
   // (-inf past the end)
-  __device__ __forceinline__ void load(int c, int t, float (&v)[kAcceptEach]) const {
+  __device__ __forceinline__ void load(int c, int t, float (&v)[kEach<T>]) const {
 #pragma unroll
-    for (int j = 0; j < kAcceptEach; j += kVec) {
+    for (int j = 0; j < kEach<T>; j += kVec) {
       const int i = index(c, t, j);
       if (i + kVec <= vocab) {
         const uint4 w = ldg16(x + i);
@@ -143,13 +144,13 @@ template <typename T> struct AcceptRow {
 };
 
 // Takes score `skip` (-1: none) out of what thread t holds of piece c: it is one thread's, there, and only there, it is looked for.  Whether it was a NaN.
-template <typename T> __device__ __forceinline__ bool accept_drop(const AcceptRow<T>& x, int c, int t, int skip, float (&v)[kAcceptEach]) {
+template <typename T> __device__ __forceinline__ bool accept_drop(const AcceptRow<T>& x, int c, int t, int skip, float (&v)[kEach<T>]) {
   constexpr int kVec = AcceptRow<T>::kVec;
   const int in = skip - x.index(c, t, 0);
   bool nan = false;
-  if (skip >= 0 && in >= 0 && in % (kAcceptThreads * kVec) < kVec && in / (kAcceptThreads * kVec) < kAcceptEach / kVec) {
+  if (skip >= 0 && in >= 0 && in % (kAcceptThreads * kVec) < kVec && in / (kAcceptThreads * kVec) < kEach<T> / kVec) {
 #pragma unroll
-    for (int j = 0; j < kAcceptEach; ++j)
+    for (int j = 0; j < kEach<T>; ++j)
       if (x.index(c, t, j) == skip) { nan = v[j] != v[j]; v[j] = -INFINITY; }
   }
   return nan;
@@ -179,14 +180,14 @@ __global__ __launch_bounds__(kAcceptThreads) void k_accept_stats(AcceptArgs a) {
   if ((int)blockIdx.y >= sq.n) return;
   const int row = sq.row0 + blockIdx.y;
   const AcceptRow<T> x(a, row);
-  float v[kAcceptEach];
+  float v[kEach<T>];
   x.load(c, t, v);
   const float head = t < x.heads(c) ? x.at(t) : -INFINITY;
   const int skip = a.probs ? -1 : a.draft[row];   // (point mass: summed apart, so that what is left beside it is not a difference)
   const double rate = accept_rate(a, b);
   float m = head;
 #pragma unroll
-  for (int j = 0; j < kAcceptEach; ++j) m = __builtin_amdgcn_fmed3f(m, v[j], INFINITY);   // (the larger; fmaxf would quiet NaN first)
+  for (int j = 0; j < kEach<T>; ++j) m = __builtin_amdgcn_fmed3f(m, v[j], INFINITY);   // (the larger; fmaxf would quiet NaN first)
   m = wave_max(m);
   if ((t & 63) == 0) ms[t >> 6] = m;
   __syncthreads();
@@ -199,7 +200,7 @@ __global__ __launch_bounds__(kAcceptThreads) void k_accept_stats(AcceptArgs a) {
     if constexpr (WIDE) {
       const double off = -(double)m * rate;
 #pragma unroll
-      for (int j = 0; j < kAcceptEach; ++j) {
+      for (int j = 0; j < kEach<T>; ++j) {
         nan = nan || v[j] != v[j];
         s += exp2_bulk(v[j], rate, off);
       }
@@ -209,12 +210,12 @@ __global__ __launch_bounds__(kAcceptThreads) void k_accept_stats(AcceptArgs a) {
       const float r = (float)rate;
       float e[4] = {here ? __builtin_amdgcn_exp2f((head - m) * r) : 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int j = 0; j < kAcceptEach; ++j) e[j % 4] += __builtin_amdgcn_exp2f((v[j] - m) * r);
+      for (int j = 0; j < kEach<T>; ++j) e[j % 4] += __builtin_amdgcn_exp2f((v[j] - m) * r);
       s = (double)((e[0] + e[1]) + (e[2] + e[3]));
     }
   } else {
 #pragma unroll
-    for (int j = 0; j < kAcceptEach; ++j) nan = nan || v[j] != v[j];
+    for (int j = 0; j < kEach<T>; ++j) nan = nan || v[j] != v[j];
   }
   if (nan) s = (double)NAN;
   s = wave_sum_f64(s);
@@ -336,14 +337,14 @@ __global__ __launch_bounds__(kAcceptThreads) void k_accept_rest(AcceptArgs a) {
   if (f.i >= sq.n) return;
   const int row = sq.row0 + f.i;
   const AcceptRow<T> x(a, row);
-  float v[kAcceptEach];
+  float v[kEach<T>];
   x.load(c, t, v);
   const AcceptWeight<PROBS> w(a, row, f.m, f.z, rate);
   accept_drop(x, c, t, w.skip, v);
   {
     double s = 0.0;
 #pragma unroll
-    for (int j = 0; j < kAcceptEach; ++j) {
+    for (int j = 0; j < kEach<T>; ++j) {
       const int at = x.index(c, t, j);
       if (at < a.vocab) s += w(at, v[j]);
     }
@@ -359,7 +360,7 @@ __global__ __launch_bounds__(kAcceptThreads) void k_accept_rest(AcceptArgs a) {
 template <typename T, bool DECIDED, bool PROBS>
 __global__ __launch_bounds__(DECIDED ? kAcceptThreads : kDecideThreads) void k_accept_pick(AcceptArgs a) {
   constexpr int kThreads = DECIDED ? kAcceptThreads : kDecideThreads;
-  constexpr int kVec = AcceptRow<T>::kVec, kGroups = kAcceptEach / kVec;
+  constexpr int kVec = AcceptRow<T>::kVec, kGroups = kEach<T> / kVec;
   __shared__ int first, token;
   __shared__ double round[kGroups * 4];
   const int b = blockIdx.x, t = threadIdx.x, lane = t & 63;
@@ -428,13 +429,13 @@ __global__ __launch_bounds__(DECIDED ? kAcceptThreads : kDecideThreads) void k_a
         if (at < 0) { at = last; base = last_base; }   // (rounding: the last piece that holds anything)
         // Its weights: sums of kVec scores side by side by thread, in kGroups rounds of the workgroup's four waves, which is the order of their indices; the round and
         // wave, the thread, the score in which the running sum passes `want` (else the last that weighs anything).
-        double each[kAcceptEach], own[kGroups];
+        double each[kEach<T>], own[kGroups];
         if (t < kAcceptThreads) {
-          float v[kAcceptEach];
+          float v[kEach<T>];
           x.load(at, t, v);
           accept_drop(x, at, t, w.skip, v);
 #pragma unroll
-          for (int j = 0; j < kAcceptEach; j += kVec) {
+          for (int j = 0; j < kEach<T>; j += kVec) {
             double s = 0.0;
 #pragma unroll
             for (int e = 0; e < kVec; ++e) {
@@ -487,7 +488,7 @@ __global__ __launch_bounds__(DECIDED ? kAcceptThreads : kDecideThreads) void k_a
               const int l = over ? __ffsll(over) - 1 : 63 - __clzll(some);
               run += upto - mine;
 #pragma unroll
-              for (int j = 0; j < kAcceptEach; ++j)
+              for (int j = 0; j < kEach<T>; ++j)
                 if (j / kVec == in / 4) {   // (every thread its own scores: the thread's that was found counts)
                   run += each[j];
                   if (each[j] > 0.0 && hit < 0) {
@@ -532,17 +533,18 @@ void launch_accept_inputs(const int* draft, const float* u, const float* v, cons
   k_accept_inputs<<<n_seq, 64, 0, s>>>(draft, u, v, t, k_max, row_start, draft_out, u_out, v_out, t_out);
 }
 
-int accept_pieces(int vocab) { return (vocab + kAcceptPiece - 1) / kAcceptPiece; }
+static int pieces_of(int vocab, int piece) { return (vocab + piece - 1) / piece; }
 static size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 size_t accept_bytes(int n_seq, int rows, int vocab) {
-  const size_t p = accept_pieces(vocab);
+  const size_t p = pieces_of(vocab, kPiece<float>);   // (bf16 has half as many)
   return up256(rows * p * 8) + up256(rows * p * 4) + up256((size_t)n_seq * p * 8) + up256(rows * sizeof(AcceptRowInfo));
 }
 void launch_accept_sampled(int dtype, AcceptArgs a, void* ws, hipStream_t s) {
-  a.pieces = accept_pieces(a.vocab);
+  a.pieces = pieces_of(a.vocab, dtype == AD_BF16 ? kPiece<bf16_t> : kPiece<float>);
   // Sums in 64 bits of every row serve the draw as well as the test, and the draw is the second and last launch.  Where all rows together are large, only the deciding
-  // ones get them, in launches of their own (352 rows of 100,003 bf16 scores: 47 us all, 41 the deciding ones; 8 rows of 32,000: 9.4 and 12.5).
-  const bool wide = a.probs || (size_t)a.rows * a.vocab < ((size_t)1 << 22);
+  // ones get them, in launches of their own (us, all rows / the deciding ones: 8 rows of 32,000 8.1 / 10.8, 128 rows 16.6 / 18.9, 800 rows 41.1 / 33.5,
+  // 352 rows of 100,003 in bf16 47 / 39).
+  const bool wide = a.probs || (size_t)a.rows * a.vocab < ((size_t)1 << 23);
   a.rest = a.probs || !wide;
   char* w = (char*)ws;
   a.piece_sum = (double*)w;
