@@ -315,7 +315,7 @@ int ad_set_gadpp(ad_ctx* ctx, int32_t beta, float tau);
  * alone, not on how many came in a call or which were taken back, and its result, bit for bit, on the cache's description and those tokens.
  * A closed cache (an encoder's memory) is written in one call per sequence and read in 8 bits throughout.
  * A token with a key or value of a head that is not finite reads as NaN there, and so does its whole block once in 8 bits; rows that
- * do not see it are not touched by it.
+ * do not see it are not touched by it.  Finite ones are to stay below 2^100, so that sums over them do.
  *
  * The calls enqueue kernels on `hip_stream` of the current device and return; they allocate nothing, copy nothing and may be captured
  * into graphs.  `row_start` [n_seq + 1], `length` [n_seq] and the like are DEVICE arrays here, read when the kernels run: sequence b has
@@ -369,7 +369,7 @@ int ad_kv8_attend(const ad_kv8_config* cfg, const void* cache, const void* q, in
  *   temperature  DEVICE [n_seq] T, or NULL (1)
  *   accept_u     DEVICE [rows]; pick_u: DEVICE [n_seq]
  *   n_accept     DEVICE [n_seq] out: tokens of the sequence's block, the replacement included
- *   tokens       DEVICE [rows] out: those tokens, AD_NEVER behind them
+ *   tokens       DEVICE [rows] out: those tokens, AD_NEVER behind them to the end of the sequence's rows
  * A sequence whose next row has no distribution (no finite score, a NaN or +inf among them, T not a positive number) ends before that row.
  * `workspace`: ad_accept_sampled_bytes of device memory, as ad_kv8_attend's.  Enqueues kernels on `hip_stream`, as the calls above. */
 size_t ad_accept_sampled_bytes(int32_t n_seq, int32_t rows, int32_t vocab);

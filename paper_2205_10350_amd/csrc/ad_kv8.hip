@@ -54,7 +54,9 @@ template <int FMT> __device__ __forceinline__ unsigned kv8_pack4(const float (&x
 }
 
 // One workgroup per (touched block, head, sequence), 4 * DH threads: the first half takes the keys, the second the values, a thread 16 elements.
-// Both sides load rows 8 columns at a time; the values are turned in LDS.  Bound by memory (2 bytes in, 3 out for an element).
+// Both sides load rows 8 columns at a time; the values are turned in LDS.  Bound by memory (2 bytes in, 3 out for an element of an
+// open block or a ring that a row may read): 8 prompts of 1000 to 2048 rows, 16 heads of width 64, 125 MB in 28 us, 4.5 TB/s; one token 4.4 us, a launch and three waits.
+// (A thread's bytes are packed into words by hand: through arrays that were read under another type the compiler put them into scratch memory, 41 us.)
 template <int DH, int FMT, bool CLOSED>
 __global__ __launch_bounds__(4 * DH) void k_kv8_append(unsigned char* __restrict__ cache, const bf16_t* __restrict__ k, const bf16_t* __restrict__ v,
                                                        size_t k_stride, size_t v_stride, Kv8Rows rt, Kv8Dims dm) {
@@ -156,7 +158,8 @@ __global__ __launch_bounds__(4 * DH) void k_kv8_append(unsigned char* __restrict
   if (u == 0) gstore((float*)(cache + dm.scales) + (bh * dm.blocks + blk) * 2 + (values ? 1 : 0), any_spoilt && !values ? __uint_as_float(0x7fc00000u) : q.scale);
 }
 
-// One workgroup per (block, head, sequence), 4 * DH threads; keys' rows are written as they are held, values turned in LDS.  Bound by memory.
+// One workgroup per (block, head, sequence), 4 * DH threads; keys' rows are written as they are held, values turned in LDS.  Bound by memory:
+// 75 MB in 14.4 us, 5.2 TB/s; one token 3.3 us.
 template <int DH, int FMT, typename T>
 __global__ __launch_bounds__(4 * DH) void k_kv8_read(const unsigned char* __restrict__ cache, Kv8Rows rt, const int* __restrict__ length,
                                                      T* __restrict__ k_out, T* __restrict__ v_out, Kv8Dims dm) {

@@ -4,11 +4,17 @@
 // lane holds one query row (lane % 16) throughout and its probabilities are the right operand of the second product as they are.
 //  * A wave takes 16 R query rows of a (sequence, head), those of the query heads that share the head among them, and every fourth block of
 //    a split's keys: four waves of a workgroup, then the splits, each an online softmax of its own, joined in their order.
+//  * Two blocks (8 or 16 KB a wave) are on their way while one is worked on, from memory to operand registers without LDS.
 //  * Bytes become bf16 operands in registers, exactly; the keys' scale multiplies the scores, the values' the probabilities before they are rounded (e4m3: a
 //    power of two, which the conversion of the values applies).
 //  * Blocks of 8 bits first, those that every row of the tile sees without a mask; then the rows' own blocks from the bf16 ring.
 // A row's sums depend on the cache's sizes and the row's position alone: not on the call's other rows, nor on R, nor on how many splits are launched (blocks and
 // splits that a row does not see change nothing in it, to the bit).
+//
+// What bounds it: few rows over many keys, memory (8 sequences of 16,000 to 32,000 keys, 8 heads of width 128, 4 query heads each: 394 MB in 80 us, 4.9 TB/s, where
+// a large copy reaches 5.2; 32 sequences of 1 to 8192 keys, 16 heads of width 64, 1 to 25 rows: 272 MB in 67 us); one sequence, a chain of waits for memory (41 keys
+// 4 us, 8216 keys of 16 heads 12); 512 rows, the exponentials and what surrounds them, 130 vector instructions (17 of them exponentials) for 16 matrix
+// instructions over 32 rows and 32 keys (26 GFLOP in 65 us, 400 TFLOP/s; a library product reaches 1160).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -45,14 +51,20 @@ __device__ __forceinline__ Kv8Sum kv8_join(Kv8Sum a, Kv8Sum b, float& fa, float&
   return Kv8Sum{t, fmaf(b.sum, fb, a.sum * fa)};
 }
 
-// the larger of two (of a NaN and a number the number), one instruction where fmaxf first makes signalling NaNs quiet
-__device__ __forceinline__ float kv8_max(float a, float b) { return __builtin_amdgcn_fmed3f(a, b, INFINITY); }
+// the larger of two (of a NaN and a number the number), one instruction where fmaxf first makes signalling NaNs quiet: the middle one of them and infinity, which the
+// compiler must not know to be it, or it makes that a maximum again
+__device__ __forceinline__ float kv8_max(float a, float b, float inf) { return __builtin_amdgcn_fmed3f(a, b, inf); }
+__device__ __forceinline__ float kv8_inf() {
+  float v = INFINITY;
+  asm("" : "+v"(v));
+  return v;
+}
 // maximum / sum over the four lane groups that hold a row's keys
-__device__ __forceinline__ float kv8_rows_max(float m) {
+__device__ __forceinline__ float kv8_rows_max(float m, float inf) {
   auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(m), __float_as_uint(m), false, false);
-  m = kv8_max(__uint_as_float(p[0]), __uint_as_float(p[1]));
+  m = kv8_max(__uint_as_float(p[0]), __uint_as_float(p[1]), inf);
   p = __builtin_amdgcn_permlane32_swap(__float_as_uint(m), __float_as_uint(m), false, false);
-  return kv8_max(__uint_as_float(p[0]), __uint_as_float(p[1]));
+  return kv8_max(__uint_as_float(p[0]), __uint_as_float(p[1]), inf);
 }
 __device__ __forceinline__ float kv8_rows_sum(float v) {
   auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -62,11 +74,12 @@ __device__ __forceinline__ float kv8_rows_sum(float v) {
 }
 
 // waves a SIMD should hold (its registers are shared out accordingly)
-constexpr int kv8_waves(int dh, int r) { return dh == 128 ? (r == 2 ? 1 : 2) : r == 4 ? 2 : r == 2 ? 3 : 4; }
+constexpr int kv8_waves(int dh, int r) { return dh == 128 ? 3 - r : 5 - r; }
 
 template <int DH, int R> struct Kv8State {
   bf16x8 q[R][DH / 32];
   f32x4 o[R][DH / 16];
+  float inf;          // kv8_inf()
   float m[R], l[R];   // of this lane's row: the exponents' reference (all lane groups alike), the denominator's part of this lane's keys
 };
 
@@ -96,8 +109,9 @@ __device__ __forceinline__ void kv8_block(Kv8State<DH, R>& st, const KF& kf, con
     float x[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = !MASK || ((bits >> i) & 1) ? score(i) : -INFINITY;
-    float top = kv8_max(kv8_max(kv8_max(x[0], x[1]), kv8_max(x[2], x[3])), kv8_max(kv8_max(x[4], x[5]), kv8_max(x[6], x[7])));
-    top = kv8_rows_max(top) * c1;   // (the largest product is the product of the largest; NaN: ignored here, in the sums below it is not)
+    auto larger = [&](float a, float b) { return kv8_max(a, b, st.inf); };
+    float top = larger(larger(larger(x[0], x[1]), larger(x[2], x[3])), larger(larger(x[4], x[5]), larger(x[6], x[7])));
+    top = kv8_rows_max(top, st.inf) * c1;   // (the largest product is the product of the largest; NaN: ignored here, in the sums below it is not)
     // The reference that a row's exponents are taken from follows its maximum in steps of 2^kStep or more: sums stay far from the ends of fp32 either way, and the
     // sums so far need no rescaling in most blocks.  Which blocks do is a row's own affair; a tile does it for all of its rows, by one for the others.
     const bool step = top > st.m[rt] + kStep;
@@ -114,13 +128,19 @@ __device__ __forceinline__ void kv8_block(Kv8State<DH, R>& st, const KF& kf, con
     const float off = st.m[rt] == -INFINITY ? 0.f : st.m[rt];   // (a row that has seen nothing yet)
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = !MASK || ((bits >> i) & 1) ? __builtin_amdgcn_exp2f(fmaf(score(i), c1, -off)) : 0.f;
-    st.l[rt] += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
-    // (the probabilities of the output product have 8 bits, half a step of 2^-8 relative each, as in every attention of bf16 here; the denominator has 24)
     if constexpr (VSCALE) {
+      st.l[rt] += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
 #pragma unroll
       for (int i = 0; i < 8; ++i) x[i] *= cv;
     }
+    // (the probabilities of the output product have 8 bits, half a step of 2^-8 relative each, as in every attention of bf16 here; the denominator has 24, of the rounded
+    // ones where they are what the values are multiplied by: two to an instruction)
     const uint4 w = uint4{f2bf_pair(x[0], x[1]), f2bf_pair(x[2], x[3]), f2bf_pair(x[4], x[5]), f2bf_pair(x[6], x[7])};
+    if constexpr (!VSCALE) {
+      auto two = [](unsigned v) { return __builtin_bit_cast(kv8_bf16x2, v); };
+      const kv8_bf16x2 one = two(0x3f803f80u);
+      st.l[rt] = __builtin_amdgcn_fdot2_f32_bf16(two(w.w), one, __builtin_amdgcn_fdot2_f32_bf16(two(w.z), one, __builtin_amdgcn_fdot2_f32_bf16(two(w.y), one, __builtin_amdgcn_fdot2_f32_bf16(two(w.x), one, st.l[rt], false), false), false), false);
+    }
     pf[rt] = __builtin_bit_cast(bf16x8, w);
   }
 #pragma unroll
@@ -154,10 +174,10 @@ __device__ __forceinline__ void kv8_wave(Kv8State<DH, R>& st, const unsigned cha
   const float2* scales = (const float2*)(cache + dm.scales) + bh * dm.blocks;
   const int whole = min(blk1, own_lo), end = min(blk1, own_hi);
   int blk = blk0 + wave;
-  constexpr int AHEAD = 2;
-  Kv8Bytes<DH> x[AHEAD + 1];
+  constexpr int kAhead = 2;
+  Kv8Bytes<DH> x[kAhead + 1];
 #pragma unroll
-  for (int n = 0; n < AHEAD; ++n)
+  for (int n = 0; n < kAhead; ++n)
     if (blk + 4 * n < whole) kv8_fetch(x[n], blocks, scales, blk + 4 * n, lane);
   int pos[R];   // position of this lane's row (closed: the length; rows past the last one repeat it)
 #pragma unroll
@@ -176,6 +196,7 @@ __device__ __forceinline__ void kv8_wave(Kv8State<DH, R>& st, const unsigned cha
 #pragma unroll
     for (int c = 0; c < DH / 16; ++c) st.o[rt][c] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
+  st.inf = kv8_inf();
   const float scale = fabsf(a.scale);
   auto take = [&](auto mask, const Kv8Bytes<DH>& x, int blk) {
     auto kf = [&](int kt, int s) { return kv8_operand<FMT>(kt == 0 ? uint2{x.k[s].x, x.k[s].y} : uint2{x.k[s].z, x.k[s].w}, 1.f); };
@@ -197,8 +218,8 @@ __device__ __forceinline__ void kv8_wave(Kv8State<DH, R>& st, const unsigned cha
   const std::true_type some{};
   while (blk < whole) {
 #pragma unroll
-    for (int n = 0; n <= AHEAD; ++n) {
-      if (blk + 4 * AHEAD < whole) kv8_fetch(x[(n + AHEAD) % (AHEAD + 1)], blocks, scales, blk + 4 * AHEAD, lane);
+    for (int n = 0; n <= kAhead; ++n) {
+      if (blk + 4 * kAhead < whole) kv8_fetch(x[(n + kAhead) % (kAhead + 1)], blocks, scales, blk + 4 * kAhead, lane);
       take(all, x[n], blk);
       blk += 4;
       if (blk >= whole) break;
@@ -276,7 +297,7 @@ __device__ __forceinline__ void kv8_merge(const Kv8State<DH, R>& st, float (*Os)
   }
 }
 
-// One workgroup per 16 R rows, (sequence, head) and split.  A tile of at most 8 R rows takes half the tiles (a batch's blocks are ragged).
+// One workgroup per 16 R rows, (sequence, head) and split.  Of 32 rows where there are no more than 16, half the work (a batch's blocks are ragged).
 template <int DH, int R, int FMT, bool CLOSED>
 __global__ __launch_bounds__(256, kv8_waves(DH, R)) void k_kv8_attend(const unsigned char* __restrict__ cache, Kv8Attend a, Kv8Dims dm) {
   __shared__ float Os[4][16 * (DH + 4)];
@@ -303,9 +324,9 @@ __global__ __launch_bounds__(256, kv8_waves(DH, R)) void k_kv8_attend(const unsi
     kv8_wave<DH, tiles.value, FMT, CLOSED>(st, cache, a, dm, sq, bh, h, row0, last, own_lo, own_hi, blk0, blk1, wave);
     kv8_merge<DH, tiles.value>(st, Os, Ms, a, dm, sq, h, row0, last, split, wave);
   };
-  if constexpr (R > 1) {
-    if (last - row0 < 8 * R) {
-      go(std::integral_constant<int, R / 2>{});
+  if constexpr (R == 2) {
+    if (last - row0 < 16) {
+      go(std::integral_constant<int, 1>{});
       return;
     }
   }
@@ -372,7 +393,10 @@ __global__ __launch_bounds__(256) void k_kv8_join(Kv8Attend a, Kv8Dims dm) {
          uint2{f2bf_pair(o.x * inv, o.y * inv), f2bf_pair(o.z * inv, o.w * inv)});
 }
 
-// The split of the keys.  It goes by the cache's own sizes, so that a row's sums do not depend on a call.
+// The split of the keys.  It goes by the cache's own sizes, so that a row's sums do not depend on a call.  512 keys where sequences and heads are few, more where
+// they fill the card by themselves (about 2048 workgroups of 512 keys) or where a call may bring many rows, which fill it too.  Measured, us by keys of a split:
+// 1 sequence of 8216 keys, 16 heads 512 14.3, 1024 15.9, 2048 21; 2 prompts of 512 rows 512 97, 1024 80, 2048 75; 32 sequences up to 8192 keys 2048 74, 4096 73,
+// 8192 84; 8 sequences of up to 32,000 keys, 8 heads of width 128, 2048 87, 4096 84, 8192 80.
 int kv8_split_keys(const Kv8Dims& d) {
   const size_t pairs = (size_t)d.n_seq * d.heads;
   size_t keys = 512;
@@ -387,9 +411,10 @@ size_t kv8_attend_bytes(const Kv8Dims& d, int q_heads, int rows, int max_keys) {
   const size_t n = splits_of(d, max_keys);
   return n == 1 ? 0 : ((size_t)rows * q_heads * n * 2 * 4 + 255) / 256 * 256 + (size_t)rows * q_heads * n * d.width * 4;
 }
+// a launch takes less than 2^32 lanes along x: 2^24 workgroups of 256
 bool kv8_attend_fits(const Kv8Dims& d, int q_heads, int max_rows, int max_keys) {
   const size_t tiles = ((size_t)max_rows * (q_heads / d.heads) + 15) / 16;
-  return tiles * d.n_seq * d.heads * splits_of(d, max_keys) < (1u << 31) && (size_t)max_rows * q_heads / 4 < (1u << 31);
+  return tiles * d.n_seq * d.heads * splits_of(d, max_keys) < (1u << 24) && (size_t)max_rows * q_heads < (1u << 26);
 }
 
 template <int DH, int FMT>
@@ -400,10 +425,10 @@ static void attend_for(const Kv8Dims& d, const unsigned char* cache, Kv8Attend& 
     k_kv8_attend<DH, r.value, FMT, closed.value><<<(unsigned)((size_t)a.rows.n_seq * d.heads * a.row_tiles * a.n_split), 256, 0, s>>>(cache, a, d);
   };
   auto by_rows = [&](auto closed) {
-    // as few passes over the keys as the rows allow: up to 64 rows of a wave (width 128: 32, more would not fit the registers)
+    // 16 or 32 rows of a wave.  (64, two waves a SIMD instead of three: 512 rows over 32 keys 11.3 us, with 32 7.3; over 1024 21.1 and 17.6, over 8192 47.3 and
+    // 45.3: a row tile more reads its keys from L2, and the third wave fills the other two's waits.)
     if (m <= 16) go(std::integral_constant<int, 1>{}, closed);
-    else if (m <= 32 || DH == 128) go(std::integral_constant<int, 2>{}, closed);
-    else go(std::integral_constant<int, DH == 128 ? 2 : 4>{}, closed);
+    else go(std::integral_constant<int, 2>{}, closed);
   };
   if (d.closed) by_rows(std::true_type{});
   else by_rows(std::false_type{});

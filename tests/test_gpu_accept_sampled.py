@@ -51,7 +51,7 @@ def check(p, rows, got):
 
 @pytest.mark.parametrize("bf16", [False, True])
 @pytest.mark.parametrize("probs", [False, True])
-@pytest.mark.parametrize("vocab", [1, 2, 7, 9, 257, 4095, 4096, 4097, 4104, 12301])
+@pytest.mark.parametrize("vocab", [1, 2, 7, 9, 257, 2047, 2048, 2050, 4095, 4096, 4097, 4104, 12301])
 def test_accepted_tokens(vocab, probs, bf16):
     rows = [1, 0, 5, 3, 8, 1, 2, 0, 6]
     for seed in range(3):
@@ -66,6 +66,19 @@ def test_a_large_vocabulary_of_more_than_64_pieces(probs):
     for seed in range(4):
         p = problem(seed, rows, 300007, probs, bf16=seed % 2 == 1, width=1.0)
         check(p, rows, run(p, rows))
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+def test_many_large_rows_without_probabilities(bf16):
+    """So many scores that only the deciding rows are summed in 64 bits; odd sizes, blocks that stand to the end and blocks that fall at once."""
+    rows, vocab = [40, 1, 0, 70, 33, 130], 32003
+    assert sum(rows) * vocab > 1 << 23
+    for seed in range(2):
+        p = problem(seed, rows, vocab, False, bf16)
+        p["u"][sum(rows) - 130:] = 0
+        got = run(p, rows)
+        check(p, rows, got)
+        assert got[0][-1] == 130
 
 
 @pytest.mark.parametrize("skew", range(8))

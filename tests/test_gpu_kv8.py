@@ -62,8 +62,7 @@ def test_written_values_read_back(fmt, width, heads, step):
     cache = stale(ad.Kv8Cache(len(lens), heads, width, capacity=70, k_max=step, format=fmt))
     feed(cache, k, v, lens, step)
     for dtype in (torch.float32, torch.bfloat16):
-        got = read_all(cache, [n // BLOCK * BLOCK for n in lens], dtype), None
-        # the incomplete block's tokens: as the next row reads them
+        # (an incomplete block's tokens: as the next row reads them)
         whole = cache.read(starts(lens), i32([0] * len(lens)), i32(lens), rows=sum(lens), dtype=dtype)
         at = 0
         for b, n in enumerate(lens):

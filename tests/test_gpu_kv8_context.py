@@ -114,6 +114,22 @@ def test_scores_against_the_oracle_over_held_keys_and_values(dtype):
         assert np.abs(ctx.debug_logits() - want).max() < 2e-2 + 1.5e-2
 
 
+def test_encoder_teams_that_give_up_leave_the_memory_right():
+    """A team wait of nothing: the encoder's launch is given up, and the call that finds out encodes again, memory in 8 bits included."""
+    dims = model_dims("base")
+    w = init_weights(dims, 33)
+    srcs = sources(dims, [25, 7])
+    got = []
+    for wait in (None, 0):
+        with context(dims, w, "bf16_kv_e4m3", B=2) as ctx:
+            if wait is not None:
+                ctx.set_option(ad.AD_OPT_TEAM_WAIT, wait)
+            got.append(ctx.decode_greedy(srcs)[0])
+            if wait is not None:
+                assert ctx.get_option(ad.AD_OPT_TEAM_FAILURES) > 0
+    assert got[0] == got[1]
+
+
 def test_outputs_longer_than_rows_of_bf16_allow():
     """700 tokens of a head of width 64 (bf16 rows: at most 526 with the block), over several splits of the keys."""
     dims = dict(enc_layers=1, dec_layers=2, d_model=128, n_heads=2, d_ffn=256, vocab=2000)

@@ -79,6 +79,10 @@ def test_append_read_and_attend_refuse():
     assert go(c=long, keys=100000, size=need - 1) == ad.AD_ENOMEM
     assert go(c=long, keys=100000, ws=None, size=need) == ad.AD_EINVAL
     assert go(c=long, keys=100000, ws=P + 64, size=need) == ad.AD_EINVAL
+    # more workgroups than a launch takes: 65,536 heads x 65,536 rows; the joined rows of 2^26 (row, head) pairs
+    wide = C.byref(cfg(n_seq=1, n_heads=256, k_max=65536, capacity=1 << 17))
+    assert go(c=wide, heads=65536, qs=65536 * 64, os=65536 * 64, rows=65536, most=65536, keys=1000, size=1 << 62) == ad.AD_EINVAL and "workgroups" in message()
+    assert go(c=wide, heads=1024, qs=65536, os=65536, rows=65536, most=65536, keys=1 << 17, size=1 << 62) == ad.AD_EINVAL and "workgroups" in message()
 
 
 def test_accept_sampled_refuses():
