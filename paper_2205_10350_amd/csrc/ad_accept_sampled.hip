@@ -51,11 +51,12 @@ __device__ __forceinline__ double exp2_down(double t) {
   p = fma(p, f, 1.0);
   return ldexp(p, (int)n);
 }
-// The same for the bulk of the scores, 16 instructions: t = fma(x, rate, off) held to [-1020, ..] (what is smaller weighs nothing beside the 1 of the maximum; a NaN is
+// The same for the bulk of the scores, 17 instructions: t = (x - m) rate (the difference first, which is exact: at temperatures near 0 a rounded product of the maximum
+// would be no small part of what is left of it) held to [-1020, ..] (what is smaller weighs nothing beside the 1 of the maximum; a NaN is
 // the caller's to see), the whole part through the low word of t + 1.5 * 2^52 straight into the exponent, and 2^f to f^9 (7e-12 relative: a drawn number falls
 // between this and the exact border once in 10^11 / vocab draws).
-__device__ __forceinline__ double exp2_bulk(float x, double rate, double off) {
-  const double t = fmax(fma((double)x, rate, off), -1020.0);
+__device__ __forceinline__ double exp2_bulk(float x, double rate, double m) {
+  const double t = fmax(((double)x - m) * rate, -1020.0);
   const double big = t + 6755399441055744.0, f = t - (big - 6755399441055744.0);
   double p = 1.01780860092396997275e-7;    // ln(2)^k / k!, k = 9 .. 0
   p = fma(p, f, 1.32154867901443094884e-6);
@@ -72,8 +73,8 @@ __device__ __forceinline__ double exp2_bulk(float x, double rate, double off) {
   return __builtin_bit_cast(double, (long long)((unsigned long long)hi << 32 | (unsigned)bits));
 }
 // and to f^11, nothing below 2^-1000, for the rows that are drawn from
-__device__ __forceinline__ double exp2_weight(float x, double rate, double off) {
-  const double u = fma((double)x, rate, off), t = fmax(u, -1020.0);
+__device__ __forceinline__ double exp2_weight(float x, double rate, double m) {
+  const double u = ((double)x - m) * rate, t = fmax(u, -1020.0);
   const double big = t + 6755399441055744.0, f = t - (big - 6755399441055744.0);
   double p = 4.44553827187081149760e-10;   // ln(2)^k / k!, k = 11 .. 0
   p = fma(p, f, 7.05491162080112332988e-9);
@@ -201,16 +202,15 @@ __global__ __launch_bounds__(kAcceptThreads) void k_accept_stats(AcceptArgs a) {
     const bool here = t < x.heads(c) && t != skip;
     nan = accept_drop(x, c, t, skip, v) || nan;
     if constexpr (WIDE) {
-      const double off = -(double)m * rate;
 #pragma unroll
       for (int j = 0; j < kEach<T>; ++j) {
         nan = nan || v[j] != v[j];
-        s += exp2_bulk(v[j], rate, off);
+        s += exp2_bulk(v[j], rate, (double)m);
       }
-      if (here) s += exp2_bulk(head, rate, off);
+      if (here) s += exp2_bulk(head, rate, (double)m);
     } else {
       // (a row's test alone rests on these sums: 2^-24 of a probability is where a drawn number of 24 bits may fall either way)
-      const float r = (float)rate;
+      const float r = fminf((float)rate, 0x1.fffffep127f);   // (of a temperature below 2^-127 no infinity, which times a difference of 0 would be NaN)
       float e[4] = {here ? __builtin_amdgcn_exp2f((head - m) * r) : 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int j = 0; j < kEach<T>; ++j) e[j % 4] += __builtin_amdgcn_exp2f((v[j] - m) * r);
@@ -312,17 +312,17 @@ template <bool PROBS> struct AcceptWeight {
   const float* q;
   float drafted;   // 0: nothing was drafted, q does not count
   int skip;
-  double rate, off, inv_z;
-  __device__ __forceinline__ AcceptWeight(const AcceptArgs& a, int row, float m, double z, double rate_) {
+  double rate, m, inv_z;
+  __device__ __forceinline__ AcceptWeight(const AcceptArgs& a, int row, float m_, double z, double rate_) {
     const int d = a.draft[row];
     const bool is = accept_drafted(a, d);
     q = PROBS ? a.probs + (size_t)row * a.probs_stride : nullptr;
     drafted = is ? 1.f : 0.f;
     skip = !PROBS && is ? d : -1;
-    rate = rate_; off = -(double)m * rate_; inv_z = 1.0 / z;
+    rate = rate_; m = m_; inv_z = 1.0 / z;
   }
   __device__ __forceinline__ double operator()(int i, float x) const {
-    const double e = exp2_weight(x, rate, off);
+    const double e = exp2_weight(x, rate, m);
     if constexpr (PROBS) return fmax(fma(e, inv_z, -(double)(drafted != 0.f ? q[i] : 0.f)), 0.0);
     return e;
   }

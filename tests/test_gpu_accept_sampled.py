@@ -81,6 +81,38 @@ def test_many_large_rows_without_probabilities(bf16):
         assert got[0][-1] == 130
 
 
+@pytest.mark.parametrize("probs", [False, True])
+@pytest.mark.parametrize("rows,vocab", [([3, 1, 4], 4100), ([90, 100, 80], 32003)])
+def test_temperatures_near_zero_and_very_high(rows, vocab, probs):
+    """Towards 0 the most likely token alone is left, whatever the sizes of scores and their sums; a very high one leaves all alike."""
+    for t in (1e-6, 1e-8, 1e-20, 1e-40):
+        p = problem(7, rows, vocab, probs, width=30.0)
+        two = p["x"].topk(2, -1).values
+        assert (two[:, 0] - two[:, 1]).min() > 1e-5 * 20
+        best = p["x"].argmax(-1).numpy()
+        p["t"][:] = t
+        p["u"][:] = 0.999
+        p["d"][:] = best
+        if probs:
+            p["q"][:] = torch.nn.functional.one_hot(torch.tensor(best), vocab).float()
+        check(p, rows, run(p, rows))
+        assert run(p, rows)[0] == rows                                   # every drafted token stands
+        for last in np.cumsum(rows) - 1:
+            p["d"][last] = (best[last] + 1) % vocab
+            if probs:
+                p["q"][last] = p["q"][last].roll(1)                      # (the drafter is as sure of the wrong token)
+        got = run(p, rows)
+        check(p, rows, got)
+        assert got[0] == rows and [got[1][i] for i in np.cumsum(rows) - 1] == [best[i] for i in np.cumsum(rows) - 1]
+    p = problem(8, rows, vocab, probs)
+    p["t"][:] = 3e38
+    p["d"][:] = ad.AD_NEVER
+    n, tok = run(p, rows)
+    assert n == [1] * len(rows)
+    for b, at in enumerate(np.cumsum([0] + rows[:-1])):
+        assert abs(tok[at] - float(p["v"][b]) * vocab) <= 1
+
+
 @pytest.mark.parametrize("skew", range(8))
 @pytest.mark.parametrize("bf16", [False, True])
 def test_rows_at_every_alignment(skew, bf16):
