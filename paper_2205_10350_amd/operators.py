@@ -43,6 +43,12 @@ def _rows(t, name, index, dtype, heads, width):
     _refuse(f"{name} must be a {dtype} tensor [rows, {heads}, {width}] on cuda:{index}, the heads of a row side by side")
 
 
+def _count(name, n):
+    if not -2**31 <= n < 2**31:
+        _refuse(f"{name}: {n} is no 32-bit number")
+    return n
+
+
 def _on(index, call):
     """call(stream) with GPU `index` current and its current stream."""
     import torch
@@ -69,20 +75,36 @@ class Kv8Cache:
         import torch
         if format not in _FORMATS:
             _refuse("format must be 'e4m3' or 'i8'")
+        for n in (n_seq, n_heads, head_width, capacity, k_max):
+            _count("the cache's sizes", n)
         self.cfg = B.AdKv8Config(n_seq, n_heads, head_width, capacity, k_max, _FORMATS[format], int(bool(closed)))
         self._cfg = C.byref(self.cfg)
         self.L = B.lib()
         B._check(self.L.ad_kv8_check(self._cfg))
         self.most_rows = capacity if closed else k_max
         device = torch.device(device)
+        if device.type != "cuda":
+            _refuse("the cache must be on a GPU")
         self.index = torch.cuda.current_device() if device.index is None else device.index
         self.device = torch.device("cuda", self.index)
         self.memory = torch.empty(self.L.ad_kv8_bytes(self._cfg), dtype=torch.uint8, device=self.device)
+        self._streams = {torch.cuda.current_stream(self.device).cuda_stream}
         self._at = self.memory.data_ptr()
         self._start, self._len = (n_seq + 1,), (n_seq,)
         self._i32, self._bf16 = torch.int32, torch.bfloat16
         self._scale = 1.0 / math.sqrt(head_width)
         self._need = {}
+
+    def _call(self, call):
+        def on(stream):
+            if stream not in self._streams:   # (the allocator is to wait for that stream, too, before it gives the memory to others)
+                import torch
+                self.memory.record_stream(torch.cuda.current_stream(self.device))
+                self._streams.add(stream)
+            return call(stream)
+        rc = _on(self.index, on)
+        if rc:
+            B._check(rc)
 
     def append(self, k, v, row_start, length, max_rows=None):
         """Rows k, v [rows, n_heads, head_width] bf16 become the tokens from length[b] on."""
@@ -92,10 +114,8 @@ class Kv8Cache:
         if vrows != rows:
             _refuse("k and v must have as many rows")
         start, at = _flat(row_start, "row_start", i, self._i32, self._start), _flat(length, "length", i, self._i32, self._len)
-        most = min(rows, self.most_rows) if max_rows is None else max_rows
-        rc = _on(i, lambda stream: self.L.ad_kv8_append(self._cfg, self._at, kp, ks, vp, vs, start, at, rows, most, stream))
-        if rc:
-            B._check(rc)
+        most = min(rows, self.most_rows) if max_rows is None else _count("max_rows", max_rows)
+        self._call(lambda stream: self.L.ad_kv8_append(self._cfg, self._at, kp, ks, vp, vs, start, at, rows, most, stream))
 
     def read(self, row_start, begin, length, rows, max_rows=None, dtype=None):
         """The values the cache stands for, (k, v) [rows, n_heads, head_width]: tokens begin[b] .. of sequence b, as the row at position
@@ -105,15 +125,15 @@ class Kv8Cache:
         if dtype not in (torch.bfloat16, torch.float32):
             _refuse("dtype must be bfloat16 or float32")
         c, i = self.cfg, self.index
+        _count("rows", rows)
         start, first = _flat(row_start, "row_start", i, self._i32, self._start), _flat(begin, "begin", i, self._i32, self._len)
         at = _flat(length, "length", i, self._i32, self._len)
         k = torch.empty((rows, c.n_heads, c.head_width), dtype=dtype, device=self.device)
         v = torch.empty_like(k)
         kp, vp = k.data_ptr(), v.data_ptr()
-        rc = _on(i, lambda stream: self.L.ad_kv8_read(self._cfg, self._at, start, first, at, rows, rows if max_rows is None else max_rows,
-                                                      B.AD_F32 if dtype is torch.float32 else B.AD_BF16, kp, vp, stream))
-        if rc:
-            B._check(rc)
+        most = rows if max_rows is None else _count("max_rows", max_rows)
+        kind = B.AD_F32 if dtype is torch.float32 else B.AD_BF16
+        self._call(lambda stream: self.L.ad_kv8_read(self._cfg, self._at, start, first, at, rows, most, kind, kp, vp, stream))
         return k, v
 
     def attend(self, q, row_start, length, max_rows=None, max_keys=None, scale=None, out=None):
@@ -124,8 +144,8 @@ class Kv8Cache:
         heads = q.shape[1] if isinstance(q, torch.Tensor) and q.dim() == 3 else 0
         qp, qs, rows = _rows(q, "q", i, self._bf16, heads, c.head_width)
         start, at = _flat(row_start, "row_start", i, self._i32, self._start), _flat(length, "length", i, self._i32, self._len)
-        most = (rows if c.closed else min(rows, c.k_max)) if max_rows is None else max_rows
-        keys = c.capacity if max_keys is None else max_keys
+        most = (rows if c.closed else min(rows, c.k_max)) if max_rows is None else _count("max_rows", max_rows)
+        keys = c.capacity if max_keys is None else min(max_keys, c.capacity)
         scale = self._scale if scale is None else scale
 
         def call(stream):
@@ -148,9 +168,7 @@ class Kv8Cache:
             ws = torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
             return self.L.ad_kv8_attend(self._cfg, self._at, qp, qs, heads, start, at, rows, most, keys, scale, op, os,
                                         None if ws is None else ws.data_ptr(), need, stream)
-        rc = _on(i, call)
-        if rc:
-            B._check(rc)
+        self._call(call)
         return out
 
 
@@ -186,7 +204,7 @@ def accept_sampled(logits, draft, row_start, accept_u, pick_u, temperature=None,
         ws = torch.empty(max(need, 1), dtype=torch.uint8, device=logits.device)
         return B.lib().ad_accept_sampled(logits.data_ptr(), B.AD_F32 if logits.dtype is f32 else B.AD_BF16, stride if rows > 1 else vocab, vocab,
                                          drafted, probs, probs_stride if rows > 1 else vocab, temp, u, v, start, n_seq, rows,
-                                         rows if max_rows is None else max_rows, n_accept.data_ptr(), tokens.data_ptr(), ws.data_ptr(), need, stream)
+                                         rows if max_rows is None else _count("max_rows", max_rows), n_accept.data_ptr(), tokens.data_ptr(), ws.data_ptr(), need, stream)
     rc = _on(i, call)
     if rc:
         B._check(rc)

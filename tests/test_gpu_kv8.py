@@ -298,6 +298,27 @@ def test_on_another_stream():
     assert torch.equal(got, want.attend(q, some, tail))
 
 
+def test_memory_outlives_the_calls_of_another_stream():
+    """A cache that is dropped while another stream's calls on it wait keeps its memory until they have run."""
+    heads, w, n = 2, 64, 4000
+    k, v, q = draw(33, 1, n, heads, w), draw(34, 1, n, heads, w), draw(35, 5, heads, w).cuda()
+    cache = ad.Kv8Cache(1, heads, w, capacity=n, k_max=n)
+    feed(cache, k, v, [n], n)
+    some, tail = starts([5]), i32([n - 5])
+    want = cache.attend(q, some, tail)
+    side, busy = torch.cuda.Stream(), torch.zeros(4096, 4096, device="cuda")
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for _ in range(40):
+            busy = busy @ busy
+        got = cache.attend(q, some, tail)
+    size = cache.memory.numel()
+    del cache
+    others = [torch.full((size,), 0x55, dtype=torch.uint8, device="cuda") for _ in range(4)]
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and len(others) == 4
+
+
 def test_a_long_cache_past_32_bits():
     """Offsets of the last sequence lie beyond 4 GiB."""
     heads, w, cap, n_seq = 8, 128, 1 << 17, 17

@@ -105,6 +105,10 @@ def test_wrappers_refuse_tensors_that_do_not_fit():
     torch = pytest.importorskip("torch")
     with pytest.raises(ad.AdError):
         ad.Kv8Cache(1, 4, 64, 100, format="fp4", device="cuda:0")
+    with pytest.raises(ad.AdError, match="GPU"):
+        ad.Kv8Cache(1, 4, 64, 100, device="cpu")
+    with pytest.raises(ad.AdError, match="32-bit"):
+        ad.Kv8Cache(1, 4, 64, (1 << 32) + 100, device="cuda:0")
     with pytest.raises(ad.AdError):
         ad.accept_sampled(torch.zeros(2, 10), None, None, None, None)      # not on a GPU
     with pytest.raises(ad.AdError):
