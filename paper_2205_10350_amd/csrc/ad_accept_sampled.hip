@@ -25,6 +25,7 @@
 namespace ad {
 
 constexpr int kAcceptThreads = 256;
+constexpr int kRowsY = 32768;                                       // rows along y of a launch, the others along z
 constexpr int kDecideThreads = 1024;                                // where a sequence's rows are tested, a wave a row
 // scores of a workgroup (8 KB: 32 blocks with the drafter's probabilities 39 us with 16 KB, 35 with 8; 64 of bf16 41 with 4 KB, 39 with 8) and of a thread
 template <typename T> constexpr int kPiece = 8192 / (int)sizeof(T);
@@ -168,6 +169,24 @@ __device__ __forceinline__ AcceptSeq accept_seq(const AcceptArgs& a, int b) {
   if (s.row0 < 0 || s.row0 > a.rows) s.n = 0;
   return s;
 }
+// The packed row that a workgroup or wave works on and its sequence; b = -1: none.
+// By sequence: row i of sequence b.  By packed row `at` (PACKED): the last sequence that starts there or before (of several, those before it are empty), found by each
+// wave for itself: every 64th start at once, then those between two of them.
+struct AcceptAt { int b, row; };
+template <bool PACKED> __device__ __forceinline__ AcceptAt accept_at(const AcceptArgs& a, int b, int i) {
+  if constexpr (!PACKED) {
+    const AcceptSeq sq = accept_seq(a, b);
+    return AcceptAt{i < sq.n ? b : -1, sq.row0 + i};
+  }
+  const int lane = threadIdx.x & 63, apart = (a.n_seq + 63) / 64, at = b * kRowsY + i;
+  int q = __popcll(__ballot(lane * apart < a.n_seq && a.row_start[min(lane * apart, a.n_seq - 1)] <= at)) - 1;
+  if (q < 0 || at >= a.rows) return AcceptAt{-1, 0};
+  q *= apart;
+  if (apart > 1) q += __popcll(__ballot(lane < apart && q + lane < a.n_seq && a.row_start[min(q + lane, a.n_seq - 1)] <= at)) - 1;
+  if (q < 0) return AcceptAt{-1, 0};   // (starts that do not ascend)
+  const AcceptSeq sq = accept_seq(a, q);
+  return AcceptAt{at >= sq.row0 && at - sq.row0 < sq.n ? q : -1, at};
+}
 // log2(e) / T; NaN where T is no positive number
 __device__ __forceinline__ double accept_rate(const AcceptArgs& a, int b) {
   const float t = a.temperature ? a.temperature[b] : 1.f;
@@ -175,14 +194,14 @@ __device__ __forceinline__ double accept_rate(const AcceptArgs& a, int b) {
 }
 __device__ __forceinline__ bool accept_drafted(const AcceptArgs& a, int d) { return d >= 0 && d < a.vocab; }
 
-template <typename T, bool WIDE>
+template <typename T, bool WIDE, bool PACKED>
 __global__ __launch_bounds__(kAcceptThreads) void k_accept_stats(AcceptArgs a) {
   __shared__ float ms[kAcceptThreads / 64];
   __shared__ double ss[kAcceptThreads / 64];
-  const int c = blockIdx.x, b = blockIdx.z, t = threadIdx.x;
-  const AcceptSeq sq = accept_seq(a, b);
-  if ((int)blockIdx.y >= sq.n) return;
-  const int row = sq.row0 + blockIdx.y;
+  const int c = blockIdx.x, t = threadIdx.x;
+  const AcceptAt at = accept_at<PACKED>(a, blockIdx.z, blockIdx.y);
+  if (at.b < 0) return;
+  const int b = at.b, row = at.row;
   const AcceptRow<T> x(a, row);
   float v[kEach<T>];
   x.load(c, t, v);
@@ -283,13 +302,12 @@ template <typename T> __device__ __forceinline__ int accept_first(const AcceptAr
 }
 
 // The test of all rows at once, a wave a row
-template <typename T>
+template <typename T, bool PACKED>
 __global__ __launch_bounds__(kAcceptThreads) void k_accept_rows(AcceptArgs a) {
-  const int i = blockIdx.x * (kAcceptThreads / 64) + (threadIdx.x >> 6), b = blockIdx.y;
-  const AcceptSeq sq = accept_seq(a, b);
-  if (i >= sq.n) return;
-  const AcceptRowInfo r = accept_decide<T>(a, sq.row0 + i, accept_rate(a, b));
-  if ((threadIdx.x & 63) == 0) a.row_info[sq.row0 + i] = r;
+  const AcceptAt at = accept_at<PACKED>(a, blockIdx.y, blockIdx.x * (kAcceptThreads / 64) + (threadIdx.x >> 6));
+  if (at.b < 0) return;
+  const AcceptRowInfo r = accept_decide<T>(a, at.row, accept_rate(a, at.b));
+  if ((threadIdx.x & 63) == 0) a.row_info[at.row] = r;
 }
 // The first row whose token does not stand, with its maximum and sum, from there, by each wave for itself
 struct AcceptFirst { int i; float m; double z; };
@@ -549,18 +567,23 @@ void launch_accept_sampled(int dtype, AcceptArgs a, void* ws, hipStream_t s) {
   // 352 rows of 100,003 in bf16 47 / 39).
   const bool wide = a.probs || (size_t)a.rows * a.vocab < ((size_t)1 << 23);
   a.rest = a.probs || !wide;
+  // Rows by sequence (max_rows of every one), or packed, which costs each workgroup the search for its sequence, where that would be mostly rows that are not there (us, by
+  // sequence / packed: 32 blocks of up to 25 rows 35.2 / 36.1, 64 of 8 rows of 100,003 45.8 / 47; 256 of 8 rows of 32,000 and max_rows = 8 62 / 69, without a bound 2041 / 69).
+  const bool packed = (size_t)a.n_seq * a.max_rows > 4 * (size_t)a.rows;
+  const dim3 by = packed ? dim3(1, std::min(a.rows, kRowsY), (a.rows + kRowsY - 1) / kRowsY) : dim3(1, a.max_rows, a.n_seq);
   char* w = (char*)ws;
   a.piece_sum = (double*)w;
   a.piece_max = (float*)(w + up256((size_t)a.rows * a.pieces * 8));
   a.rest_sum = (double*)((char*)a.piece_max + up256((size_t)a.rows * a.pieces * 4));
   a.row_info = (AcceptRowInfo*)((char*)a.rest_sum + up256((size_t)a.n_seq * a.pieces * 8));
-  auto go = [&](auto one) {
+  auto go = [&](auto one, auto pk) {
     typedef decltype(one) T;
-    const dim3 grid(a.pieces, a.max_rows, a.n_seq);
-    if (wide) k_accept_stats<T, true><<<grid, kAcceptThreads, 0, s>>>(a);
-    else k_accept_stats<T, false><<<grid, kAcceptThreads, 0, s>>>(a);
+    constexpr bool PK = pk.value;
+    const dim3 grid(a.pieces, by.y, by.z);
+    if (wide) k_accept_stats<T, true, PK><<<grid, kAcceptThreads, 0, s>>>(a);
+    else k_accept_stats<T, false, PK><<<grid, kAcceptThreads, 0, s>>>(a);
     if (a.rest) {
-      k_accept_rows<T><<<dim3((a.max_rows + 3) / 4, a.n_seq), kAcceptThreads, 0, s>>>(a);
+      k_accept_rows<T, PK><<<dim3((by.y + 3) / 4, by.z), kAcceptThreads, 0, s>>>(a);
       auto draw = [&](auto probs) {
         k_accept_rest<T, probs.value><<<dim3(a.pieces, a.n_seq), kAcceptThreads, 0, s>>>(a);
         k_accept_pick<T, true, probs.value><<<a.n_seq, kAcceptThreads, 0, s>>>(a);
@@ -571,8 +594,12 @@ void launch_accept_sampled(int dtype, AcceptArgs a, void* ws, hipStream_t s) {
       k_accept_pick<T, false, false><<<a.n_seq, kDecideThreads, 0, s>>>(a);
     }
   };
-  if (dtype == AD_BF16) go(bf16_t{});
-  else go(float{});
+  auto of_type = [&](auto pk) {
+    if (dtype == AD_BF16) go(bf16_t{}, pk);
+    else go(float{}, pk);
+  };
+  if (packed) of_type(std::true_type{});
+  else of_type(std::false_type{});
 }
 
 }  // namespace ad

@@ -48,6 +48,15 @@ struct Kv8Rows {
   const int *start, *count, *base;
   int stride, rows, max_rows, n_seq;
 };
+// How a launch deals out a sequence's pieces of 2^shift / mul rows: as many to every sequence as max_rows have, or, where most of those would not be there, packed:
+// sequence b's begin at (start[b] mul >> shift) + extra b, and each workgroup looks its sequence up.  (256 sequences of 25 rows over closed caches of 400 tokens, us without a bound:
+// by sequence 653, packed 57, with max_rows = 25 and by sequence 50.)
+struct Kv8Deal { int packed, mul, shift, extra; size_t pieces; };   // pieces: of a sequence; packed: of all
+inline Kv8Deal kv8_deal(const Kv8Rows& r, int mul, int shift, int extra, size_t of_one) {
+  const size_t all = ((size_t)r.rows * mul >> shift) + (size_t)extra * r.n_seq;
+  const bool packed = of_one * r.n_seq > 4 * all && all < ((size_t)1 << 23);
+  return Kv8Deal{packed, mul, shift, extra, packed ? all : of_one};
+}
 
 // Keys and values of the rows (bf16, [rows, heads, width] with row strides in elements) behind base[b] tokens.
 void launch_kv8_append(const Kv8Dims& d, void* cache, const void* k, const void* v, size_t k_stride, size_t v_stride, const Kv8Rows& r, hipStream_t s);
@@ -57,7 +66,7 @@ void launch_kv8_read(const Kv8Dims& d, const void* cache, const Kv8Rows& r, cons
 int kv8_split_keys(const Kv8Dims& d);
 // Attention of the rows over the cache; q_heads / heads query heads share a head.  ws: kv8_attend_bytes().
 size_t kv8_attend_bytes(const Kv8Dims& d, int q_heads, int rows, int max_keys);
-bool kv8_attend_fits(const Kv8Dims& d, int q_heads, int max_rows, int max_keys);   // its workgroups are fewer than a launch may have
+bool kv8_attend_fits(const Kv8Dims& d, const Kv8Rows& r, int q_heads, int max_keys);   // its workgroups are fewer than a launch may have
 void launch_kv8_attend(const Kv8Dims& d, const void* cache, const void* q, size_t q_stride, void* out, size_t out_stride, int q_heads,
                        const Kv8Rows& r, int max_keys, float scale, void* ws, hipStream_t s);
 

@@ -59,15 +59,18 @@ template <int FMT> __device__ __forceinline__ unsigned kv8_pack4(const float (&x
 // (A thread's bytes are packed into words by hand: through arrays that were read under another type the compiler put them into scratch memory, 41 us.)
 template <int DH, int FMT, bool CLOSED>
 __global__ __launch_bounds__(4 * DH) void k_kv8_append(unsigned char* __restrict__ cache, const bf16_t* __restrict__ k, const bf16_t* __restrict__ v,
-                                                       size_t k_stride, size_t v_stride, Kv8Rows rt, Kv8Dims dm) {
+                                                       size_t k_stride, size_t v_stride, Kv8Rows rt, Kv8Deal deal, Kv8Dims dm) {
   constexpr int kThreads = 4 * DH, kHalf = 2 * DH, kWaves = kThreads / 64, kLdv = DH + 2;
   __shared__ bf16_t Vs[kKv8Block * kLdv];
   __shared__ unsigned bad[kKv8Block];
   __shared__ float most[kWaves];
-  const int b = blockIdx.z, h = blockIdx.y;
+  const int b = deal.packed ? kv8_owner(rt, deal, blockIdx.x) : blockIdx.z, h = blockIdx.y;
+  if (b < 0) return;
   const Kv8Seq sq = kv8_seq(rt, b, dm.capacity);
   if (sq.n <= 0 || (CLOSED && sq.base != 0)) return;
-  const int blk = sq.base / kKv8Block + blockIdx.x, tok0 = blk * kKv8Block, end = sq.base + sq.n;
+  const int piece = deal.packed ? (int)blockIdx.x - kv8_first(rt, deal, b) : (int)blockIdx.x;
+  if (piece < 0) return;
+  const int blk = sq.base / kKv8Block + piece, tok0 = blk * kKv8Block, end = sq.base + sq.n;
   if (tok0 >= end) return;
   const int t = threadIdx.x, u = t % kHalf, lane = t & 63, r = lane & 15, g = lane >> 4;
   const bool values = t >= kHalf;   // (whole waves: kHalf is a multiple of 64)
@@ -162,15 +165,18 @@ __global__ __launch_bounds__(4 * DH) void k_kv8_append(unsigned char* __restrict
 // 75 MB in 14.4 us, 5.2 TB/s; one token 3.3 us.
 template <int DH, int FMT, typename T>
 __global__ __launch_bounds__(4 * DH) void k_kv8_read(const unsigned char* __restrict__ cache, Kv8Rows rt, const int* __restrict__ length,
-                                                     T* __restrict__ k_out, T* __restrict__ v_out, Kv8Dims dm) {
+                                                     T* __restrict__ k_out, T* __restrict__ v_out, Kv8Deal deal, Kv8Dims dm) {
   constexpr int kHalf = 2 * DH, kLdv = DH + 1;
   __shared__ float Vs[kKv8Block * kLdv];
-  const int b = blockIdx.z, h = blockIdx.y;
+  const int b = deal.packed ? kv8_owner(rt, deal, blockIdx.x) : blockIdx.z, h = blockIdx.y;
+  if (b < 0) return;
   Kv8Seq sq = kv8_seq(rt, b, dm.capacity);
   const int len = min(max(length[(size_t)b * rt.stride], 0), dm.capacity);
   sq.n = min(sq.n, len - sq.base);
   if (sq.n <= 0) return;
-  const int blk = sq.base / kKv8Block + blockIdx.x, tok0 = blk * kKv8Block, end = sq.base + sq.n;
+  const int piece = deal.packed ? (int)blockIdx.x - kv8_first(rt, deal, b) : (int)blockIdx.x;
+  if (piece < 0) return;
+  const int blk = sq.base / kKv8Block + piece, tok0 = blk * kKv8Block, end = sq.base + sq.n;
   if (tok0 >= end) return;
   const int t = threadIdx.x, u = t % kHalf, lane = t & 63, r = lane & 15, g = lane >> 4, s = u >> 6;
   const bool values = t >= kHalf;
@@ -217,24 +223,28 @@ __global__ __launch_bounds__(4 * DH) void k_kv8_read(const unsigned char* __rest
 }
 
 template <int DH, int FMT>
-static void append_for(const Kv8Dims& d, unsigned char* cache, const bf16_t* k, const bf16_t* v, size_t ks, size_t vs, const Kv8Rows& r, dim3 grid, hipStream_t s) {
-  if (d.closed) k_kv8_append<DH, FMT, true><<<grid, 4 * DH, 0, s>>>(cache, k, v, ks, vs, r, d);
-  else k_kv8_append<DH, FMT, false><<<grid, 4 * DH, 0, s>>>(cache, k, v, ks, vs, r, d);
+static void append_for(const Kv8Dims& d, unsigned char* cache, const bf16_t* k, const bf16_t* v, size_t ks, size_t vs, const Kv8Rows& r, const Kv8Deal& deal, dim3 grid, hipStream_t s) {
+  if (d.closed) k_kv8_append<DH, FMT, true><<<grid, 4 * DH, 0, s>>>(cache, k, v, ks, vs, r, deal, d);
+  else k_kv8_append<DH, FMT, false><<<grid, 4 * DH, 0, s>>>(cache, k, v, ks, vs, r, deal, d);
 }
+// blocks that rows touch: wherever they begin, one or two more than fill them
+static Kv8Deal kv8_blocks(const Kv8Rows& r) { return kv8_deal(r, 1, 5, 2, ((size_t)r.max_rows + kKv8Block - 2) / kKv8Block + 1); }
 void launch_kv8_append(const Kv8Dims& d, void* cache, const void* k, const void* v, size_t k_stride, size_t v_stride, const Kv8Rows& r, hipStream_t s) {
-  const dim3 grid((r.max_rows + kKv8Block - 2) / kKv8Block + 1, d.heads, r.n_seq);
+  const Kv8Deal deal = kv8_blocks(r);
+  const dim3 grid((unsigned)deal.pieces, d.heads, deal.packed ? 1 : r.n_seq);
   kv8_dispatch(d, [&](auto width, auto fmt) {
-    append_for<width.value, fmt.value>(d, (unsigned char*)cache, (const bf16_t*)k, (const bf16_t*)v, k_stride, v_stride, r, grid, s);
+    append_for<width.value, fmt.value>(d, (unsigned char*)cache, (const bf16_t*)k, (const bf16_t*)v, k_stride, v_stride, r, deal, grid, s);
   });
 }
 
 void launch_kv8_read(const Kv8Dims& d, const void* cache, const Kv8Rows& r, const int* length, int dtype, void* k_out, void* v_out, hipStream_t s) {
-  const dim3 grid((r.max_rows + kKv8Block - 2) / kKv8Block + 1, d.heads, r.n_seq);
+  const Kv8Deal deal = kv8_blocks(r);
+  const dim3 grid((unsigned)deal.pieces, d.heads, deal.packed ? 1 : r.n_seq);
   kv8_dispatch(d, [&](auto width, auto fmt) {
     if (dtype == AD_BF16)
-      k_kv8_read<width.value, fmt.value, bf16_t><<<grid, 4 * width.value, 0, s>>>((const unsigned char*)cache, r, length, (bf16_t*)k_out, (bf16_t*)v_out, d);
+      k_kv8_read<width.value, fmt.value, bf16_t><<<grid, 4 * width.value, 0, s>>>((const unsigned char*)cache, r, length, (bf16_t*)k_out, (bf16_t*)v_out, deal, d);
     else
-      k_kv8_read<width.value, fmt.value, float><<<grid, 4 * width.value, 0, s>>>((const unsigned char*)cache, r, length, (float*)k_out, (float*)v_out, d);
+      k_kv8_read<width.value, fmt.value, float><<<grid, 4 * width.value, 0, s>>>((const unsigned char*)cache, r, length, (float*)k_out, (float*)v_out, deal, d);
   });
 }
 

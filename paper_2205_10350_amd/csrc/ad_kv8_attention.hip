@@ -36,7 +36,7 @@ struct Kv8Attend {
   Kv8Rows rows;
   int group;                 // query heads that share a head
   int split_blocks, n_split; // blocks of a split; splits launched
-  int row_tiles;             // workgroups of 16 R rows for a (sequence, head)
+  Kv8Deal tiles, one;        // how tiles of 16 R rows, and single rows, are dealt out
   float scale;               // of the scores, times log2(e)
 };
 
@@ -305,10 +305,20 @@ __global__ __launch_bounds__(256, kv8_waves(DH, R)) void k_kv8_attend(const unsi
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // workgroup -> ((split, row tile), (sequence, head)): those of one (sequence, head) lie a multiple of n_seq * heads apart, on one XCD where that is
   // a multiple of 8, so that row tiles read the keys from one L2
-  const int pairs = a.rows.n_seq * dm.heads;
-  const int pair = blockIdx.x % pairs, rest = blockIdx.x / pairs;
-  const int tile = rest % a.row_tiles, split = rest / a.row_tiles;
-  const int b = pair / dm.heads, h = pair % dm.heads;
+  int b, h, tile, split;
+  if (a.tiles.packed) {
+    const int rest = blockIdx.x / dm.heads;
+    h = blockIdx.x % dm.heads;
+    tile = rest % (int)a.tiles.pieces; split = rest / (int)a.tiles.pieces;
+    b = kv8_owner(a.rows, a.tiles, tile);
+    if (b < 0) return;
+    tile -= kv8_first(a.rows, a.tiles, b);
+    if (tile < 0) return;
+  } else {
+    const int pairs = a.rows.n_seq * dm.heads, pair = blockIdx.x % pairs, rest = blockIdx.x / pairs;
+    tile = rest % (int)a.tiles.pieces; split = rest / (int)a.tiles.pieces;
+    b = pair / dm.heads; h = pair % dm.heads;
+  }
   const Kv8Seq sq = kv8_seq(a.rows, b, dm.capacity, !CLOSED);
   const int m_rows = sq.n * a.group, row0 = tile * 16 * R;
   if (row0 >= m_rows) return;
@@ -338,11 +348,12 @@ template <int DH>
 __global__ __launch_bounds__(256) void k_kv8_join(Kv8Attend a, Kv8Dims dm) {
   constexpr int kLanes = DH / 4, kAtOnce = 64 / kLanes;
   const int lane = threadIdx.x & 63, part = lane / kLanes, col = 4 * (lane % kLanes);
-  const int b = blockIdx.y, heads = dm.heads * a.group;
+  const int heads = dm.heads * a.group, m = blockIdx.x * 4 + (threadIdx.x >> 6), hq = m % heads;
+  const int b = a.one.packed ? kv8_owner(a.rows, a.one, m / heads) : blockIdx.y;
+  if (b < 0) return;
   const Kv8Seq sq = kv8_seq(a.rows, b, dm.capacity, !dm.closed);
-  const int m = blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (m >= sq.n * heads) return;
-  const int i = m / heads, hq = m % heads;
+  const int i = m / heads - (a.one.packed ? kv8_first(a.rows, a.one, b) : 0);
+  if (i < 0 || i >= sq.n) return;
   // a tile's splits are written up to its last row's block; a row's own end is enough, what lies behind holds nothing of it
   const int end = dm.closed ? (sq.base + kKv8Block - 1) / kKv8Block : (sq.base + i) / kKv8Block + 1;
   const int n = min(max(1, (end + a.split_blocks - 1) / a.split_blocks), a.n_split);
@@ -411,28 +422,31 @@ size_t kv8_attend_bytes(const Kv8Dims& d, int q_heads, int rows, int max_keys) {
   const size_t n = splits_of(d, max_keys);
   return n == 1 ? 0 : ((size_t)rows * q_heads * n * 2 * 4 + 255) / 256 * 256 + (size_t)rows * q_heads * n * d.width * 4;
 }
+// 16 or 32 rows of a wave.  (64, two waves a SIMD instead of three: 512 rows over 32 keys 11.3 us, with 32 7.3; over 1024 21.1 and 17.6, over 8192 47.3 and
+// 45.3: a row tile more reads its keys from L2, and the third wave fills the other two's waits.)
+static bool one_tile(const Kv8Rows& r, int group) { return (size_t)r.max_rows * group <= 16; }
+static Kv8Deal tiles_of(const Kv8Rows& r, int group) {
+  const int shift = one_tile(r, group) ? 4 : 5;
+  return kv8_deal(r, group, shift, 1, (((size_t)r.max_rows * group - 1) >> shift) + 1);
+}
+static size_t of_all(const Kv8Deal& d, const Kv8Rows& r) { return d.packed ? d.pieces : d.pieces * r.n_seq; }
 // a launch takes less than 2^32 lanes along x: 2^24 workgroups of 256
-bool kv8_attend_fits(const Kv8Dims& d, int q_heads, int max_rows, int max_keys) {
-  const size_t tiles = ((size_t)max_rows * (q_heads / d.heads) + 15) / 16;
-  return tiles * d.n_seq * d.heads * splits_of(d, max_keys) < (1u << 24) && (size_t)max_rows * q_heads < (1u << 26);
+bool kv8_attend_fits(const Kv8Dims& d, const Kv8Rows& r, int q_heads, int max_keys) {
+  return of_all(tiles_of(r, q_heads / d.heads), r) * d.heads * splits_of(d, max_keys) < (1u << 24) && kv8_deal(r, 1, 0, 0, r.max_rows).pieces * q_heads < (1u << 26);
 }
 
 template <int DH, int FMT>
 static void attend_for(const Kv8Dims& d, const unsigned char* cache, Kv8Attend& a, hipStream_t s) {
-  const int m = a.rows.max_rows * a.group;
   auto go = [&](auto r, auto closed) {
-    a.row_tiles = (m + 16 * r.value - 1) / (16 * r.value);
-    k_kv8_attend<DH, r.value, FMT, closed.value><<<(unsigned)((size_t)a.rows.n_seq * d.heads * a.row_tiles * a.n_split), 256, 0, s>>>(cache, a, d);
+    k_kv8_attend<DH, r.value, FMT, closed.value><<<(unsigned)(of_all(a.tiles, a.rows) * d.heads * a.n_split), 256, 0, s>>>(cache, a, d);
   };
   auto by_rows = [&](auto closed) {
-    // 16 or 32 rows of a wave.  (64, two waves a SIMD instead of three: 512 rows over 32 keys 11.3 us, with 32 7.3; over 1024 21.1 and 17.6, over 8192 47.3 and
-    // 45.3: a row tile more reads its keys from L2, and the third wave fills the other two's waits.)
-    if (m <= 16) go(std::integral_constant<int, 1>{}, closed);
+    if (one_tile(a.rows, a.group)) go(std::integral_constant<int, 1>{}, closed);
     else go(std::integral_constant<int, 2>{}, closed);
   };
   if (d.closed) by_rows(std::true_type{});
   else by_rows(std::false_type{});
-  if (a.n_split > 1) k_kv8_join<DH><<<dim3((a.rows.max_rows * d.heads * a.group + 3) / 4, a.rows.n_seq), 256, 0, s>>>(a, d);
+  if (a.n_split > 1) k_kv8_join<DH><<<dim3((unsigned)((a.one.pieces * d.heads * a.group + 3) / 4), a.one.packed ? 1 : a.rows.n_seq), 256, 0, s>>>(a, d);
 }
 void launch_kv8_attend(const Kv8Dims& d, const void* cache, const void* q, size_t q_stride, void* out, size_t out_stride, int q_heads,
                        const Kv8Rows& r, int max_keys, float scale, void* ws, hipStream_t s) {
@@ -441,7 +455,8 @@ void launch_kv8_attend(const Kv8Dims& d, const void* cache, const void* q, size_
   a.rows = r; a.group = q_heads / d.heads; a.scale = scale * kLog2e;
   a.split_blocks = kv8_split_keys(d) / kKv8Block;
   a.n_split = splits_of(d, max_keys);
-  a.row_tiles = 1;
+  a.tiles = tiles_of(r, a.group);
+  a.one = kv8_deal(r, 1, 0, 0, r.max_rows);
   a.part_ml = (float*)ws;
   a.part_o = (float*)((char*)ws + ((size_t)r.rows * q_heads * a.n_split * 2 * 4 + 255) / 256 * 256);
   kv8_dispatch(d, [&](auto width, auto fmt) { attend_for<width.value, fmt.value>(d, (const unsigned char*)cache, a, s); });

@@ -22,6 +22,20 @@ __device__ __forceinline__ Kv8Seq kv8_seq(const Kv8Rows& t, int b, int capacity,
   return s;
 }
 
+// where the packed pieces of sequence b begin, and the sequence that has packed piece `at` (-1: none), found by each wave for itself: every 64th sequence at once, then
+// those between two of them
+__device__ __forceinline__ int kv8_first(const Kv8Rows& t, const Kv8Deal& d, int b) {
+  return (int)((long long)min(max(t.start[(size_t)b * t.stride], 0), t.rows) * d.mul >> d.shift) + d.extra * b;
+}
+__device__ __forceinline__ int kv8_owner(const Kv8Rows& t, const Kv8Deal& d, int at) {
+  const int lane = threadIdx.x & 63, apart = (t.n_seq + 63) / 64;
+  int b = __popcll(__ballot(lane * apart < t.n_seq && kv8_first(t, d, min(lane * apart, t.n_seq - 1)) <= at)) - 1;
+  if (b < 0) return -1;
+  b *= apart;
+  if (apart > 1) b += __popcll(__ballot(lane < apart && b + lane < t.n_seq && kv8_first(t, d, min(b + lane, t.n_seq - 1)) <= at)) - 1;
+  return b;
+}
+
 // the key that element j of lane group g holds in the values' operand
 __device__ __forceinline__ constexpr int kv8_key(int g, int j) { return j < 4 ? 4 * g + j : 16 + 4 * g + j - 4; }
 

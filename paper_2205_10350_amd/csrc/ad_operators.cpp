@@ -100,9 +100,9 @@ int ad_kv8_attend(const ad_kv8_config* c, const void* cache, const void* q, int6
   const size_t need = kv8_attend_bytes(d, q_heads, rows, max_keys);
   if (need && (!workspace || ((uintptr_t)workspace & 255))) return refuse("ad_kv8_attend: the workspace must be 256-byte aligned device memory");
   if (workspace_bytes < need) { set_global_error("ad_kv8_attend: workspace smaller than ad_kv8_attend_bytes()"); return AD_ENOMEM; }
-  if (!kv8_attend_fits(d, q_heads, max_rows, max_keys)) return refuse("ad_kv8_attend: more workgroups than a launch takes (sequences x heads x rows x keys)");
-  launch_kv8_attend(d, cache, q, (size_t)q_stride, out, (size_t)out_stride, q_heads, Kv8Rows{row_start, nullptr, length, 1, rows, max_rows, c->n_seq},
-                    max_keys, scale, workspace, (hipStream_t)hip_stream);
+  const Kv8Rows r{row_start, nullptr, length, 1, rows, max_rows, c->n_seq};
+  if (!kv8_attend_fits(d, r, q_heads, max_keys)) return refuse("ad_kv8_attend: more workgroups than a launch takes (sequences x heads x rows x keys)");
+  launch_kv8_attend(d, cache, q, (size_t)q_stride, out, (size_t)out_stride, q_heads, r, max_keys, scale, workspace, (hipStream_t)hip_stream);
   return launched("ad_kv8_attend");
 }
 

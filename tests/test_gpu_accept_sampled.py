@@ -113,6 +113,29 @@ def test_temperatures_near_zero_and_very_high(rows, vocab, probs):
         assert abs(tok[at] - float(p["v"][b]) * vocab) <= 1
 
 
+@pytest.mark.parametrize("n_seq", [40, 65, 700])
+@pytest.mark.parametrize("probs", [False, True])
+def test_many_sequences_with_and_without_a_bound(n_seq, probs):
+    """Rows looked up in the table (no bound: mostly rows that are not there) and by sequence; empty sequences among, before and behind the others."""
+    rng = np.random.default_rng(n_seq)
+    rows = [0, 0] + [int(r) for r in rng.integers(0, 4, n_seq - 4)] + [0, 0]
+    p = problem(n_seq, rows, 50, probs)
+    got = run(p, rows)
+    check(p, rows, got)
+    assert got == run(p, rows, max_rows=3)
+
+
+def test_a_table_that_does_not_fit_stays_inside_its_buffers():
+    rows = [3] * 70
+    p = problem(70, rows, 40, False)
+    n = sum(rows)
+    start = i32(np.random.default_rng(0).integers(-5, n + 5, 71))
+    for most in (n, 3):
+        _, tok = ad.accept_sampled(p["x"].cuda(), i32(p["d"]), start, f32(p["u"]), f32(p["v"]), max_rows=most)
+        torch.cuda.synchronize()
+        assert tok.shape == (n,)
+
+
 @pytest.mark.parametrize("skew", range(8))
 @pytest.mark.parametrize("bf16", [False, True])
 def test_rows_at_every_alignment(skew, bf16):

@@ -281,6 +281,41 @@ def test_captured_and_replayed():
         assert torch.equal(out, eager.attend(rows[2], start, i32([i, i]), max_rows=3)), i
 
 
+@pytest.mark.parametrize("closed", [False, True])
+@pytest.mark.parametrize("n_seq,heads,q_heads", [(40, 1, 1), (150, 2, 6)])
+def test_many_sequences_with_and_without_a_bound(n_seq, heads, q_heads, closed):
+    """Blocks, tiles and rows looked up in the table (no bound: mostly ones that are not there) and by sequence, splits and empty sequences among them."""
+    w, cap = 32, 1400
+    rng = np.random.default_rng(n_seq)
+    lens = [0] + [int(x) for x in rng.integers(1, 90, n_seq - 2)] + [1200]
+    lens[7] = 0
+    k, v = draw(40, n_seq, cap, heads, w), draw(41, n_seq, cap, heads, w)
+    wide, tight = (ad.Kv8Cache(n_seq, heads, w, capacity=cap, k_max=cap, closed=closed) for _ in range(2))
+    at = i32([0] * n_seq)
+    kk, vv = packed(k, [0] * n_seq, lens), packed(v, [0] * n_seq, lens)
+    wide.append(kk, vv, starts(lens), at)
+    for b in range(n_seq):                                                # one sequence a call
+        one = [lens[b] if i == b else 0 for i in range(n_seq)]
+        lo = sum(lens[:b])
+        if lens[b]:
+            tight.append(kk[lo:lo + lens[b]], vv[lo:lo + lens[b]], starts(one), at, max_rows=lens[b])
+    for got, want in zip(read_all(wide, lens), read_all(tight, lens)):
+        assert torch.equal(got, want)
+    some = wide.read(starts(lens), at, i32(lens), rows=sum(lens), max_rows=max(lens), dtype=torch.float32)
+    assert all(torch.equal(a, b) for a, b in zip(some, read_all(wide, lens)))
+    rows = [min(n, int(x)) for n, x in zip(lens, rng.integers(0, 40, n_seq))]
+    before = lens if closed else [n - r for n, r in zip(lens, rows)]
+    q = draw(42, sum(rows), q_heads, w).cuda()
+    got = wide.attend(q, starts(rows), i32(before))
+    assert torch.equal(got, tight.attend(q, starts(rows), i32(before), max_rows=max(rows)))
+    lo = 0
+    for b in range(n_seq):                                                # and each sequence by itself
+        if rows[b] and b % 9 == 0 or b == n_seq - 1:
+            one = [rows[b] if i == b else 0 for i in range(n_seq)]
+            assert torch.equal(got[lo:lo + rows[b]], tight.attend(q[lo:lo + rows[b]].contiguous(), starts(one), i32(before), max_rows=max(rows[b], 1)) if rows[b] else got[lo:lo])
+        lo += rows[b]
+
+
 def test_on_another_stream():
     heads, w, n = 2, 64, 400
     k, v, q = draw(30, 1, n, heads, w), draw(31, 1, n, heads, w), draw(32, 5, heads, w).cuda()
