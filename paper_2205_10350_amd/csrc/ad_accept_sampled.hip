@@ -169,23 +169,29 @@ __device__ __forceinline__ AcceptSeq accept_seq(const AcceptArgs& a, int b) {
   if (s.row0 < 0 || s.row0 > a.rows) s.n = 0;
   return s;
 }
-// The packed row that a workgroup or wave works on and its sequence; b = -1: none.
-// By sequence: row i of sequence b.  By packed row `at` (PACKED): the last sequence that starts there or before (of several, those before it are empty), found by each
-// wave for itself: every 64th start at once, then those between two of them.
-struct AcceptAt { int b, row; };
-template <bool PACKED> __device__ __forceinline__ AcceptAt accept_at(const AcceptArgs& a, int b, int i) {
-  if constexpr (!PACKED) {
-    const AcceptSeq sq = accept_seq(a, b);
-    return AcceptAt{i < sq.n ? b : -1, sq.row0 + i};
-  }
-  const int lane = threadIdx.x & 63, apart = (a.n_seq + 63) / 64, at = b * kRowsY + i;
-  int q = __popcll(__ballot(lane * apart < a.n_seq && a.row_start[min(lane * apart, a.n_seq - 1)] <= at)) - 1;
-  if (q < 0 || at >= a.rows) return AcceptAt{-1, 0};
+// The sequence of packed row `row` (-1: none, or the row is one too many of it): the last one that starts there or before (of several, those before it are empty), found by
+// each wave for itself: every 64th start at once, then those between two of them.
+__device__ __forceinline__ int accept_owner(const AcceptArgs& a, int row) {
+  const int lane = threadIdx.x & 63, apart = (a.n_seq + 63) / 64;
+  int q = __popcll(__ballot(lane * apart < a.n_seq && a.row_start[min(lane * apart, a.n_seq - 1)] <= row)) - 1;
+  if (q < 0 || row >= a.rows) return -1;
   q *= apart;
-  if (apart > 1) q += __popcll(__ballot(lane < apart && q + lane < a.n_seq && a.row_start[min(q + lane, a.n_seq - 1)] <= at)) - 1;
-  if (q < 0) return AcceptAt{-1, 0};   // (starts that do not ascend)
+  if (apart > 1) q += __popcll(__ballot(lane < apart && q + lane < a.n_seq && a.row_start[min(q + lane, a.n_seq - 1)] <= row)) - 1;
+  if (q < 0) return -1;   // (starts that do not ascend)
   const AcceptSeq sq = accept_seq(a, q);
-  return AcceptAt{at >= sq.row0 && at - sq.row0 < sq.n ? q : -1, at};
+  return row >= sq.row0 && row - sq.row0 < sq.n ? q : -1;
+}
+// Row i of sequence b, or (PACKED) packed row b kRowsY + i and its sequence, to `b` and `row`; whether there is such a row.
+template <bool PACKED> __device__ __forceinline__ bool accept_find(const AcceptArgs& a, int i, int& b, int& row) {
+  if constexpr (PACKED) {
+    row = b * kRowsY + i;
+    b = accept_owner(a, row);
+    return b >= 0;
+  } else {
+    const AcceptSeq sq = accept_seq(a, b);
+    row = sq.row0 + i;
+    return i < sq.n;
+  }
 }
 // log2(e) / T; NaN where T is no positive number
 __device__ __forceinline__ double accept_rate(const AcceptArgs& a, int b) {
@@ -199,9 +205,8 @@ __global__ __launch_bounds__(kAcceptThreads) void k_accept_stats(AcceptArgs a) {
   __shared__ float ms[kAcceptThreads / 64];
   __shared__ double ss[kAcceptThreads / 64];
   const int c = blockIdx.x, t = threadIdx.x;
-  const AcceptAt at = accept_at<PACKED>(a, blockIdx.z, blockIdx.y);
-  if (at.b < 0) return;
-  const int b = at.b, row = at.row;
+  int b = blockIdx.z, row;
+  if (!accept_find<PACKED>(a, blockIdx.y, b, row)) return;
   const AcceptRow<T> x(a, row);
   float v[kEach<T>];
   x.load(c, t, v);
@@ -304,10 +309,10 @@ template <typename T> __device__ __forceinline__ int accept_first(const AcceptAr
 // The test of all rows at once, a wave a row
 template <typename T, bool PACKED>
 __global__ __launch_bounds__(kAcceptThreads) void k_accept_rows(AcceptArgs a) {
-  const AcceptAt at = accept_at<PACKED>(a, blockIdx.y, blockIdx.x * (kAcceptThreads / 64) + (threadIdx.x >> 6));
-  if (at.b < 0) return;
-  const AcceptRowInfo r = accept_decide<T>(a, at.row, accept_rate(a, at.b));
-  if ((threadIdx.x & 63) == 0) a.row_info[at.row] = r;
+  int b = blockIdx.y, row;
+  if (!accept_find<PACKED>(a, blockIdx.x * (kAcceptThreads / 64) + (threadIdx.x >> 6), b, row)) return;
+  const AcceptRowInfo r = accept_decide<T>(a, row, accept_rate(a, b));
+  if ((threadIdx.x & 63) == 0) a.row_info[row] = r;
 }
 // The first row whose token does not stand, with its maximum and sum, from there, by each wave for itself
 struct AcceptFirst { int i; float m; double z; };
