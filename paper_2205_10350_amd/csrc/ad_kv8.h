@@ -13,6 +13,10 @@
 //   values: chunk c (of head width / 16), lane slot l, element j: column 16 c + l % 16 of key kv8_key(l / 16, j)
 #pragma once
 
+#include <limits.h>
+
+#include <algorithm>
+
 #include "ad_internal.h"
 
 namespace ad {
@@ -51,11 +55,11 @@ struct Kv8Rows {
 // How a launch deals out a sequence's pieces of 2^shift / mul rows: as many to every sequence as max_rows have, or, where most of those would not be there, packed:
 // sequence b's begin at (start[b] mul >> shift) + extra b, and each workgroup looks its sequence up.  (256 sequences of 25 rows over closed caches of 400 tokens, us without a bound:
 // by sequence 653, packed 57, with max_rows = 25 and by sequence 50.)
-struct Kv8Deal { int packed, mul, shift, extra; size_t pieces; };   // pieces: of a sequence; packed: of all
+struct Kv8Deal { int packed, pieces, mul, shift, extra; };   // pieces: of a sequence; packed: of all
 inline Kv8Deal kv8_deal(const Kv8Rows& r, int mul, int shift, int extra, size_t of_one) {
   const size_t all = ((size_t)r.rows * mul >> shift) + (size_t)extra * r.n_seq;
   const bool packed = of_one * r.n_seq > 4 * all && all < ((size_t)1 << 23);
-  return Kv8Deal{packed, mul, shift, extra, packed ? all : of_one};
+  return Kv8Deal{packed, (int)std::min(packed ? all : of_one, (size_t)INT_MAX), mul, shift, extra};
 }
 
 // Keys and values of the rows (bf16, [rows, heads, width] with row strides in elements) behind base[b] tokens.

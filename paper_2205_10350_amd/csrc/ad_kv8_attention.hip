@@ -36,7 +36,7 @@ struct Kv8Attend {
   Kv8Rows rows;
   int group;                 // query heads that share a head
   int split_blocks, n_split; // blocks of a split; splits launched
-  Kv8Deal tiles, one;        // how tiles of 16 R rows, and single rows, are dealt out
+  Kv8Deal tiles;             // how tiles of 16 R rows are dealt out
   float scale;               // of the scores, times log2(e)
 };
 
@@ -309,14 +309,14 @@ __global__ __launch_bounds__(256, kv8_waves(DH, R)) void k_kv8_attend(const unsi
   if (a.tiles.packed) {
     const int rest = blockIdx.x / dm.heads;
     h = blockIdx.x % dm.heads;
-    tile = rest % (int)a.tiles.pieces; split = rest / (int)a.tiles.pieces;
+    tile = rest % a.tiles.pieces; split = rest / a.tiles.pieces;
     b = kv8_owner(a.rows, a.tiles, tile);
     if (b < 0) return;
     tile -= kv8_first(a.rows, a.tiles, b);
     if (tile < 0) return;
   } else {
     const int pairs = a.rows.n_seq * dm.heads, pair = blockIdx.x % pairs, rest = blockIdx.x / pairs;
-    tile = rest % (int)a.tiles.pieces; split = rest / (int)a.tiles.pieces;
+    tile = rest % a.tiles.pieces; split = rest / a.tiles.pieces;
     b = pair / dm.heads; h = pair % dm.heads;
   }
   const Kv8Seq sq = kv8_seq(a.rows, b, dm.capacity, !CLOSED);
@@ -345,14 +345,14 @@ __global__ __launch_bounds__(256, kv8_waves(DH, R)) void k_kv8_attend(const unsi
 
 // The splits of a (row, query head): one wave, DH / 4 lanes a group of kGroup and 256 / DH groups at once; joined group by group, a group's in their order.
 template <int DH>
-__global__ __launch_bounds__(256) void k_kv8_join(Kv8Attend a, Kv8Dims dm) {
+__global__ __launch_bounds__(256) void k_kv8_join(Kv8Attend a, Kv8Deal one, Kv8Dims dm) {
   constexpr int kLanes = DH / 4, kAtOnce = 64 / kLanes;
   const int lane = threadIdx.x & 63, part = lane / kLanes, col = 4 * (lane % kLanes);
   const int heads = dm.heads * a.group, m = blockIdx.x * 4 + (threadIdx.x >> 6), hq = m % heads;
-  const int b = a.one.packed ? kv8_owner(a.rows, a.one, m / heads) : blockIdx.y;
+  const int b = one.packed ? kv8_owner(a.rows, one, m / heads) : blockIdx.y;
   if (b < 0) return;
   const Kv8Seq sq = kv8_seq(a.rows, b, dm.capacity, !dm.closed);
-  const int i = m / heads - (a.one.packed ? kv8_first(a.rows, a.one, b) : 0);
+  const int i = m / heads - (one.packed ? kv8_first(a.rows, one, b) : 0);
   if (i < 0 || i >= sq.n) return;
   // a tile's splits are written up to its last row's block; a row's own end is enough, what lies behind holds nothing of it
   const int end = dm.closed ? (sq.base + kKv8Block - 1) / kKv8Block : (sq.base + i) / kKv8Block + 1;
@@ -429,10 +429,10 @@ static Kv8Deal tiles_of(const Kv8Rows& r, int group) {
   const int shift = one_tile(r, group) ? 4 : 5;
   return kv8_deal(r, group, shift, 1, (((size_t)r.max_rows * group - 1) >> shift) + 1);
 }
-static size_t of_all(const Kv8Deal& d, const Kv8Rows& r) { return d.packed ? d.pieces : d.pieces * r.n_seq; }
+static size_t of_all(const Kv8Deal& d, const Kv8Rows& r) { return d.packed ? d.pieces : (size_t)d.pieces * r.n_seq; }
 // a launch takes less than 2^32 lanes along x: 2^24 workgroups of 256
 bool kv8_attend_fits(const Kv8Dims& d, const Kv8Rows& r, int q_heads, int max_keys) {
-  return of_all(tiles_of(r, q_heads / d.heads), r) * d.heads * splits_of(d, max_keys) < (1u << 24) && kv8_deal(r, 1, 0, 0, r.max_rows).pieces * q_heads < (1u << 26);
+  return of_all(tiles_of(r, q_heads / d.heads), r) * d.heads * splits_of(d, max_keys) < (1u << 24) && (size_t)kv8_deal(r, 1, 0, 0, r.max_rows).pieces * q_heads < (1u << 26);
 }
 
 template <int DH, int FMT>
@@ -446,7 +446,10 @@ static void attend_for(const Kv8Dims& d, const unsigned char* cache, Kv8Attend& 
   };
   if (d.closed) by_rows(std::true_type{});
   else by_rows(std::false_type{});
-  if (a.n_split > 1) k_kv8_join<DH><<<dim3((unsigned)((a.one.pieces * d.heads * a.group + 3) / 4), a.one.packed ? 1 : a.rows.n_seq), 256, 0, s>>>(a, d);
+  if (a.n_split > 1) {
+    const Kv8Deal one = kv8_deal(a.rows, 1, 0, 0, a.rows.max_rows);
+    k_kv8_join<DH><<<dim3((unsigned)(((size_t)one.pieces * d.heads * a.group + 3) / 4), one.packed ? 1 : a.rows.n_seq), 256, 0, s>>>(a, one, d);
+  }
 }
 void launch_kv8_attend(const Kv8Dims& d, const void* cache, const void* q, size_t q_stride, void* out, size_t out_stride, int q_heads,
                        const Kv8Rows& r, int max_keys, float scale, void* ws, hipStream_t s) {
@@ -456,7 +459,6 @@ void launch_kv8_attend(const Kv8Dims& d, const void* cache, const void* q, size_
   a.split_blocks = kv8_split_keys(d) / kKv8Block;
   a.n_split = splits_of(d, max_keys);
   a.tiles = tiles_of(r, a.group);
-  a.one = kv8_deal(r, 1, 0, 0, r.max_rows);
   a.part_ml = (float*)ws;
   a.part_o = (float*)((char*)ws + ((size_t)r.rows * q_heads * a.n_split * 2 * 4 + 255) / 256 * 256);
   kv8_dispatch(d, [&](auto width, auto fmt) { attend_for<width.value, fmt.value>(d, (const unsigned char*)cache, a, s); });
