@@ -5,7 +5,8 @@
 // probabilities: p without d; no token drafted: p), and the token is the least t with r(0) + .. + r(t) > v (r(0) + .. + r(V - 1)).
 // Tokens so accepted are distributed as p.
 //
-// A drawn number may lie next to the border between two tokens, so sums over the vocabulary and what goes into them have 64 bits:
+// A drawn number may lie next to the border between two tokens, so sums over the vocabulary and what goes into them have 64 bits, and the tokens of a row are the same
+// to the bit in every call that it may be part of (where a call is large a row's test is tried in 32 bits first: kNear):
 //   k_accept_stats   a workgroup per 8 KB of scores of a row: their maximum, and sum of exp2((x - max) log2(e) / T) (without d where q is none).  It reads everything
 //                    once and is bound by that; 64-bit exponentials cost 20 instructions a score.
 //   k_accept_rows    (q given, or many or large rows) a wave per row: its test
@@ -73,6 +74,10 @@ __device__ __forceinline__ double exp2_bulk(float x, double rate, double m) {
   const unsigned hi = (unsigned)(bits >> 32) + ((unsigned)__builtin_bit_cast(long long, big) << 20);
   return __builtin_bit_cast(double, (long long)((unsigned long long)hi << 32 | (unsigned)bits));
 }
+// Sums in 32 bits, what a row's test may be tried with: z off by less than 2^-15.9 of itself.  A weight 2^t, |t| <= 126, has three roundings in t (difference, rate,
+// product), 3 * 2^-24 |t|, that is ln(2) * 378 * 2^-24 = 262 * 2^-24 of the weight, the exponential's own 2 * 2^-24, and at most 7 * 2^-24 by additions; what is smaller
+// is 2^-125 at most, of which 2^24 are nothing beside z >= 1.  Within this part of u z, u < p is looked at again with the sums in 64 bits.
+constexpr double kNear = 0x1p-15;
 // and to f^11, nothing below 2^-1000, for the rows that are drawn from
 __device__ __forceinline__ double exp2_weight(float x, double rate, double m) {
   const double u = ((double)x - m) * rate, t = fmax(u, -1020.0);
@@ -161,6 +166,30 @@ template <typename T> __device__ __forceinline__ bool accept_drop(const AcceptRo
   return nan;
 }
 
+// Weights of what thread t holds of piece c, whose largest score is m, in 64 bits and without score `skip`; NaN where one of the scores is
+template <typename T> __device__ __forceinline__ double accept_wide(const AcceptRow<T>& x, int c, int t, int skip, float (&v)[kEach<T>], float head, double rate, float m) {
+  bool nan = accept_drop(x, c, t, skip, v) || head != head;
+  double s = 0.0;
+#pragma unroll
+  for (int j = 0; j < kEach<T>; ++j) {
+    nan = nan || v[j] != v[j];
+    s += exp2_bulk(v[j], rate, (double)m);
+  }
+  if (t < x.heads(c) && t != skip) s += exp2_bulk(head, rate, (double)m);
+  return nan ? (double)NAN : s;
+}
+// A piece's sum as it is kept, of its four waves'
+__device__ __forceinline__ double accept_piece(double s0, double s1, double s2, double s3) {
+  const double sum = (s0 + s1) + (s2 + s3);
+  return sum < kNothing ? 0.0 : sum;
+}
+// What a piece of largest score mc and sum s weighs beside a row's maximum m (s is 0 where mc is -inf, or NaN).  (No product is fused into a sum, here or where it is added up:
+// the same roundings in every kernel.)
+__device__ __forceinline__ double accept_share(float mc, double s, float m, double rate) {
+#pragma clang fp contract(off)
+  return mc > -INFINITY ? s * exp2_down(((double)mc - (double)m) * rate) : s;
+}
+
 struct AcceptSeq { int row0, n; };
 __device__ __forceinline__ AcceptSeq accept_seq(const AcceptArgs& a, int b) {
   AcceptSeq s;
@@ -223,17 +252,12 @@ __global__ __launch_bounds__(kAcceptThreads) void k_accept_stats(AcceptArgs a) {
   double s = 0.0;
   bool nan = head != head || !(m < INFINITY) || rate != rate;   // (no distribution)
   if (m > -INFINITY) {
-    const bool here = t < x.heads(c) && t != skip;
-    nan = accept_drop(x, c, t, skip, v) || nan;
     if constexpr (WIDE) {
-#pragma unroll
-      for (int j = 0; j < kEach<T>; ++j) {
-        nan = nan || v[j] != v[j];
-        s += exp2_bulk(v[j], rate, (double)m);
-      }
-      if (here) s += exp2_bulk(head, rate, (double)m);
+      s = accept_wide(x, c, t, skip, v, head, rate, m);
     } else {
-      // (a row's test alone rests on these sums: 2^-24 of a probability is where a drawn number of 24 bits may fall either way)
+      // (a row's first test alone rests on these sums)
+      const bool here = t < x.heads(c) && t != skip;
+      nan = accept_drop(x, c, t, skip, v) || nan;
       const float r = fminf((float)rate, 0x1.fffffep127f);   // (of a temperature below 2^-127 no infinity, which times a difference of 0 would be NaN)
       float e[4] = {here ? __builtin_amdgcn_exp2f((head - m) * r) : 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -249,8 +273,7 @@ __global__ __launch_bounds__(kAcceptThreads) void k_accept_stats(AcceptArgs a) {
   if ((t & 63) == 0) ss[t >> 6] = s;
   __syncthreads();
   if (t == 0) {
-    const double sum = (ss[0] + ss[1]) + (ss[2] + ss[3]);
-    a.piece_sum[(size_t)row * a.pieces + c] = sum < kNothing ? 0.0 : sum;
+    a.piece_sum[(size_t)row * a.pieces + c] = accept_piece(ss[0], ss[1], ss[2], ss[3]);
     a.piece_max[(size_t)row * a.pieces + c] = m;
   }
 }
@@ -258,6 +281,7 @@ __global__ __launch_bounds__(kAcceptThreads) void k_accept_stats(AcceptArgs a) {
 // A row's maximum and the sum over its vocabulary relative to it (without the drafted token: wd), by one wave
 struct AcceptSums { float m; double z, wd; };
 template <typename T> __device__ __forceinline__ AcceptSums accept_sums(const AcceptArgs& a, int row, double rate) {
+#pragma clang fp contract(off)
   const int lane = threadIdx.x & 63;
   const float* pm = a.piece_max + (size_t)row * a.pieces;
   const double* ps = a.piece_sum + (size_t)row * a.pieces;
@@ -270,9 +294,8 @@ template <typename T> __device__ __forceinline__ AcceptSums accept_sums(const Ac
   r.m = m0;
   for (int c = lane + 64; c < a.pieces; c += 64) r.m = fmaxf(r.m, pm[c]);
   r.m = wave_max(r.m);
-  auto part = [&](float mc, double s) { return mc > -INFINITY ? s * exp2_down(((double)mc - (double)r.m) * rate) : s; };   // (s is 0 there, or NaN)
-  double z = part(m0, s0);
-  for (int c = lane + 64; c < a.pieces; c += 64) z += part(pm[c], ps[c]);
+  double z = accept_share(m0, s0, r.m, rate);
+  for (int c = lane + 64; c < a.pieces; c += 64) z += accept_share(pm[c], ps[c], r.m, rate);
   r.z = wave_sum_f64(z);
   r.wd = accept_drafted(a, d) ? exp2_down(((double)xd - (double)r.m) * rate) : 0.0;
   if (!a.probs) r.z += r.wd;
@@ -280,11 +303,37 @@ template <typename T> __device__ __forceinline__ AcceptSums accept_sums(const Ac
 }
 __device__ __forceinline__ bool accept_broken(double z) { return !(z > 0.0 && z < (double)INFINITY); }
 
-// A row's test, by one wave
-template <typename T> __device__ __forceinline__ AcceptRowInfo accept_decide(const AcceptArgs& a, int row, double rate) {
+// A row's sums over its pieces in 64 bits in place of those in 32, by one wave: the same sums in the same order as four waves', left where this lane will look for them
+template <typename T> __device__ __forceinline__ void accept_widen(const AcceptArgs& a, int row, double rate) {
+  const int lane = threadIdx.x & 63, skip = a.draft[row];
+  const AcceptRow<T> x(a, row);
+  for (int c = 0; c < a.pieces; ++c) {
+    const float m = a.piece_max[(size_t)row * a.pieces + c];
+    if (!(m > -INFINITY)) continue;
+    double s[4];
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const int t = 64 * w + lane;
+      float v[kEach<T>];
+      x.load(c, t, v);
+      s[w] = wave_sum_f64(accept_wide(x, c, t, skip, v, t < x.heads(c) ? x.at(t) : -INFINITY, rate, m));
+    }
+    if (lane == c % 64) a.piece_sum[(size_t)row * a.pieces + c] = accept_piece(s[0], s[1], s[2], s[3]);
+  }
+}
+// A row's test, by one wave.  NARROW: its sums have 32 bits.  Their error is bounded (kNear) while scores and 1 / T are far from the ends of fp32.
+template <typename T, bool NARROW> __device__ __forceinline__ AcceptRowInfo accept_decide(const AcceptArgs& a, int row, double rate) {
   const int d = a.draft[row];
   const float u = a.accept_u[row], q = !a.probs ? 1.f : accept_drafted(a, d) ? a.probs[(size_t)row * a.probs_stride + d] : 0.f;
-  const AcceptSums r = accept_sums<T>(a, row, rate);
+  AcceptSums r = accept_sums<T>(a, row, rate);
+  if constexpr (NARROW) {
+    const double uz = (double)u * r.z;
+    const bool bounded = rate >= 0x1p-100 && rate <= 0x1p100 && r.m <= 0x1p100f;
+    if (accept_drafted(a, d) && rate == rate && (!bounded || (uz > 0.0 && fabs(uz - r.wd) <= kNear * uz))) {
+      accept_widen<T>(a, row, rate);
+      r = accept_sums<T>(a, row, rate);
+    }
+  }
   return AcceptRowInfo{r.z, r.m, accept_drafted(a, d) && !accept_broken(r.z) && (double)u * (double)q < r.wd / r.z};
 }
 // The first row whose drafted token does not stand (n: all do), by the whole workgroup
@@ -295,7 +344,7 @@ template <typename T> __device__ __forceinline__ int accept_first(const AcceptAr
   for (int i0 = 0; i0 < sq.n; i0 += kDecideThreads / 64) {
     const int i = i0 + wave;
     if (i < sq.n) {
-      const bool stands = accept_decide<T>(a, sq.row0 + i, rate).stands;
+      const bool stands = accept_decide<T, false>(a, sq.row0 + i, rate).stands;
       if (!stands && (threadIdx.x & 63) == 0) atomicMin(first, i);
     }
     __syncthreads();
@@ -307,11 +356,11 @@ template <typename T> __device__ __forceinline__ int accept_first(const AcceptAr
 }
 
 // The test of all rows at once, a wave a row
-template <typename T, bool PACKED>
+template <typename T, bool PACKED, bool NARROW>
 __global__ __launch_bounds__(kAcceptThreads) void k_accept_rows(AcceptArgs a) {
   int b = blockIdx.y, row;
   if (!accept_find<PACKED>(a, blockIdx.x * (kAcceptThreads / 64) + (threadIdx.x >> 6), b, row)) return;
-  const AcceptRowInfo r = accept_decide<T>(a, row, accept_rate(a, b));
+  const AcceptRowInfo r = accept_decide<T, NARROW>(a, row, accept_rate(a, b));
   if ((threadIdx.x & 63) == 0) a.row_info[row] = r;
 }
 // The first row whose token does not stand, with its maximum and sum, from there, by each wave for itself
@@ -365,21 +414,31 @@ __global__ __launch_bounds__(kAcceptThreads) void k_accept_rest(AcceptArgs a) {
   const AcceptRow<T> x(a, row);
   float v[kEach<T>];
   x.load(c, t, v);
-  const AcceptWeight<PROBS> w(a, row, f.m, f.z, rate);
-  accept_drop(x, c, t, w.skip, v);
-  {
-    double s = 0.0;
+  double s = 0.0;
+  float mc = -INFINITY;
+  if constexpr (PROBS) {
+    const AcceptWeight<PROBS> w(a, row, f.m, f.z, rate);
 #pragma unroll
     for (int j = 0; j < kEach<T>; ++j) {
       const int at = x.index(c, t, j);
       if (at < a.vocab) s += w(at, v[j]);
     }
     if (t < x.heads(c)) s += w.head(t, x.at(t));
-    s = wave_sum_f64(s);
-    if ((t & 63) == 0) ss[t >> 6] = s;
+  } else {   // (the sums that a small call has of every row)
+    mc = a.piece_max[(size_t)row * a.pieces + c];
+    if (mc > -INFINITY) s = accept_wide(x, c, t, a.draft[row], v, t < x.heads(c) ? x.at(t) : -INFINITY, rate, mc);
   }
+  s = wave_sum_f64(s);
+  if ((t & 63) == 0) ss[t >> 6] = s;
   __syncthreads();
-  if (t == 0) a.rest_sum[(size_t)b * a.pieces + c] = (ss[0] + ss[1]) + (ss[2] + ss[3]);
+  if (t == 0) {
+    double sum = (ss[0] + ss[1]) + (ss[2] + ss[3]);
+    if constexpr (!PROBS) {
+      sum = accept_share(mc, accept_piece(ss[0], ss[1], ss[2], ss[3]), f.m, rate);
+      if (sum < kNothing) sum = 0.0;
+    }
+    a.rest_sum[(size_t)b * a.pieces + c] = sum;
+  }
 }
 
 // DECIDED: k_accept_rows has been over the rows
@@ -418,8 +477,7 @@ __global__ __launch_bounds__(DECIDED ? kAcceptThreads : kDecideThreads) void k_a
       // (the drafted token is left out of the pieces' sums where the drafter gave no probabilities)
       auto piece = [&](int c) -> double {
         if constexpr (DECIDED) return c == lane ? rest0 : a.rest_sum[(size_t)b * a.pieces + c];
-        const float mc = a.piece_max[(size_t)row * a.pieces + c];
-        const double s = mc > -INFINITY ? a.piece_sum[(size_t)row * a.pieces + c] * exp2_down(((double)mc - (double)m) * rate) : 0.0;
+        const double s = accept_share(a.piece_max[(size_t)row * a.pieces + c], a.piece_sum[(size_t)row * a.pieces + c], m, rate);
         return s < kNothing ? 0.0 : s;
       };
       // the piece in which the sum passes the wanted part of the whole: every wave finds it by itself, 64 pieces at a time
@@ -568,7 +626,7 @@ size_t accept_bytes(int n_seq, int rows, int vocab) {
 void launch_accept_sampled(int dtype, AcceptArgs a, void* ws, hipStream_t s) {
   a.pieces = pieces_of(a.vocab, dtype == AD_BF16 ? kPiece<bf16_t> : kPiece<float>);
   // Sums in 64 bits of every row serve the draw as well as the test, and the draw is the second and last launch.  Where all rows together are large, only the deciding
-  // ones get them, in launches of their own (us, all rows / the deciding ones: 8 rows of 32,000 8.1 / 10.8, 128 rows 16.6 / 18.9, 800 rows 41.1 / 33.5,
+  // ones and those whose test is close (accept_decide) get them, in launches of their own (us, all rows / the deciding ones: 8 rows of 32,000 8.1 / 10.8, 128 rows 16.6 / 18.9, 800 rows 41.1 / 33.5,
   // 352 rows of 100,003 in bf16 47 / 39).
   const bool wide = a.probs || (size_t)a.rows * a.vocab < ((size_t)1 << 23);
   a.rest = a.probs || !wide;
@@ -588,7 +646,9 @@ void launch_accept_sampled(int dtype, AcceptArgs a, void* ws, hipStream_t s) {
     if (wide) k_accept_stats<T, true, PK><<<grid, kAcceptThreads, 0, s>>>(a);
     else k_accept_stats<T, false, PK><<<grid, kAcceptThreads, 0, s>>>(a);
     if (a.rest) {
-      k_accept_rows<T, PK><<<dim3((by.y + 3) / 4, by.z), kAcceptThreads, 0, s>>>(a);
+      const dim3 of_four((by.y + 3) / 4, by.z);
+      if (wide) k_accept_rows<T, PK, false><<<of_four, kAcceptThreads, 0, s>>>(a);
+      else k_accept_rows<T, PK, true><<<of_four, kAcceptThreads, 0, s>>>(a);
       auto draw = [&](auto probs) {
         k_accept_rest<T, probs.value><<<dim3(a.pieces, a.n_seq), kAcceptThreads, 0, s>>>(a);
         k_accept_pick<T, true, probs.value><<<a.n_seq, kAcceptThreads, 0, s>>>(a);

@@ -257,3 +257,70 @@ def test_captured_and_replayed():
         assert all(torch.equal(a, b) for a, b in zip(out, want))
         r["t"][:] = 1
         check(r, rows, (out[0].cpu().tolist(), out[1].cpu().tolist()))
+
+
+def next_to_the_border(seed, n, vocab, bf16):
+    """n rows, each a sequence: every 1000th token about 2^8 times as likely as the others, so that all sums over a part of the row are of many equal weights below its
+    largest; a drafted token of probability 0.01 to 0.1, and numbers u one to three steps of fp32 beside that probability (computed in 64 bits)."""
+    rng = np.random.default_rng(seed)
+    t = (0.5 + 1.5 * rng.random(n)).astype(np.float32)
+    low = -rng.random(n)
+    x = torch.tensor(low, dtype=torch.float32)[:, None].repeat(1, vocab)
+    x[:, ::1000] += torch.tensor(t * (7 + 2 * rng.random(n)) * np.log(2), dtype=torch.float32)[:, None]
+    d = rng.integers(0, vocab, n).astype(np.int32)
+    x = x.to(torch.bfloat16) if bf16 else x
+    p = 0.01 + 0.09 * rng.random(n)
+    for b in range(n):
+        others = np.exp(x[b].double().numpy() / np.float64(t[b]))
+        others[d[b]] = 0
+        x[b, d[b]] = float(t[b]) * np.log(others.sum() * p[b] / (1 - p[b]))
+        drafted = np.exp(float(x[b, d[b]]) / np.float64(t[b]))                 # (of the rounded score)
+        p[b] = drafted / (others.sum() + drafted)
+    u = p.astype(np.float32).view(np.int32) + rng.choice([-3, -2, -1, 1, 2, 3], n).astype(np.int32)
+    u = u.view(np.float32)
+    assert np.all(np.abs(u / p - 1) > 2.0 ** -26)             # (far beyond the 7e-12 of the sums in 64 bits)
+    return dict(x=x, q=None, d=d, u=u, v=rng.random(n).astype(np.float32), t=t), u < p
+
+
+def part(p, lo, hi):
+    return {key: None if a is None else a[lo:hi] for key, a in p.items()}
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("n,vocab", [(304, 32003), (90, 100003)])
+def test_numbers_next_to_the_border_whatever_the_size_of_the_call(n, vocab, bf16):
+    """The same numbers give the same tokens in a call of 8 rows and in a large one: those of the definition."""
+    p, stands = next_to_the_border(vocab + n, n, vocab, bf16)
+    assert n * vocab > 1 << 23
+    got = run(p, [1] * n)
+    drawn = [b for b in range(n) if got[1][b] != p["d"][b]]
+    assert drawn == [b for b in range(n) if not stands[b]]
+    check(p, [1] * n, got)
+    for lo in range(0, n, 8):
+        m = min(8, n - lo)
+        assert 8 * vocab < 1 << 23
+        assert run(part(p, lo, lo + m), [1] * m) == (got[0][lo:lo + m], got[1][lo:lo + m])
+
+
+def test_scores_and_temperatures_at_the_ends_of_fp32_in_a_large_call():
+    """Differences of scores, and products with 1 / T, that 32 bits do not hold."""
+    n, vocab = 272, 32003
+    p = problem(12, [1] * n, vocab, False)
+    low = torch.finfo(torch.float32).min
+    for b in range(n):
+        kind = b % 4
+        if kind == 0:                                          # scores of +-3e38 at a temperature as large
+            p["x"][b], p["t"][b] = p["x"][b].clamp(-3, 3) * 1e38, 5e37
+        elif kind == 1:                                        # the type's lowest value beside a score of 2e38
+            p["x"][b, ::2], p["x"][b, 7], p["t"][b] = low, 2e38, 1e38
+        elif kind == 2:                                        # 1 / T next to the largest number of fp32
+            p["x"][b], p["t"][b] = p["x"][b] * 1e-38, 4e-39
+        else:                                                  # and next to the smallest
+            p["t"][b] = 3e38
+    p["u"][:] = np.random.default_rng(13).random(n) / 16000
+    assert n * vocab > 1 << 23
+    got = run(p, [1] * n)
+    check(p, [1] * n, got)
+    assert 0 < sum(a == b for a, b in zip(got[1], p["d"].tolist())) < n
+    for lo in (0, 136):
+        assert run(part(p, lo, lo + 8), [1] * 8) == (got[0][lo:lo + 8], got[1][lo:lo + 8])
