@@ -31,6 +31,8 @@ struct AcceptRowInfo { double z; float m; int stands; };
 void launch_accept_inputs(const int* draft, const float* u, const float* v, const float* t, int k_max, const int* row_start, int n_seq, int* draft_out,
                           float* u_out, float* v_out, float* t_out, hipStream_t s);
 size_t accept_bytes(int n_seq, int rows, int vocab);
+// Whether a launch looks the rows up in the table instead of taking max_rows of every sequence (by sequence: at most 65,535)
+inline bool accept_packed(int n_seq, int rows, int max_rows) { return (size_t)n_seq * max_rows > 4 * (size_t)rows; }
 void launch_accept_sampled(int dtype, AcceptArgs a, void* ws, hipStream_t s);
 
 }  // namespace ad

@@ -632,7 +632,7 @@ void launch_accept_sampled(int dtype, AcceptArgs a, void* ws, hipStream_t s) {
   a.rest = a.probs || !wide;
   // Rows by sequence (max_rows of every one), or packed, which costs each workgroup the search for its sequence, where that would be mostly rows that are not there (us, by
   // sequence / packed: 32 blocks of up to 25 rows 35.2 / 36.1, 64 of 8 rows of 100,003 45.8 / 47; 256 of 8 rows of 32,000 and max_rows = 8 62 / 69, without a bound 2041 / 69).
-  const bool packed = (size_t)a.n_seq * a.max_rows > 4 * (size_t)a.rows;
+  const bool packed = accept_packed(a.n_seq, a.rows, a.max_rows);
   const dim3 by = packed ? dim3(1, std::min(a.rows, kRowsY), (a.rows + kRowsY - 1) / kRowsY) : dim3(1, a.max_rows, a.n_seq);
   char* w = (char*)ws;
   a.piece_sum = (double*)w;

@@ -324,3 +324,19 @@ def test_scores_and_temperatures_at_the_ends_of_fp32_in_a_large_call():
     assert 0 < sum(a == b for a, b in zip(got[1], p["d"].tolist())) < n
     for lo in (0, 136):
         assert run(part(p, lo, lo + 8), [1] * 8) == (got[0][lo:lo + 8], got[1][lo:lo + 8])
+
+
+@pytest.mark.parametrize("lo,hi", [(8, 10), (15, 19)])
+def test_more_rows_than_a_launch_has_along_an_axis(lo, hi):
+    """About 33,000 and 70,000 packed rows in short blocks, without a bound and with one."""
+    rng = np.random.default_rng(lo)
+    rows = [int(r) for r in rng.integers(lo, hi, 4096)]
+    rows[17], rows[4095] = 0, 3
+    n, vocab = sum(rows), 5
+    assert n > (65536 if lo > 8 else 32768)
+    x = rng.standard_normal((n, vocab)).astype(np.float32)
+    p = dict(x=torch.tensor(x), q=None, d=np.where(rng.random(n) < 0.9, x.argmax(1), rng.integers(0, vocab, n)).astype(np.int32), u=(rng.random(n) * 0.3).astype(np.float32),
+             v=rng.random(4096).astype(np.float32), t=np.ones(4096, np.float32))
+    got = run(p, rows)
+    check(p, rows, got)
+    assert got == run(p, rows, max_rows=max(rows))

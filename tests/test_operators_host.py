@@ -163,3 +163,14 @@ def test_contexts_with_caches_in_8_bits():
 
 def test_verify_sampled_without_a_context():
     assert ad.lib().ad_verify_sampled(None, None, None, None, None, None, None, None, None) == ad.AD_EINVAL
+
+
+def test_accept_sampled_takes_as_many_rows_as_it_can_look_up():
+    """max_rows above 65,535 is refused where rows go by sequence only."""
+    L = ad.lib()
+
+    def go(n_seq, rows, most, ws=None, size=0):
+        return L.ad_accept_sampled(P, ad.AD_F32, 1000, 1000, P, None, 1000, None, P, P, P, n_seq, rows, most, P, P, ws, size, None)
+    assert go(4, 70000, 70000) == ad.AD_EINVAL and "65535" in message()
+    assert go(5, 70000, 70000) == ad.AD_EINVAL and "null" in message()               # (looked up: the next thing that is wrong)
+    assert go(5, 70000, 70000, ws=P) == ad.AD_ENOMEM
