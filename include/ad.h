@@ -370,7 +370,7 @@ int ad_kv8_attend(const ad_kv8_config* cfg, const void* cache, const void* q, in
  *   accept_u     DEVICE [rows]; pick_u: DEVICE [n_seq]
  *   n_accept     DEVICE [n_seq] out: tokens of the sequence's block, the replacement included
  *   tokens       DEVICE [rows] out: those tokens, AD_NEVER behind them to the end of the sequence's rows
- * row_start, rows and max_rows as above, rows from 1 on.  max_rows above 65535 is taken only where n_seq * max_rows > 4 * rows
+ * row_start, rows and max_rows as above; a call without rows (rows = 0) sets the counts to 0.  max_rows above 65535 is taken only where n_seq * max_rows > 4 * rows
  * (rows are looked up in the table there, and max_rows = rows will do).
  * A sequence whose next row has no distribution (no finite score, a NaN or +inf among them, T not a positive number) ends before that row.
  * `workspace`: ad_accept_sampled_bytes of device memory, as ad_kv8_attend's.  Enqueues kernels on `hip_stream`, as the calls above. */

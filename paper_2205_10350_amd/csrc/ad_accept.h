@@ -34,5 +34,6 @@ size_t accept_bytes(int n_seq, int rows, int vocab);
 // Whether a launch looks the rows up in the table instead of taking max_rows of every sequence (by sequence: at most 65,535)
 inline bool accept_packed(int n_seq, int rows, int max_rows) { return (size_t)n_seq * max_rows > 4 * (size_t)rows; }
 void launch_accept_sampled(int dtype, AcceptArgs a, void* ws, hipStream_t s);
+void launch_accept_nothing(const AcceptArgs& a, hipStream_t s);   // a.rows == 0: counts of 0
 
 }  // namespace ad

@@ -623,6 +623,7 @@ size_t accept_bytes(int n_seq, int rows, int vocab) {
   const size_t p = pieces_of(vocab, kPiece<float>);   // (bf16 has half as many)
   return up256(rows * p * 8) + up256(rows * p * 4) + up256((size_t)n_seq * p * 8) + up256(rows * sizeof(AcceptRowInfo));
 }
+void launch_accept_nothing(const AcceptArgs& a, hipStream_t s) { k_accept_pick<float, false, false><<<a.n_seq, kDecideThreads, 0, s>>>(a); }
 void launch_accept_sampled(int dtype, AcceptArgs a, void* ws, hipStream_t s) {
   a.pieces = pieces_of(a.vocab, dtype == AD_BF16 ? kPiece<bf16_t> : kPiece<float>);
   // Sums in 64 bits of every row serve the draw as well as the test, and the draw is the second and last launch.  Where all rows together are large, only the deciding

@@ -117,10 +117,17 @@ int ad_accept_sampled(const void* logits, int32_t dtype, int64_t logits_stride, 
   if (dtype != AD_F32 && dtype != AD_BF16) return refuse("ad_accept_sampled: dtype must be AD_F32 or AD_BF16");
   if (vocab < 1 || vocab > (1 << 24)) return refuse("ad_accept_sampled: vocab outside [1, 2^24]");
   if (n_seq < 1 || n_seq > 4096) return refuse("ad_accept_sampled: n_seq outside [1, 4096]");
-  if (rows < 1 || max_rows < 1 || max_rows > rows) return refuse("ad_accept_sampled: rows < 1 or max_rows outside [1, rows]");
+  if (rows < 0 || max_rows > rows || max_rows < (rows ? 1 : 0)) return refuse("ad_accept_sampled: rows < 0 or max_rows outside [1, rows]");
+  if (!pick_u || !row_start || !n_accept) return refuse("ad_accept_sampled: null buffer");
+  if (rows == 0) {   // (no sequence has a row: counts of 0)
+    AcceptArgs a{};
+    a.pick_u = pick_u; a.row_start = row_start; a.vocab = vocab; a.n_seq = n_seq; a.n_accept = n_accept;
+    launch_accept_nothing(a, (hipStream_t)hip_stream);
+    return launched("ad_accept_sampled");
+  }
   if (!accept_packed(n_seq, rows, max_rows) && max_rows > 65535)
     return refuse("ad_accept_sampled: max_rows above 65535 (taken only where n_seq * max_rows > 4 * rows)");
-  if (!logits || !draft || !accept_u || !pick_u || !row_start || !n_accept || !tokens || !workspace) return refuse("ad_accept_sampled: null buffer");
+  if (!logits || !draft || !accept_u || !tokens || !workspace) return refuse("ad_accept_sampled: null buffer");
   if (logits_stride < vocab || (draft_probs && probs_stride < vocab)) return refuse("ad_accept_sampled: row stride below vocab");
   if ((uintptr_t)logits & (dtype == AD_F32 ? 3 : 1)) return refuse("ad_accept_sampled: logits not aligned to their type");
   if ((uintptr_t)workspace & 255) return refuse("ad_accept_sampled: the workspace must be 256-byte aligned");

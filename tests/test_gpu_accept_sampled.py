@@ -340,3 +340,13 @@ def test_more_rows_than_a_launch_has_along_an_axis(lo, hi):
     got = run(p, rows)
     check(p, rows, got)
     assert got == run(p, rows, max_rows=max(rows))
+
+
+def test_no_rows():
+    """A call whose sequences have nothing to verify, as a cache takes one."""
+    none = torch.zeros((0, 100), device="cuda")
+    empty = torch.zeros(0, device="cuda")
+    for probs in (None, none):
+        for most in (None, 0):
+            n, tok = ad.accept_sampled(none, i32([]), i32([0, 0, 0, 0]), empty, f32([0.1, 0.2, 0.3]), draft_probs=probs, max_rows=most)
+            assert n.tolist() == [0, 0, 0] and n.dtype == torch.int32 and tok.shape == (0,) and tok.dtype == torch.int32

@@ -174,3 +174,12 @@ def test_accept_sampled_takes_as_many_rows_as_it_can_look_up():
     assert go(4, 70000, 70000) == ad.AD_EINVAL and "65535" in message()
     assert go(5, 70000, 70000) == ad.AD_EINVAL and "null" in message()               # (looked up: the next thing that is wrong)
     assert go(5, 70000, 70000, ws=P) == ad.AD_ENOMEM
+
+
+def test_accept_sampled_of_no_rows_needs_no_more_than_the_counts_place():
+    L = ad.lib()
+
+    def go(rows=0, most=0, u=P, start=P, n=P):
+        return L.ad_accept_sampled(None, ad.AD_F32, 1000, 1000, None, None, 1000, None, None, u, start, 3, rows, most, n, None, None, 0, None)
+    for bad in (dict(most=1), dict(rows=-1, most=-1), dict(u=None), dict(start=None), dict(n=None), dict(rows=1, most=1)):
+        assert go(**bad) == ad.AD_EINVAL, bad
