@@ -67,8 +67,10 @@ class Kv8Cache:
 
     `row_start` [n_seq + 1] and `length` [n_seq] are int32 tensors on the device: sequence b has the packed rows row_start[b] ..
     row_start[b + 1] - 1, at positions length[b] ..  Taking tokens back is passing a smaller length: any since the start of the last
-    append, or a multiple of 32.  `max_rows` (the longest sequence's rows, default: all, at most k_max) and `max_keys` (default: the capacity)
-    bound the launch; what the tables say beyond them is left out.
+    append, or a multiple of 32.  `max_rows` (the longest sequence's rows) and `max_keys` (default: the capacity) bound the launch; what the tables say
+    beyond them is left out.  Without `max_rows` a sequence may have k_max rows in a call (closed: the capacity): the tables are read on the device, so it is the caller's to
+    see that none has more, whose rows would be left out.  More packed rows than all sequences together may have are refused: some would be
+    left out, or lie behind the last sequence, and then `max_rows` says that this is meant.
     """
 
     def __init__(self, n_seq, n_heads, head_width, capacity, k_max=1, format="e4m3", closed=False, device="cuda"):
@@ -106,6 +108,11 @@ class Kv8Cache:
         if rc:
             B._check(rc)
 
+    def _most(self, rows):
+        if rows > self.cfg.n_seq * self.most_rows:
+            _refuse(f"{rows} rows, where {self.cfg.n_seq} sequence(s) may have {self.most_rows} each in a call: pass max_rows if rows lie behind the last sequence")
+        return min(rows, self.most_rows)
+
     def append(self, k, v, row_start, length, max_rows=None):
         """Rows k, v [rows, n_heads, head_width] bf16 become the tokens from length[b] on."""
         c, i = self.cfg, self.index
@@ -114,7 +121,7 @@ class Kv8Cache:
         if vrows != rows:
             _refuse("k and v must have as many rows")
         start, at = _flat(row_start, "row_start", i, self._i32, self._start), _flat(length, "length", i, self._i32, self._len)
-        most = min(rows, self.most_rows) if max_rows is None else _count("max_rows", max_rows)
+        most = self._most(rows) if max_rows is None else _count("max_rows", max_rows)
         self._call(lambda stream: self.L.ad_kv8_append(self._cfg, self._at, kp, ks, vp, vs, start, at, rows, most, stream))
 
     def read(self, row_start, begin, length, rows, max_rows=None, dtype=None):
@@ -144,7 +151,7 @@ class Kv8Cache:
         heads = q.shape[1] if isinstance(q, torch.Tensor) and q.dim() == 3 else 0
         qp, qs, rows = _rows(q, "q", i, self._bf16, heads, c.head_width)
         start, at = _flat(row_start, "row_start", i, self._i32, self._start), _flat(length, "length", i, self._i32, self._len)
-        most = (rows if c.closed else min(rows, c.k_max)) if max_rows is None else _count("max_rows", max_rows)
+        most = (rows if c.closed else self._most(rows)) if max_rows is None else _count("max_rows", max_rows)
         keys = c.capacity if max_keys is None else min(max_keys, c.capacity)
         scale = self._scale if scale is None else scale
 

@@ -367,3 +367,29 @@ def test_a_long_cache_past_32_bits():
     got = cache.read(starts([0] * (n_seq - 1) + [70]), i32([0] * (n_seq - 1) + [base]), i32([0] * (n_seq - 1) + [base + 70]), rows=70, dtype=torch.float32)
     for g, t in zip(got, (k, v)):
         assert torch.equal(g.cpu(), torch.tensor(tokens_as_read(f64(t[0]), 70, "e4m3")).to(torch.float32))
+
+
+def test_rows_that_no_sequence_may_have_are_refused_by_default():
+    """Without max_rows: more packed rows than the sequences may have in a call, of which some would be dropped."""
+    heads, w = 2, 64
+    k, v, q = (draw(54 + i, 100, heads, w).cuda() for i in range(3))
+    one = ad.Kv8Cache(1, heads, w, capacity=128)                       # (k_max = 1)
+    two = ad.Kv8Cache(2, heads, w, capacity=128, k_max=25)
+    for cache, rows in ((one, [100]), (one, [2]), (two, [25, 26])):
+        n = sum(rows)
+        at = i32([0] * len(rows))
+        with pytest.raises(ad.AdError, match="max_rows") as e:
+            cache.append(k[:n], v[:n], starts(rows), at)
+        assert e.value.code == ad.AD_EINVAL
+        with pytest.raises(ad.AdError, match="max_rows"):
+            cache.attend(q[:n], starts(rows), at)
+    # as many as there may be; rows behind the last sequence, where the caller says how many a sequence has
+    two.append(k[:50], v[:50], starts([25, 25]), i32([0, 0]))
+    one.append(k, v, starts([1]), i32([0]), max_rows=1)
+    assert torch.equal(one.read(starts([1]), i32([0]), i32([1]), rows=1)[0][0], k[0])
+    closed = ad.Kv8Cache(1, heads, w, capacity=128, closed=True)
+    with pytest.raises(ad.AdError, match="max_rows"):
+        closed.append(draw(57, 129, heads, w).cuda(), draw(58, 129, heads, w).cuda(), starts([129]), i32([0]))
+    closed.append(k, v, starts([100]), i32([0]))
+    many = closed.attend(torch.cat([q] * 3), starts([300]), i32([100]))    # (queries over a memory: as many as one likes)
+    assert torch.equal(many[:100], many[200:])
