@@ -49,6 +49,11 @@ def _count(name, n):
     return n
 
 
+def _bound(max_rows, rows):
+    """max_rows as the call takes it: no sequence has more than all rows."""
+    return min(_count("max_rows", max_rows), rows)
+
+
 def _on(index, call):
     """call(stream) with GPU `index` current and its current stream."""
     import torch
@@ -67,7 +72,7 @@ class Kv8Cache:
 
     `row_start` [n_seq + 1] and `length` [n_seq] are int32 tensors on the device: sequence b has the packed rows row_start[b] ..
     row_start[b + 1] - 1, at positions length[b] ..  Taking tokens back is passing a smaller length: any since the start of the last
-    append, or a multiple of 32.  `max_rows` (the longest sequence's rows) and `max_keys` (default: the capacity) bound the launch; what the tables say
+    append, or a multiple of 32.  `max_rows` (at least the longest sequence's rows) and `max_keys` (default: the capacity) bound the launch; what the tables say
     beyond them is left out.  Without `max_rows` a sequence may have k_max rows in a call (closed: the capacity): the tables are read on the device, so it is the caller's to
     see that none has more, whose rows would be left out.  More packed rows than all sequences together may have are refused: some would be
     left out, or lie behind the last sequence, and then `max_rows` says that this is meant.
@@ -121,7 +126,7 @@ class Kv8Cache:
         if vrows != rows:
             _refuse("k and v must have as many rows")
         start, at = _flat(row_start, "row_start", i, self._i32, self._start), _flat(length, "length", i, self._i32, self._len)
-        most = self._most(rows) if max_rows is None else _count("max_rows", max_rows)
+        most = self._most(rows) if max_rows is None else _bound(max_rows, rows)
         self._call(lambda stream: self.L.ad_kv8_append(self._cfg, self._at, kp, ks, vp, vs, start, at, rows, most, stream))
 
     def read(self, row_start, begin, length, rows, max_rows=None, dtype=None):
@@ -138,7 +143,7 @@ class Kv8Cache:
         k = torch.empty((rows, c.n_heads, c.head_width), dtype=dtype, device=self.device)
         v = torch.empty_like(k)
         kp, vp = k.data_ptr(), v.data_ptr()
-        most = rows if max_rows is None else _count("max_rows", max_rows)
+        most = rows if max_rows is None else _bound(max_rows, rows)
         kind = B.AD_F32 if dtype is torch.float32 else B.AD_BF16
         self._call(lambda stream: self.L.ad_kv8_read(self._cfg, self._at, start, first, at, rows, most, kind, kp, vp, stream))
         return k, v
@@ -151,7 +156,7 @@ class Kv8Cache:
         heads = q.shape[1] if isinstance(q, torch.Tensor) and q.dim() == 3 else 0
         qp, qs, rows = _rows(q, "q", i, self._bf16, heads, c.head_width)
         start, at = _flat(row_start, "row_start", i, self._i32, self._start), _flat(length, "length", i, self._i32, self._len)
-        most = (rows if c.closed else self._most(rows)) if max_rows is None else _count("max_rows", max_rows)
+        most = (rows if c.closed else self._most(rows)) if max_rows is None else _bound(max_rows, rows)
         keys = c.capacity if max_keys is None else min(max_keys, c.capacity)
         scale = self._scale if scale is None else scale
 
@@ -183,7 +188,8 @@ def accept_sampled(logits, draft, row_start, accept_u, pick_u, temperature=None,
     """Verification of drafted tokens for sampled decoding (include/ad.h, "acceptance of sampled blocks"): (n_accept [n_seq], tokens [rows]).
 
     logits [rows, vocab] fp32 or bf16 (rows may lie apart), draft [rows] int32 (AD_NEVER: none), row_start [n_seq + 1] int32, accept_u [rows] and pick_u [n_seq]
-    fp32 uniform in [0, 1), temperature [n_seq] fp32 or None (1), draft_probs [rows, vocab] fp32 or None (drafted tokens are certain)."""
+    fp32 uniform in [0, 1), temperature [n_seq] fp32 or None (1), draft_probs [rows, vocab] fp32 or None (drafted tokens are certain),
+    max_rows: at least the longest sequence's rows (default: all)."""
     import torch
     f32, i32 = torch.float32, torch.int32
     if not isinstance(logits, torch.Tensor) or logits.dim() != 2 or logits.dtype not in (f32, torch.bfloat16) or not logits.is_cuda:
@@ -211,7 +217,7 @@ def accept_sampled(logits, draft, row_start, accept_u, pick_u, temperature=None,
         ws = torch.empty(max(need, 1), dtype=torch.uint8, device=logits.device)
         return B.lib().ad_accept_sampled(logits.data_ptr(), B.AD_F32 if logits.dtype is f32 else B.AD_BF16, stride if rows > 1 else vocab, vocab,
                                          drafted, probs, probs_stride if rows > 1 else vocab, temp, u, v, start, n_seq, rows,
-                                         rows if max_rows is None else _count("max_rows", max_rows), n_accept.data_ptr(), tokens.data_ptr(), ws.data_ptr(), need, stream)
+                                         rows if max_rows is None else _bound(max_rows, rows), n_accept.data_ptr(), tokens.data_ptr(), ws.data_ptr(), need, stream)
     rc = _on(i, call)
     if rc:
         B._check(rc)

@@ -350,3 +350,14 @@ def test_no_rows():
         for most in (None, 0):
             n, tok = ad.accept_sampled(none, i32([]), i32([0, 0, 0, 0]), empty, f32([0.1, 0.2, 0.3]), draft_probs=probs, max_rows=most)
             assert n.tolist() == [0, 0, 0] and n.dtype == torch.int32 and tok.shape == (0,) and tok.dtype == torch.int32
+
+
+def test_a_bound_above_the_rows_is_a_bound():
+    rows = [2, 1]
+    p = problem(14, rows, 60, True)
+    assert run(p, rows) == run(p, rows, max_rows=25) == run(p, rows, max_rows=2)
+    for most in (0, -1):
+        with pytest.raises(ad.AdError):
+            run(p, rows, max_rows=most)
+    n, tok = ad.accept_sampled(torch.zeros((0, 60), device="cuda"), i32([]), i32([0, 0]), f32([]), f32([0.5]), max_rows=25)
+    assert n.tolist() == [0] and tok.shape == (0,)

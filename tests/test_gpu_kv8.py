@@ -393,3 +393,18 @@ def test_rows_that_no_sequence_may_have_are_refused_by_default():
     closed.append(k, v, starts([100]), i32([0]))
     many = closed.attend(torch.cat([q] * 3), starts([300]), i32([100]))    # (queries over a memory: as many as one likes)
     assert torch.equal(many[:100], many[200:])
+
+
+def test_a_bound_above_the_rows_is_a_bound():
+    """max_rows as a program sets it once, for its longest blocks, in a call of few rows."""
+    heads, w = 2, 64
+    k, v, q = (draw(60 + i, 3, heads, w).cuda() for i in range(3))
+    got = []
+    for most in (3, 25):
+        cache = stale(ad.Kv8Cache(1, heads, w, capacity=40, k_max=25))
+        cache.append(k, v, starts([3]), i32([0]), max_rows=most)
+        got.append((cache.attend(q, starts([3]), i32([0]), max_rows=most), *cache.read(starts([3]), i32([0]), i32([3]), rows=3, max_rows=most)))
+        assert cache.attend(q[:0], starts([0]), i32([3]), max_rows=most).shape == (0, heads, w)
+        with pytest.raises(ad.AdError):
+            cache.append(k, v, starts([3]), i32([0]), max_rows=-1)
+    assert all(torch.equal(a, b) for a, b in zip(*got))
