@@ -159,9 +159,11 @@ _DTYPES = {"bf16": AD_BF16, "fp32": AD_F32, "bf16_kv_e4m3": AD_BF16_KV_E4M3, "bf
 
 def make_config(dims: dict, *, max_batch, max_src, max_len, k_max, dtype, special, tie_output=False,
                 debug_logits=False) -> AdConfig:
+    if dtype not in _DTYPES:
+        raise AdError(AD_EINVAL, f"dtype must be one of {', '.join(_DTYPES)}, not {dtype!r}")
     return AdConfig(dims["enc_layers"], dims["dec_layers"], dims["d_model"], dims["n_heads"], dims["d_ffn"],
                     dims["vocab"], max_batch, max_src, max_len, k_max, special["bos"], special["pad"],
-                    special["eos"], special["mask"], _DTYPES.get(dtype, AD_F32),
+                    special["eos"], special["mask"], _DTYPES[dtype],
                     int(tie_output), int(debug_logits))
 
 

@@ -183,3 +183,10 @@ def test_accept_sampled_of_no_rows_needs_no_more_than_the_counts_place():
         return L.ad_accept_sampled(None, ad.AD_F32, 1000, 1000, None, None, 1000, None, None, u, start, 3, rows, most, n, None, None, 0, None)
     for bad in (dict(most=1), dict(rows=-1, most=-1), dict(u=None), dict(start=None), dict(n=None), dict(rows=1, most=1)):
         assert go(**bad) == ad.AD_EINVAL, bad
+
+
+@pytest.mark.parametrize("dtype", ["bf16_kv_e4m", "BF16", "i8", None, 0])
+def test_unknown_dtypes_of_contexts_are_refused(dtype):
+    with pytest.raises(ad.AdError, match="dtype") as e:
+        config(dtype=dtype)
+    assert e.value.code == ad.AD_EINVAL
