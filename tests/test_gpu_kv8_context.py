@@ -4,6 +4,7 @@ import pytest
 
 import paper_2205_10350_amd as ad
 from ad_inputs import SPECIAL, edit_guide, init_weights, model_dims, positional_draft
+import kv8_oracle as K
 from kv8_reference import accept, tokens_as_read
 from oracle import ad_oracle as O
 
@@ -282,3 +283,15 @@ def test_sampled_verification_refuses():
         ctx.set_gadpp(1, 0.0)
         n, _ = ctx.verify_sampled([[5]], [[0.5]], [0.5])      # and the context is as it was
         assert n.tolist() == [1]
+
+
+@pytest.mark.parametrize("model", K.MODELS)
+def test_scores_of_peaked_attention_against_the_oracle_over_held_keys_and_values(model):
+    """Models in which wrong keys, scales, blocks or caches that are not held in 8 bits move the scores well past the tolerance (test_kv8_oracle.py shows it)."""
+    fmt = model[0]
+    dims, w, src, tok = K.problem(*model)
+    want, tol = K.tolerance(fmt, dims, w, src, tok)
+    with context(dims, w, "bf16_kv_" + fmt, B=1, max_src=K.S, max_len=K.T, k_max=K.T, logits=True) as ctx:
+        ctx.encode(ad.AD_VERIFIER, [src])
+        ctx.verify([tok])
+        assert K.far(ctx.debug_logits(), want) <= tol, K.far(ctx.debug_logits(), want) / tol
