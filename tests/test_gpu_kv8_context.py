@@ -295,3 +295,47 @@ def test_scores_of_peaked_attention_against_the_oracle_over_held_keys_and_values
         ctx.encode(ad.AD_VERIFIER, [src])
         ctx.verify([tok])
         assert K.far(ctx.debug_logits(), want) <= tol, K.far(ctx.debug_logits(), want) / tol
+
+
+@pytest.mark.parametrize("dtype", ["bf16_kv_e4m3", "bf16_kv_i8"])
+def test_ragged_batches_of_many_sequences(dtype):
+    """40 sequences, one long source and one long output among short ones and finished ones: writes, tiles and joins of rows go by the table of packed rows there, over two
+    splits of the keys.  Each sequence's scores are bit for bit those that it has by itself, where they go by sequence."""
+    dims = dict(enc_layers=1, dec_layers=2, d_model=128, n_heads=4, d_ffn=256, vocab=512)
+    w = init_weights(dims, 34, 0.1)
+    w["out.w"][EOS] = 0      # (an end of sentence that never scores highest)
+    n_seq, long, step = 40, 1300, 300
+    srcs = sources(dims, [700 if b == 3 else 1 + b % 3 for b in range(n_seq)], seed=35)
+    most = [long if b == 5 else 1 + b % 4 for b in range(n_seq)]
+    rng = np.random.default_rng(36)
+    with context(dims, w, dtype, B=n_seq, max_src=800, max_len=long, k_max=step, logits=True) as ctx:
+        greedy = ctx.decode_greedy([srcs[5]], max_out=[long])[0][0]
+        assert len(greedy) == long
+
+        def decode(which, drafts=None):
+            """All drafts of a run, per call, and every sequence's scores."""
+            ctx.encode(ad.AD_VERIFIER, [srcs[b] for b in which], max_out=[most[b] for b in which])
+            done, used, got = [0] * len(which), [], [[] for _ in which]
+            while done[which.index(5)] < long if 5 in which else any(d < most[b] for d, b in zip(done, which)):
+                d = []
+                for i, b in enumerate(which):
+                    if drafts is not None:
+                        d.append(drafts[len(used)][b])
+                    elif b == 5:
+                        d.append(greedy[done[i]:done[i] + step])
+                    else:
+                        d.append(rng.integers(5, 512, size=int(rng.integers(1, 4))).tolist() if done[i] < most[b] else [])
+                n, _ = ctx.verify(d)
+                s, at = ctx.debug_logits(), 0
+                for i in range(len(which)):
+                    got[i].append(s[at:at + len(d[i])])
+                    at += len(d[i])
+                    done[i] += int(n[i])
+                used.append({b: x for b, x in zip(which, d)})
+            return used, [np.concatenate(x) for x in got]
+        drafts, together = decode(list(range(n_seq)))
+        assert len(drafts) == -(-long // step)
+        for b in (3, 5, 0, 1, 22, 39):
+            _, alone = decode([b], drafts)
+            assert np.array_equal(alone[0], together[b][:len(alone[0])]), b
+            assert len(alone[0]) == len(together[b]), b
