@@ -408,3 +408,33 @@ def test_a_bound_above_the_rows_is_a_bound():
         with pytest.raises(ad.AdError):
             cache.append(k, v, starts([3]), i32([0]), max_rows=-1)
     assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+def check_scaled(got, q, k, v, at, rows, fmt, scale, closed):
+    got = got.float().cpu().numpy().astype(np.float64)
+    r = 0
+    for b, (n, m) in enumerate(zip(at, rows)):
+        for i in range(m):
+            kk, vv = f64(k[b]), f64(v[b])
+            if closed:
+                kk, vv = kk[:n], vv[:n]
+            ref, size, dots = attend(f64(q[r]), kk, vv, n + i, fmt, scale, closed)
+            tol = attend_tolerance(ref, size, dots, q.shape[2])
+            assert np.all(np.abs(got[r] - ref) <= tol), (b, i, np.max(np.abs(got[r] - ref) / tol))
+            r += 1
+
+
+@pytest.mark.parametrize("scale", [-0.2, 0.0, 0.7])
+@pytest.mark.parametrize("closed", [False, True])
+@pytest.mark.parametrize("fmt,width,heads,q_heads,at,rows", CASES[:5])
+def test_attention_with_a_scale_of_any_sign(fmt, width, heads, q_heads, at, rows, closed, scale):
+    """A negative scale prefers the smallest products, 0 weighs every visible key alike; tiles over a block's border, where some rows see a block and some do not."""
+    most = max(a + m for a, m in zip(at, rows))
+    k, v, q = draw(51, len(at), most, heads, width), draw(52, len(at), most, heads, width), draw(53, sum(rows), q_heads, width)
+    cache = stale(ad.Kv8Cache(len(at), heads, width, capacity=most, k_max=max(rows + [1]), format=fmt, closed=closed))
+    if closed:
+        feed(cache, k, v, at, max(at))
+    else:
+        feed(cache, k, v, at, max(rows + [1]))
+        cache.append(packed(k, at, rows), packed(v, at, rows), starts(rows), i32(at))
+    check_scaled(cache.attend(q.cuda(), starts(rows), i32(at), scale=scale), q, k, v, at, rows, fmt, scale, closed)
