@@ -172,6 +172,7 @@ int ad_verify_static(ad_ctx* ctx, const int32_t* draft, const int32_t* k,
  * drafter's are), from the given random numbers.  So outputs are distributed as sampled from the model token by token, at
  * temperature[b] (HOST [B], positive and finite; NULL: 1).  accept_u HOST [B, k_max] as draft, pick_u HOST [B]: in [0, 1).
  * verified[b][i]: the accepted tokens, the drawn one, and behind it the rows' arg maxima.  AD_NEVER as the last draft draws that row's token.
+ * A row without a distribution (a score that is NaN or +inf) keeps its arg max, and where that is the drafted token verification goes on behind it by arg maxima.
  * Needs cfg.debug_logits (AD_ESTATE otherwise: the scores it draws from are kept in the workspace) and beta = 1 (ad_set_gadpp). */
 int ad_verify_sampled(ad_ctx* ctx, const int32_t* draft, const int32_t* k, const float* accept_u, const float* pick_u,
                       const float* temperature, int32_t* n_accept, int32_t* next_token, int32_t* verified);
@@ -320,7 +321,7 @@ int ad_set_gadpp(ad_ctx* ctx, int32_t beta, float tau);
  * The calls enqueue kernels on `hip_stream` of the current device and return; they allocate nothing, copy nothing and may be captured
  * into graphs.  `row_start` [n_seq + 1], `length` [n_seq] and the like are DEVICE arrays here, read when the kernels run: sequence b has
  * the packed rows row_start[b] .. row_start[b + 1] - 1.  Tables are held to what the host arguments say (`rows` packed rows in all, at
- * most `max_rows` for a sequence, the capacity): what lies beyond is left out and its outputs are left as they were.
+ * most `max_rows` <= rows for a sequence, the capacity): what lies beyond is left out and its outputs are left as they were.
  * Calls on one cache that overlap in time race unless both only read it. */
 enum { AD_KV_E4M3 = 0, AD_KV_I8 = 1 };
 typedef struct {
@@ -348,7 +349,8 @@ int ad_kv8_read(const ad_kv8_config* cfg, const void* cache, const int32_t* row_
                 int32_t rows, int32_t max_rows, int32_t dtype, void* k_out, void* v_out, void* hip_stream);
 /* Attention, softmax(scale q k^T) v over what each row sees.  Growing: the rows at positions length[b] .. (append them first); closed:
  * every row sees length[b] tokens, a row of an empty memory becomes 0.  q, out: bf16 [rows, q_heads, head_width] with row strides
- * as above; query heads h * q_heads / n_heads .. share head h.  max_keys: at least the most tokens a row sees (growing: length[b] + rows
+ * as above; query heads h * q_heads / n_heads .. share head h.  scale: any finite number, below 0 and 0 too; scale * log2(e) and the scores are to stay finite in
+ * fp32.  max_keys: at least the most tokens a row sees (growing: length[b] + rows
  * of b).  `workspace`: ad_kv8_attend_bytes of device memory that no call overlapping in time uses, 256-byte aligned (null where 0 bytes). */
 size_t ad_kv8_attend_bytes(const ad_kv8_config* cfg, int32_t q_heads, int32_t rows, int32_t max_keys);
 int ad_kv8_attend(const ad_kv8_config* cfg, const void* cache, const void* q, int64_t q_stride, int32_t q_heads,
@@ -362,7 +364,7 @@ int ad_kv8_attend(const ad_kv8_config* cfg, const void* cache, const void* q, in
  * r(0) + .. + r(t) > pick_u (r(0) + .. + r(vocab - 1)), r = max(p_i - q_i, 0), and the sequence's block ends there.  With accept_u and pick_u uniform
  * in [0, 1) the tokens are distributed as drawn from p one by one.  draft_probs = NULL: the drafter is certain of its tokens (q_i = 1 at d_i:
  * a guide, an arg max).  AD_NEVER, or any id outside the vocabulary, stands for no draft: the row's token is drawn from p_i.
- * Sums over the vocabulary are kept in 64 bits, so that the same numbers give the same tokens.
+ * Sums over the vocabulary are kept in 64 bits, so that the same numbers give the same tokens, whatever other rows a call has.
  *   logits       DEVICE, AD_F32 or AD_BF16, [rows, vocab], rows logits_stride elements apart; -inf: never drawn
  *   draft        DEVICE [rows]: d_i of the packed rows, sequence by sequence (row_start as above)
  *   draft_probs  DEVICE fp32 [rows, vocab], rows probs_stride apart, or NULL

@@ -9,11 +9,12 @@
 // to the bit in every call that it may be part of (where a call is large a row's test is tried in 32 bits first: kNear):
 //   k_accept_stats   a workgroup per 8 KB of scores of a row: their maximum, and sum of exp2((x - max) log2(e) / T) (without d where q is none).  It reads everything
 //                    once and is bound by that; 64-bit exponentials cost 20 instructions a score.
-//   k_accept_rows    (q given, or many or large rows) a wave per row: its test
+//   k_accept_rows    (q given, or many or large rows) a wave per row: its test.  A row whose number is too close for sums in 32 bits, of random ones p in 16,000, is summed
+//                    again by its wave: 46 us more for a call over 32,000 fp32 scores, 121 over 100,003 in bf16 (all of 304 and 90 rows: 59 and 147).
 //   k_accept_rest    (then) a workgroup per 8 KB of scores of each sequence's deciding row: sum of r
 //   k_accept_pick    a workgroup per sequence: the rows' tests if they have not been made, the piece of the deciding row that holds the wanted sum, the token in it
-// One sentence of 8 rows over 32,000 scores: 3.9 and 4.7 us, launches and chains of waits.  32 blocks of up to 25 rows over 32,000 with probabilities (57 MB): 18.9,
-// 4.1, 6.3 and 7.5 us; 64 blocks of 3 to 8 rows over 100,003 bf16 scores (70 MB): 18.3, 4.1, 11.7 and 7.7.  The first of them reads at 3 to 3.8 TB/s with its
+// One sentence of 8 rows over 32,000 scores: 3.9 and 4.8 us, launches and chains of waits.  32 blocks of up to 25 rows over 32,000 with probabilities (57 MB): 19.5,
+// 4.5, 6.2 and 7.2 us; 64 blocks of 3 to 8 rows over 100,003 bf16 scores (70 MB): 18.2, 4.7, 9.0 and 7.8.  The first of them reads at 3 to 3.8 TB/s with its
 // exponentials; the three behind it wait for each other more than for memory.
 #include <hip/hip_runtime.h>
 #include <math.h>
@@ -627,8 +628,8 @@ void launch_accept_nothing(const AcceptArgs& a, hipStream_t s) { k_accept_pick<f
 void launch_accept_sampled(int dtype, AcceptArgs a, void* ws, hipStream_t s) {
   a.pieces = pieces_of(a.vocab, dtype == AD_BF16 ? kPiece<bf16_t> : kPiece<float>);
   // Sums in 64 bits of every row serve the draw as well as the test, and the draw is the second and last launch.  Where all rows together are large, only the deciding
-  // ones and those whose test is close (accept_decide) get them, in launches of their own (us, all rows / the deciding ones: 8 rows of 32,000 8.1 / 10.8, 128 rows 16.6 / 18.9, 800 rows 41.1 / 33.5,
-  // 352 rows of 100,003 in bf16 47 / 39).
+  // ones and those whose test is close (accept_decide) get them, in launches of their own (us, all rows / the deciding ones: 8 rows of 32,000 6.8 / 9.5, 128 rows 15.0 / 16.5, 263 rows 19.6 / 22.1,
+  // 800 rows 38.4 / 30.5, 352 rows of 100,003 in bf16 43.0 / 34.8).
   const bool wide = a.probs || (size_t)a.rows * a.vocab < ((size_t)1 << 23);
   a.rest = a.probs || !wide;
   // Rows by sequence (max_rows of every one), or packed, which costs each workgroup the search for its sequence, where that would be mostly rows that are not there (us, by

@@ -404,10 +404,11 @@ __global__ __launch_bounds__(256) void k_kv8_join(Kv8Attend a, Kv8Deal one, Kv8D
          uint2{f2bf_pair(o.x * inv, o.y * inv), f2bf_pair(o.z * inv, o.w * inv)});
 }
 
-// The split of the keys.  It goes by the cache's own sizes, so that a row's sums do not depend on a call.  512 keys where sequences and heads are few, more where
-// they fill the card by themselves (about 2048 workgroups of 512 keys) or where a call may bring many rows, which fill it too.  Measured, us by keys of a split:
-// 1 sequence of 8216 keys, 16 heads 512 14.3, 1024 15.9, 2048 21; 2 prompts of 512 rows 512 97, 1024 80, 2048 75; 32 sequences up to 8192 keys 2048 74, 4096 73,
-// 8192 84; 8 sequences of up to 32,000 keys, 8 heads of width 128, 2048 87, 4096 84, 8192 80.
+// The split of the keys.  It goes by the cache's own sizes, so that a row's sums do not depend on a call: few rows over one output want short splits, many rows or
+// sequences long ones, and the rule lies between them.  512 keys where sequences and heads are few, more where all of them together
+// would have over 2048 splits, which fill the card, or where a call may bring many rows, which fill it too.  Measured in caches for calls of up to 512 rows, us a replay by keys of a split (512, 1024, 2048, 4096, 8192; in
+// brackets what the rule takes): 25 rows over 8216 keys, 16 heads 12.1 [13.6] 17.5 25.4 42.3; 2 prompts' pieces of 512 rows over up to 8000 keys 83.6 [71.5] 65.0 65.0
+// 57.7; 32 sequences of up to 8192 keys, i8, 66.2 59.5 [58.8] 56.2 67.0; 8 sequences of up to 32,000 keys, 8 heads of width 128, 89.7 [84.1] 83.5 80.7 75.5.
 int kv8_split_keys(const Kv8Dims& d) {
   const size_t pairs = (size_t)d.n_seq * d.heads;
   size_t keys = 512;
