@@ -75,10 +75,6 @@ __device__ __forceinline__ double exp2_bulk(float x, double rate, double m) {
   const unsigned hi = (unsigned)(bits >> 32) + ((unsigned)__builtin_bit_cast(long long, big) << 20);
   return __builtin_bit_cast(double, (long long)((unsigned long long)hi << 32 | (unsigned)bits));
 }
-// Sums in 32 bits, what a row's test may be tried with: z off by less than 2^-15.9 of itself.  A weight 2^t, |t| <= 126, has three roundings in t (difference, rate,
-// product), 3 * 2^-24 |t|, that is ln(2) * 378 * 2^-24 = 262 * 2^-24 of the weight, the exponential's own 2 * 2^-24, and at most 7 * 2^-24 by additions; what is smaller
-// is 2^-125 at most, of which 2^24 are nothing beside z >= 1.  Within this part of u z, u < p is looked at again with the sums in 64 bits.
-constexpr double kNear = 0x1p-15;
 // and to f^11, nothing below 2^-1000, for the rows that are drawn from
 __device__ __forceinline__ double exp2_weight(float x, double rate, double m) {
   const double u = ((double)x - m) * rate, t = fmax(u, -1020.0);
@@ -99,6 +95,10 @@ __device__ __forceinline__ double exp2_weight(float x, double rate, double m) {
   const unsigned hi = (unsigned)(bits >> 32) + ((unsigned)__builtin_bit_cast(long long, big) << 20);
   return u < -1000.0 ? 0.0 : __builtin_bit_cast(double, (long long)((unsigned long long)hi << 32 | (unsigned)bits));
 }
+// Sums in 32 bits, what a row's test may be tried with: z off by less than 2^-15.9 of itself.  A weight 2^t, |t| <= 126, has three roundings in t (difference, rate,
+// product), 3 * 2^-24 |t|, that is ln(2) * 378 * 2^-24 = 262 * 2^-24 of the weight, the exponential's own 2 * 2^-24, and at most 7 * 2^-24 by additions; what is smaller
+// is 2^-125 at most, of which 2^24 are nothing beside z >= 1.  Within this part of u z, u < p is looked at again with the sums in 64 bits.
+constexpr double kNear = 0x1p-15;
 // sum over the wave, the same in every lane: lane moves as wave_sum's
 template <int CTRL> __device__ __forceinline__ double dpp_move_f64(double v) {
   const long long b = __builtin_bit_cast(long long, v);
