@@ -182,7 +182,7 @@ def _texts(c, seed):
 
 def _pick(t, lens, rows):
     """The packed rows [sum(rows), ..] of t [batch, tokens, ..] at tokens lens[b] .. lens[b] + rows[b] - 1."""
-    return torch.cat([t[b, n:n + r] for b, (n, r) in enumerate(zip(lens, rows))])
+    return torch.cat([t[b, n:n + r] for b, (n, r) in enumerate(zip(lens, rows)) if r])
 
 
 def _fill(cache, k, v, lens, piece):
