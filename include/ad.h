@@ -357,6 +357,26 @@ int ad_kv8_attend(const ad_kv8_config* cfg, const void* cache, const void* q, in
                   const int32_t* row_start, const int32_t* length, int32_t rows, int32_t max_rows, int32_t max_keys, float scale,
                   void* out, int64_t out_stride, void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/* Attention of continuations that share texts: ad_kv8_attend of rows whose sequences have, in front of their own tokens, the tokens of a text that another cache (or this
+ * one) holds once for all of them: softmax(scale q [K; K']^T) [V; V'], K the text's keys and K' what the row sees of its own sequence.  `cache` grows, `shared` is of the same heads,
+ * width and format, growing or closed; its sequence g is text g, with shared_length[g] (DEVICE [shared n_seq]) tokens: of a growing cache whole blocks of 32 (what is
+ * beyond the last whole one is left out), all of them in 8 bits.  Text g belongs to sequences seq_start[g] .. seq_start[g + 1] - 1 (DEVICE [shared n_seq + 1], ascending, within [0, n_seq]);
+ * sequences of no text see their own tokens alone.  Positions, `length` and max_keys are those of the sequences' own tokens.  max_shared_rows <= rows: at least the most packed
+ * rows of a text's sequences together; max_shared_keys: at least the longest text.  Everything else, the workspace too, as with ad_kv8_attend; a row's result
+ * depends, bit for bit, on both caches' descriptions, q_heads and the tokens it sees. */
+size_t ad_kv8_attend_shared_bytes(const ad_kv8_config* cfg, const ad_kv8_config* shared_cfg, int32_t q_heads, int32_t rows, int32_t max_keys, int32_t max_shared_keys);
+int ad_kv8_attend_shared(const ad_kv8_config* cfg, const void* cache, const ad_kv8_config* shared_cfg, const void* shared, const void* q, int64_t q_stride, int32_t q_heads,
+                         const int32_t* row_start, const int32_t* length, const int32_t* seq_start, const int32_t* shared_length, int32_t rows, int32_t max_rows,
+                         int32_t max_keys, int32_t max_shared_rows, int32_t max_shared_keys, float scale, void* out, int64_t out_stride, void* workspace,
+                         size_t workspace_bytes, void* hip_stream);
+/* Copies sequences, to fork them, to move them together or to take them over from another cache: tokens begin[i] .. end[i] - 1 of sequence source[i] of `from` become the first tokens
+ * of sequence place[i] of `cache`, i < n <= cache's n_seq (DEVICE arrays of n), as if all were read before any is written.  Both caches have the same heads, width and format
+ * and both grow or both are closed; they may be one (same description, begin = NULL) or must not overlap.  begin: multiples of 32 (NULL: 0).  end[i]: any length that the source may be
+ * taken back to; the copy may be taken back to any multiple of 32, or within its last block.  Blocks are copied as they are held: the copy reads as the source does, bit for bit.  What is outside either
+ * cache or beyond max_tokens tokens of an entry is left out; of entries with the same place the first counts. */
+int ad_kv8_copy(const ad_kv8_config* from_cfg, const void* from, const ad_kv8_config* cfg, void* cache, const int32_t* source, const int32_t* place, const int32_t* begin,
+                const int32_t* end, int32_t n, int32_t max_tokens, void* hip_stream);
+
 /* ---- acceptance of sampled blocks ---------------------------------------------------------------
  * Verification of drafted tokens where the output is drawn from the model's probabilities instead of being its arg max.  Row i of a
  * sequence has scores x_i over the vocabulary (what the model says in that place), p_i = softmax(x_i / T), a drafted token d_i and the
@@ -381,6 +401,29 @@ int ad_accept_sampled(const void* logits, int32_t dtype, int64_t logits_stride, 
                       const float* draft_probs, int64_t probs_stride, const float* temperature, const float* accept_u, const float* pick_u,
                       const int32_t* row_start, int32_t n_seq, int32_t rows, int32_t max_rows, int32_t* n_accept, int32_t* tokens,
                       void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* ---- truncated distributions ---------------------------------------------------------------------
+ * A row of scores x gives weights w = exp((x - max x) / T).  In order of falling score, equal ones by rising index, the first k tokens stay; of them the least number whose weights sum to p or more of
+ * theirs (one at least); of them those with w >= q (a probability of q or more of the most likely one's).  Settings are DEVICE arrays with an entry for each sequence:
+ *   temperature  T, positive and finite (NULL: 1)
+ *   top_k        k; 0, less, or the vocabulary and more: all (NULL: all)
+ *   top_p        p; 1 or more: all, 0 or less: one (NULL: all)
+ *   min_p        q; 0 or less: all, more than 1 as 1 (NULL: all)
+ * row_start DEVICE [n_seq + 1]: the packed rows of each sequence, n_seq <= 4096; rows of no sequence are left as they were.  NULL: row b is sequence b, n_seq = rows.
+ * logits as ad_accept_sampled's, rows < 2^22.  Weights are whole numbers of 2^-S of the largest (S = min(51, 62 - log2 vocab)) whose sums are exact: a row's result
+ * depends on its scores and settings alone.  A row without a distribution (no finite score, a NaN or +inf among them, T not a positive number, p or q NaN) gives AD_NEVER, or -inf throughout.
+ * The calls enqueue one kernel on `hip_stream` of the current device, need no workspace and may be captured into graphs.
+ *
+ * ad_sample_tokens draws: the least token t whose weights, summed over the tokens up to it that stay, exceed u times those of all that stay.
+ *   u            DEVICE [rows], in [0, 1)
+ *   tokens       DEVICE [rows] out
+ *   log_probs    DEVICE [rows] out, or NULL: the logarithm of the drawn token's probability among those that stay (NaN without a distribution) */
+int ad_sample_tokens(const void* logits, int32_t dtype, int64_t logits_stride, int32_t vocab, const float* temperature, const int32_t* top_k, const float* top_p,
+                     const float* min_p, const int32_t* row_start, int32_t n_seq, const float* u, int32_t rows, int32_t* tokens, float* log_probs, void* hip_stream);
+/* ad_truncate_scores writes the scores that stay, and -inf in place of the others: what ad_accept_sampled takes to verify drafts against the truncated distributions (at the same T).
+ * out: DEVICE [rows, vocab] of the scores' type, rows out_stride apart: the scores themselves (same stride) or not overlapping them. */
+int ad_truncate_scores(const void* logits, int32_t dtype, int64_t logits_stride, int32_t vocab, const float* temperature, const int32_t* top_k, const float* top_p,
+                       const float* min_p, const int32_t* row_start, int32_t n_seq, int32_t rows, void* out, int64_t out_stride, void* hip_stream);
 
 /* ---- host-only logic, exposed so that it can be tested without a GPU -------------------------- */
 

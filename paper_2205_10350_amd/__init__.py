@@ -6,4 +6,4 @@ from .binding import (  # noqa: F401
     AdConfig, AdError, AdKv8Config, AdStats, Context, EXPORTS, calibration_copy, calibration_mfma, LIB_PATH, config_check, host_simulate, lib, make_config,
     pack_weights, pack_weights_host, suffix_match, weights_layout, workspace_bytes,
 )
-from .operators import Kv8Cache, accept_sampled  # noqa: F401
+from .operators import Kv8Cache, accept_sampled, sample_tokens, truncate_scores  # noqa: F401

@@ -29,7 +29,8 @@ EXPORTS = [
     "ad_create", "ad_destroy", "ad_last_error", "ad_encode", "ad_verify", "ad_verify_static", "ad_verify_sampled", "ad_draft_nat", "ad_output",
     "ad_decode_greedy", "ad_decode_iad", "ad_decode_gad", "ad_debug_logits", "ad_time_verify_forward",
     "ad_suffix_match", "ad_host_simulate", "ad_set_option", "ad_get_option", "ad_calibration_copy", "ad_set_gadpp", "ad_time_output_projection", "ad_calibration_mfma",
-    "ad_kv8_check", "ad_kv8_bytes", "ad_kv8_append", "ad_kv8_read", "ad_kv8_attend_bytes", "ad_kv8_attend", "ad_accept_sampled_bytes", "ad_accept_sampled",
+    "ad_kv8_check", "ad_kv8_bytes", "ad_kv8_append", "ad_kv8_read", "ad_kv8_attend_bytes", "ad_kv8_attend", "ad_kv8_attend_shared_bytes", "ad_kv8_attend_shared", "ad_kv8_copy",
+    "ad_accept_sampled_bytes", "ad_accept_sampled", "ad_sample_tokens", "ad_truncate_scores",
 ]
 AD_OPT_GRAPHS = 3
 AD_OPT_GRAPHS_CAPTURED = 4
@@ -137,6 +138,12 @@ def lib():
     L.ad_accept_sampled_bytes.argtypes = [i32, i32, i32]; L.ad_accept_sampled_bytes.restype = C.c_size_t
     L.ad_accept_sampled.argtypes = [vp, i32, i64, i32, vp, vp, i64, vp, vp, vp, vp, i32, i32, i32, vp, vp, vp, C.c_size_t, vp]
     L.ad_accept_sampled.restype = C.c_int
+    L.ad_kv8_attend_shared_bytes.argtypes = [kvp, kvp, i32, i32, i32, i32]; L.ad_kv8_attend_shared_bytes.restype = C.c_size_t
+    L.ad_kv8_attend_shared.argtypes = [kvp, vp, kvp, vp, vp, i64, i32, vp, vp, vp, vp, i32, i32, i32, i32, i32, C.c_float, vp, i64, vp, C.c_size_t, vp]
+    L.ad_kv8_attend_shared.restype = C.c_int
+    L.ad_kv8_copy.argtypes = [kvp, vp, kvp, vp, vp, vp, vp, vp, i32, i32, vp]; L.ad_kv8_copy.restype = C.c_int
+    L.ad_sample_tokens.argtypes = [vp, i32, i64, i32, vp, vp, vp, vp, vp, i32, vp, i32, vp, vp, vp]; L.ad_sample_tokens.restype = C.c_int
+    L.ad_truncate_scores.argtypes = [vp, i32, i64, i32, vp, vp, vp, vp, vp, i32, i32, vp, i64, vp]; L.ad_truncate_scores.restype = C.c_int
     _lib = L
     return L
 

@@ -74,4 +74,23 @@ bool kv8_attend_fits(const Kv8Dims& d, const Kv8Rows& r, int q_heads, int max_ke
 void launch_kv8_attend(const Kv8Dims& d, const void* cache, const void* q, size_t q_stride, void* out, size_t out_stride, int q_heads,
                        const Kv8Rows& r, int max_keys, float scale, void* ws, hipStream_t s);
 
+// Texts that sequences share: group g's are seq_start[g] .. seq_start[g + 1] - 1, at most max_rows packed rows together, and its text has length[g] tokens of sequence g of another cache.
+struct Kv8Texts {
+  const int *seq_start, *length;
+  int n, max_rows;
+};
+// Attention of the rows over their text's cache and their own; ws: kv8_attend_shared_bytes().
+size_t kv8_attend_shared_bytes(const Kv8Dims& d, const Kv8Dims& texts, int q_heads, int rows, int max_keys, int max_text_keys);
+bool kv8_attend_shared_fits(const Kv8Dims& d, const Kv8Dims& texts, const Kv8Rows& r, const Kv8Texts& x, int q_heads, int max_keys, int max_text_keys);
+void launch_kv8_attend_shared(const Kv8Dims& d, const void* cache, const Kv8Dims& texts, const void* text_cache, const void* q, size_t q_stride, void* out, size_t out_stride,
+                              int q_heads, const Kv8Rows& r, const Kv8Texts& x, int max_keys, int max_text_keys, float scale, void* ws, hipStream_t s);
+
+// Tokens begin[i] (null: 0; a multiple of 32) .. end[i] - 1 of sequence source[i] become the first ones of sequence place[i], i < n <= 4096, as if all were read before any is
+// written.  What the tables say is held to the caches' sizes and max_tokens; of entries with one place the first counts.
+struct Kv8Moves {
+  const int *source, *place, *begin, *end;
+  int n, max_tokens;
+};
+void launch_kv8_copy(const Kv8Dims& from, const void* origin, const Kv8Dims& to, void* cache, const Kv8Moves& m, hipStream_t s);
+
 }  // namespace ad

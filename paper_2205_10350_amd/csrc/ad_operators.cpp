@@ -1,4 +1,4 @@
-// The operators behind the C ABI that need no context: 8-bit key/value caches and the acceptance of sampled blocks.
+// The operators behind the C ABI that need no context: 8-bit key/value caches, the acceptance of sampled blocks, and truncated distributions.
 // Arguments are checked here; the kernels hold device tables to what the host arguments say.
 #include <hip/hip_runtime.h>
 #include <stdio.h>
@@ -8,6 +8,7 @@
 #include "ad_accept.h"
 #include "ad_internal.h"
 #include "ad_kv8.h"
+#include "ad_truncate.h"
 
 using namespace ad;
 
@@ -106,6 +107,64 @@ int ad_kv8_attend(const ad_kv8_config* c, const void* cache, const void* q, int6
   return launched("ad_kv8_attend");
 }
 
+size_t ad_kv8_attend_shared_bytes(const ad_kv8_config* c, const ad_kv8_config* texts, int32_t q_heads, int32_t rows, int32_t max_keys, int32_t max_shared_keys) {
+  if (ad_kv8_check(c) != AD_OK || ad_kv8_check(texts) != AD_OK || q_heads < c->n_heads || rows < 1 || max_keys < 0 || max_shared_keys < 0) return 0;
+  return kv8_attend_shared_bytes(kv8_dims(*c), kv8_dims(*texts), q_heads, rows, max_keys, max_shared_keys);
+}
+
+int ad_kv8_attend_shared(const ad_kv8_config* c, const void* cache, const ad_kv8_config* texts, const void* text_cache, const void* q, int64_t q_stride, int32_t q_heads,
+                         const int32_t* row_start, const int32_t* length, const int32_t* seq_start, const int32_t* shared_length, int32_t rows, int32_t max_rows,
+                         int32_t max_keys, int32_t max_shared_rows, int32_t max_shared_keys, float scale, void* out, int64_t out_stride, void* workspace,
+                         size_t workspace_bytes, void* hip_stream) {
+  int rc = kv8_common(c, cache, row_start, length, rows, max_rows);
+  if (rc == AD_OK) rc = kv8_common(texts, text_cache, seq_start, shared_length, rows, max_shared_rows);
+  if (rc != AD_OK) return rc;
+  if (c->closed) return refuse("ad_kv8_attend_shared: the sequences' own cache must be a growing one");
+  if (texts->n_heads != c->n_heads || texts->head_width != c->head_width || texts->format != c->format)
+    return refuse("ad_kv8_attend_shared: both caches must have the same heads, head width and format");
+  if (q_heads < c->n_heads || q_heads % c->n_heads || q_heads / c->n_heads > 256) return refuse("ad_kv8_attend_shared: q_heads must be a multiple of n_heads, at most 256 times it");
+  if (!(scale > -INFINITY && scale < INFINITY)) return refuse("ad_kv8_attend_shared: scale must be finite");
+  if (max_keys < 0 || max_shared_keys < 0) return refuse("ad_kv8_attend_shared: max_keys or max_shared_keys < 0");
+  if (max_rows == 0) return AD_OK;
+  if (!q || !out) return refuse("ad_kv8_attend_shared: null buffer");
+  const int64_t width = (int64_t)q_heads * c->head_width;
+  if (q_stride < width || out_stride < width || off16(q, q_stride) || off16(out, out_stride))
+    return refuse("ad_kv8_attend_shared: q and out must be 16-byte aligned, their row strides multiples of 8 and at least q_heads * head_width");
+  const Kv8Dims d = kv8_dims(*c), t = kv8_dims(*texts);
+  if (max_rows > d.k_max) return refuse("ad_kv8_attend_shared: max_rows above k_max");
+  const size_t need = kv8_attend_shared_bytes(d, t, q_heads, rows, max_keys, max_shared_keys);
+  if (need && (!workspace || ((uintptr_t)workspace & 255))) return refuse("ad_kv8_attend_shared: the workspace must be 256-byte aligned device memory");
+  if (workspace_bytes < need) { set_global_error("ad_kv8_attend_shared: workspace smaller than ad_kv8_attend_shared_bytes()"); return AD_ENOMEM; }
+  const Kv8Rows r{row_start, nullptr, length, 1, rows, max_rows, c->n_seq};
+  const Kv8Texts x{seq_start, shared_length, texts->n_seq, max_shared_rows};
+  if (!kv8_attend_shared_fits(d, t, r, x, q_heads, max_keys, max_shared_keys)) return refuse("ad_kv8_attend_shared: more workgroups than a launch takes (sequences x heads x rows x keys)");
+  launch_kv8_attend_shared(d, cache, t, text_cache, q, (size_t)q_stride, out, (size_t)out_stride, q_heads, r, x, max_keys, max_shared_keys, scale, workspace, (hipStream_t)hip_stream);
+  return launched("ad_kv8_attend_shared");
+}
+
+int ad_kv8_copy(const ad_kv8_config* from, const void* origin, const ad_kv8_config* c, void* cache, const int32_t* source, const int32_t* place, const int32_t* begin,
+                const int32_t* end, int32_t n, int32_t max_tokens, void* hip_stream) {
+  int rc = ad_kv8_check(from);
+  if (rc == AD_OK) rc = ad_kv8_check(c);
+  if (rc != AD_OK) return rc;
+  if (!origin || !cache) return refuse("ad_kv8_copy: null buffer");
+  if (((uintptr_t)origin | (uintptr_t)cache) & 255) return refuse("ad_kv8_copy: the caches must be 256-byte aligned");
+  if (from->n_heads != c->n_heads || from->head_width != c->head_width || from->format != c->format || from->closed != c->closed)
+    return refuse("ad_kv8_copy: both caches must have the same heads, head width and format, and both grow or both be closed");
+  const Kv8Dims d = kv8_dims(*from), t = kv8_dims(*c);
+  if (origin == cache) {
+    if (d.n_seq != t.n_seq || d.capacity != t.capacity || d.k_max != t.k_max) return refuse("ad_kv8_copy: two descriptions of one cache");
+    if (begin) return refuse("ad_kv8_copy: within a cache sequences are copied from their first token on (begin must be null)");
+  } else if ((uintptr_t)origin < (uintptr_t)cache + t.bytes && (uintptr_t)cache < (uintptr_t)origin + d.bytes) {
+    return refuse("ad_kv8_copy: the caches overlap");
+  }
+  if (n < 0 || n > c->n_seq || max_tokens < 0) return refuse("ad_kv8_copy: n outside [0, n_seq] or max_tokens < 0");
+  if (n == 0 || max_tokens == 0) return AD_OK;
+  if (!source || !place || !end) return refuse("ad_kv8_copy: null buffer");
+  launch_kv8_copy(d, origin, t, cache, Kv8Moves{source, place, begin, end, n, max_tokens}, (hipStream_t)hip_stream);
+  return launched("ad_kv8_copy");
+}
+
 size_t ad_accept_sampled_bytes(int32_t n_seq, int32_t rows, int32_t vocab) {
   return n_seq < 1 || rows < 1 || vocab < 1 ? 0 : accept_bytes(n_seq, rows, vocab);
 }
@@ -138,6 +197,53 @@ int ad_accept_sampled(const void* logits, int32_t dtype, int64_t logits_stride, 
   a.vocab = vocab; a.n_seq = n_seq; a.rows = rows; a.max_rows = max_rows; a.n_accept = n_accept; a.tokens = tokens; a.keep = 0;
   launch_accept_sampled(dtype, a, workspace, (hipStream_t)hip_stream);
   return launched("ad_accept_sampled");
+}
+
+static int truncate_common(const char* what, const void* logits, int32_t dtype, int64_t stride, int32_t vocab, const int32_t* row_start, int32_t n_seq, int32_t rows) {
+  auto no = [&](const char* why) {
+    char msg[200];
+    snprintf(msg, sizeof(msg), "%s: %s", what, why);
+    return refuse(msg);
+  };
+  if (dtype != AD_F32 && dtype != AD_BF16) return no("dtype must be AD_F32 or AD_BF16");
+  if (vocab < 1 || vocab > (1 << 24)) return no("vocab outside [1, 2^24]");
+  if (rows < 0 || rows >= (1 << 22)) return no("rows outside [0, 2^22)");
+  if (row_start ? n_seq < 1 || n_seq > 4096 : n_seq != rows) return no("n_seq outside [1, 4096], or without row_start not the rows");
+  if (rows == 0) return AD_OK;
+  if (!logits) return no("null buffer");
+  if (stride < vocab) return no("row stride below vocab");
+  if ((uintptr_t)logits & (dtype == AD_F32 ? 3 : 1)) return no("scores not aligned to their type");
+  return AD_OK;
+}
+
+int ad_sample_tokens(const void* logits, int32_t dtype, int64_t logits_stride, int32_t vocab, const float* temperature, const int32_t* top_k, const float* top_p,
+                     const float* min_p, const int32_t* row_start, int32_t n_seq, const float* u, int32_t rows, int32_t* tokens, float* log_probs, void* hip_stream) {
+  const int rc = truncate_common("ad_sample_tokens", logits, dtype, logits_stride, vocab, row_start, n_seq, rows);
+  if (rc != AD_OK || rows == 0) return rc;
+  if (!u || !tokens) return refuse("ad_sample_tokens: null buffer");
+  TruncateArgs a{};
+  a.x = logits; a.stride = (size_t)logits_stride; a.vocab = vocab; a.n_seq = n_seq; a.rows = rows; a.row_start = row_start;
+  a.temperature = temperature; a.top_k = top_k; a.top_p = top_p; a.min_p = min_p; a.u = u; a.tokens = tokens; a.log_probs = log_probs;
+  launch_sample(dtype, a, (hipStream_t)hip_stream);
+  return launched("ad_sample_tokens");
+}
+
+int ad_truncate_scores(const void* logits, int32_t dtype, int64_t logits_stride, int32_t vocab, const float* temperature, const int32_t* top_k, const float* top_p,
+                       const float* min_p, const int32_t* row_start, int32_t n_seq, int32_t rows, void* out, int64_t out_stride, void* hip_stream) {
+  const int rc = truncate_common("ad_truncate_scores", logits, dtype, logits_stride, vocab, row_start, n_seq, rows);
+  if (rc != AD_OK || rows == 0) return rc;
+  if (!out) return refuse("ad_truncate_scores: null buffer");
+  if (out_stride < vocab) return refuse("ad_truncate_scores: row stride below vocab");
+  const size_t size = dtype == AD_F32 ? 4 : 2;
+  if ((uintptr_t)out & (size - 1)) return refuse("ad_truncate_scores: out not aligned to its type");
+  if (out == logits ? out_stride != logits_stride && rows > 1
+                    : (uintptr_t)out < (uintptr_t)logits + ((size_t)logits_stride * (rows - 1) + vocab) * size && (uintptr_t)logits < (uintptr_t)out + ((size_t)out_stride * (rows - 1) + vocab) * size)
+    return refuse("ad_truncate_scores: out must be the scores themselves, with their stride, or not overlap them");
+  TruncateArgs a{};
+  a.x = logits; a.stride = (size_t)logits_stride; a.vocab = vocab; a.n_seq = n_seq; a.rows = rows; a.row_start = row_start;
+  a.temperature = temperature; a.top_k = top_k; a.top_p = top_p; a.min_p = min_p; a.out = out; a.out_stride = (size_t)out_stride;
+  launch_truncate(dtype, a, (hipStream_t)hip_stream);
+  return launched("ad_truncate_scores");
 }
 
 }  // extern "C"

@@ -1,4 +1,5 @@
-"""The library's operators that need no context, over torch tensors: key/value caches in 8 bits and the acceptance of sampled blocks.
+"""The library's operators that need no context, over torch tensors: key/value caches in 8 bits, the acceptance of sampled blocks, and distributions cut by
+top-k, top-p and min-p.
 
 Argument marshalling only, as in `binding`.  Work goes to torch's current stream of the tensors' device; row tables are int32 tensors
 on that device, read when the kernels run, so the calls never wait and may be captured into graphs.  Workspaces come from torch's allocator
@@ -102,12 +103,17 @@ class Kv8Cache:
         self._scale = 1.0 / math.sqrt(head_width)
         self._need = {}
 
-    def _call(self, call):
+    def _used_on(self, stream):
+        if stream not in self._streams:   # (the allocator is to wait for that stream, too, before it gives the memory to others)
+            import torch
+            self.memory.record_stream(torch.cuda.current_stream(self.device))
+            self._streams.add(stream)
+
+    def _call(self, call, other=None):
         def on(stream):
-            if stream not in self._streams:   # (the allocator is to wait for that stream, too, before it gives the memory to others)
-                import torch
-                self.memory.record_stream(torch.cuda.current_stream(self.device))
-                self._streams.add(stream)
+            self._used_on(stream)
+            if other is not None:
+                other._used_on(stream)
             return call(stream)
         rc = _on(self.index, on)
         if rc:
@@ -183,6 +189,62 @@ class Kv8Cache:
         self._call(call)
         return out
 
+    def attend_shared(self, q, row_start, length, shared, seq_start, shared_length, max_rows=None, max_keys=None, max_shared_rows=None,
+                      max_shared_keys=None, scale=None, out=None):
+        """`attend` of rows whose sequences share texts: softmax over the text's tokens and the sequence's own up to the row, what texts hold being read once for all of
+        their sequences.  `shared`: a cache of the same heads and format (this one, too) with a text a sequence, the first shared_length[g] tokens of sequence g
+        (int32 [shared.n_seq]; of a growing cache whole blocks of 32, all in 8 bits).  Text g belongs to this cache's sequences seq_start[g] .. seq_start[g + 1] - 1 (int32 [shared.n_seq + 1],
+        ascending), which lie next to each other; sequences of no text see their own tokens alone.  Positions and `length` count a sequence's own tokens.  max_shared_rows:
+        at least the most rows of a text's sequences together (default: all); max_shared_keys: at least the longest text (default: the capacity)."""
+        import torch
+        c, i = self.cfg, self.index
+        if not isinstance(shared, Kv8Cache) or shared.index != i:
+            _refuse(f"shared must be a Kv8Cache on cuda:{i}")
+        heads = q.shape[1] if isinstance(q, torch.Tensor) and q.dim() == 3 else 0
+        qp, qs, rows = _rows(q, "q", i, self._bf16, heads, c.head_width)
+        start, at = _flat(row_start, "row_start", i, self._i32, self._start), _flat(length, "length", i, self._i32, self._len)
+        first, texts = _flat(seq_start, "seq_start", i, self._i32, shared._start), _flat(shared_length, "shared_length", i, self._i32, shared._len)
+        most = self._most(rows) if max_rows is None else _bound(max_rows, rows)
+        together = rows if max_shared_rows is None else min(_count("max_shared_rows", max_shared_rows), rows)
+        keys = c.capacity if max_keys is None else min(_count("max_keys", max_keys), c.capacity)
+        text_keys = shared.cfg.capacity if max_shared_keys is None else min(_count("max_shared_keys", max_shared_keys), shared.cfg.capacity)
+        scale = self._scale if scale is None else scale
+
+        def call(stream):
+            nonlocal out
+            if out is None:
+                out = torch.empty((rows, heads, c.head_width), dtype=self._bf16, device=self.device)
+            op, os, orows = _rows(out, "out", i, self._bf16, heads, c.head_width)
+            if orows != rows:
+                _refuse("out must have as many rows as q")
+            sizes = heads, rows, keys, text_keys, shared.cfg.n_seq, shared.cfg.capacity
+            need = self._need.get(sizes)
+            if need is None:
+                if len(self._need) >= 4096:
+                    self._need.clear()
+                need = self._need[sizes] = self.L.ad_kv8_attend_shared_bytes(self._cfg, shared._cfg, heads, rows, keys, text_keys)
+            # (held until the kernels are enqueued; whatever gets it from the allocator afterwards comes behind them on this stream)
+            ws = torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
+            return self.L.ad_kv8_attend_shared(self._cfg, self._at, shared._cfg, shared._at, qp, qs, heads, start, at, first, texts, rows, most, keys, together, text_keys,
+                                               scale, op, os, None if ws is None else ws.data_ptr(), need, stream)
+        self._call(call, shared)
+        return out
+
+    def copy(self, source, place, end, begin=None, origin=None, max_tokens=None):
+        """Sequences forked, moved together or taken over from another cache: the first end[i] tokens of sequence source[i] of `origin` (a cache of the same heads and format;
+        default: this one) become those of this cache's sequence place[i], as if all were read before any is written.  source, place, end: int32 [n] on the device.  `begin`
+        (int32 [n], multiples of 32, from another cache only): tokens begin[i] .. end[i] - 1 become the first ones.  end[i] is any length that the source may be taken back to.  Of
+        entries with one place the first counts; what lies outside the caches is left out.  `max_tokens`: at least the most tokens of an entry (default: the capacity)."""
+        i = self.index
+        if origin is not None and (not isinstance(origin, Kv8Cache) or origin.index != i):
+            _refuse(f"origin must be a Kv8Cache on cuda:{i}")
+        n = (source.shape[0],) if hasattr(source, "shape") and len(source.shape) == 1 else (-1,)
+        sp, pp, ep = (_flat(t, name, i, self._i32, n) for t, name in ((source, "source"), (place, "place"), (end, "end")))
+        bp = None if begin is None else _flat(begin, "begin", i, self._i32, n)
+        o = self if origin is None else origin
+        most = self.cfg.capacity if max_tokens is None else min(_count("max_tokens", max_tokens), self.cfg.capacity)
+        self._call(lambda stream: self.L.ad_kv8_copy(o._cfg, o._at, self._cfg, self._at, sp, pp, bp, ep, n[0], most, stream), origin)
+
 
 def accept_sampled(logits, draft, row_start, accept_u, pick_u, temperature=None, draft_probs=None, max_rows=None):
     """Verification of drafted tokens for sampled decoding (include/ad.h, "acceptance of sampled blocks"): (n_accept [n_seq], tokens [rows]).
@@ -227,3 +289,55 @@ def accept_sampled(logits, draft, row_start, accept_u, pick_u, temperature=None,
 @functools.lru_cache(maxsize=4096)
 def _accept_bytes(n_seq, rows, vocab):
     return B.lib().ad_accept_sampled_bytes(n_seq, rows, vocab)
+
+
+def _cut(logits, temperature, top_k, top_p, min_p, row_start):
+    """What sample_tokens and truncate_scores have in common: the call's arguments up to the number of sequences, the GPU and the rows."""
+    import torch
+    f32, i32 = torch.float32, torch.int32
+    if not isinstance(logits, torch.Tensor) or logits.dim() != 2 or logits.dtype not in (f32, torch.bfloat16) or not logits.is_cuda:
+        _refuse("logits must be a float32 or bfloat16 tensor [rows, vocab] on a GPU")
+    i, (rows, vocab), (stride, one) = logits.get_device(), logits.shape, logits.stride()
+    if vocab > 1 and one != 1:
+        _refuse("logits: a row's scores must lie side by side")
+    n_seq, start = rows, None
+    if row_start is not None:
+        n_seq = row_start.shape[0] - 1 if isinstance(row_start, torch.Tensor) and row_start.dim() == 1 else -1
+        start = _flat(row_start, "row_start", i, i32, (n_seq + 1,))
+    cut = [None if t is None else _flat(t, name, i, dtype, (n_seq,))
+           for t, name, dtype in ((temperature, "temperature", f32), (top_k, "top_k", i32), (top_p, "top_p", f32), (min_p, "min_p", f32))]
+    return (logits.data_ptr(), B.AD_F32 if logits.dtype is f32 else B.AD_BF16, stride if rows > 1 else vocab, vocab, *cut, start, n_seq), i, rows
+
+
+def sample_tokens(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, row_start=None, log_probs=False):
+    """Tokens drawn from truncated distributions by given random numbers (include/ad.h, "truncated distributions"): tokens [rows] int32, with log_probs=True also the
+    logarithms of their probabilities [rows] fp32.
+
+    logits [rows, vocab] fp32 or bf16 (rows may lie apart), u [rows] fp32 uniform in [0, 1).  temperature fp32, top_k int32, top_p fp32, min_p fp32: None or a tensor on the
+    device with a setting for each row, or with row_start [n_seq + 1] int32 for each sequence, whose rows are row_start[b] .. row_start[b + 1] - 1."""
+    import torch
+    args, i, rows = _cut(logits, temperature, top_k, top_p, min_p, row_start)
+    up = _flat(u, "u", i, torch.float32, (rows,))
+    tokens = torch.empty_like(u, dtype=torch.int32)
+    probs = torch.empty_like(u) if log_probs else None
+    rc = _on(i, lambda stream: B.lib().ad_sample_tokens(*args, up, rows, tokens.data_ptr(), None if probs is None else probs.data_ptr(), stream))
+    if rc:
+        B._check(rc)
+    return (tokens, probs) if log_probs else tokens
+
+
+def truncate_scores(logits, temperature=None, top_k=None, top_p=None, min_p=None, row_start=None, out=None):
+    """Scores without what top-k, top-p and min-p cut off: [rows, vocab] like logits, -inf in its place (include/ad.h, "truncated distributions").  With them as its logits, and the same
+    temperature, `accept_sampled` verifies drafts against the truncated distributions.  Arguments as sample_tokens'; `out`: a tensor like logits that does not overlap it, or logits itself."""
+    import torch
+    args, i, rows = _cut(logits, temperature, top_k, top_p, min_p, row_start)
+    vocab = logits.shape[1]
+    if out is None:
+        out = torch.empty((rows, vocab), dtype=logits.dtype, device=logits.device)
+    elif not isinstance(out, torch.Tensor) or out.dtype is not logits.dtype or out.shape != logits.shape or out.get_device() != i or (vocab > 1 and out.stride(1) != 1):
+        _refuse(f"out must be a {logits.dtype} tensor {[rows, vocab]} on cuda:{i}, a row's scores side by side")
+    stride = out.stride(0) if rows > 1 else vocab
+    rc = _on(i, lambda stream: B.lib().ad_truncate_scores(*args, rows, out.data_ptr(), stride, stream))
+    if rc:
+        B._check(rc)
+    return out
