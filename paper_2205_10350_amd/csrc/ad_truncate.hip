@@ -8,8 +8,10 @@
 // row sum to less than 2^63.  Whole sums are exact, so neither atomics nor the launch's shape change a border or a token, and p Z and u Z are compared exactly.  What rounding moves a border by,
 // 2^-S a token, is some 10^-12 of the sum at most: a drawn number falls there once in 10^8 draws.
 //
-// One workgroup a row.  A border is found by histograms: of all scores in steps of T / 16 below the maximum, then, of the step that holds it, of equal parts of the
-// floating point numbers between its least and its largest, until few enough are left to be ranked by comparing each with each, or all are equal and their indices decide.
+// One workgroup a row, which it keeps in LDS as far as it goes there.  A border is found by a histogram of the scores in steps of T / 28 below the maximum; what lies up to the bin that holds the
+// border is gathered, in its order, into a list in LDS, where everything else is done: of the bin that holds the border equal parts of the floating point numbers between its
+// least and its largest, until few enough are left to be ranked by comparing each with each, or all are equal and their indices decide.  With top_k no histogram of the row is needed: the
+// k-th largest of the largest scores of each thread's even and odd vectors bounds the border from below.  What does not go into the list is done the same way over the row.
 #include <hip/hip_runtime.h>
 #include <limits.h>
 #include <math.h>
@@ -33,6 +35,10 @@ template <int CTRL, int ROWS = 0xf> __device__ __forceinline__ u64 dpp_move_u64(
 __device__ __forceinline__ u64 lane_u64(u64 v, int lane) {
   return (u64)(unsigned)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (unsigned)__builtin_amdgcn_readlane((int)v, lane);
 }
+// what every lane has alike, told to the compiler
+__device__ __forceinline__ int alike(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ float alike(float v) { return __uint_as_float((unsigned)__builtin_amdgcn_readfirstlane((int)__float_as_uint(v))); }
+__device__ __forceinline__ u64 alike(u64 v) { return lane_u64(v, 0); }
 // sums over lanes up to this one
 __device__ __forceinline__ u64 wave_scan_u64(u64 v) {
   v += dpp_move_u64<0x111>(v);
@@ -68,7 +74,7 @@ __device__ __forceinline__ u64 ceil_part(float f, u64 z) {
 struct Border {
   float x;
   int i;
-  __device__ __forceinline__ bool holds(float v, int at) const { return (v > x) | ((v == x) & (at <= i)); }
+  __device__ __forceinline__ bool holds(float v, int at) const { return (int)(v > x) | ((int)(v == x) & (int)(at <= i)); }
 };
 
 // floats in their order as whole numbers, -0 as 0
@@ -79,40 +85,65 @@ __device__ __forceinline__ unsigned order_of(float v) {
 
 // A row's weights
 struct Weigh {
-  float m;
+  float m, half, step;  // half: of m; step: of the histograms, bins two units of the scores
   double rate, least;   // least: 2's exponent of min_p (-inf: none)
   int bits;             // S
+  const double* table;  // 2^(j / 32)
   __device__ __forceinline__ double power(float v) const { return ((double)v - (double)m) * rate; }   // (the difference is exact; at temperatures near 0 a rounded product would not do)
-  // 2^(t + S) for t <= 0 in whole numbers: 2^f, |f| <= 1/2, by its series to f^11 (7e-15 relative), the whole part straight into the exponent
+  // 2^(t + S) for t <= 0 in whole numbers: 2^f, |f| <= 1/64, by its series to f^4 (2e-12 relative), a table of the parts of 32, the whole part straight into the exponent
   __device__ __forceinline__ u64 of(double t) const {
-    const double c = fmax(t, -100.0), big = c + 6755399441055744.0, f = c - (big - 6755399441055744.0);
-    double p = 4.44553827187081149760e-10;   // ln(2)^k / k!, k = 11 .. 0
-    p = fma(p, f, 7.05491162080112332988e-9);
-    p = fma(p, f, 1.01780860092396997275e-7);
-    p = fma(p, f, 1.32154867901443094884e-6);
-    p = fma(p, f, 1.52527338040598402800e-5);
-    p = fma(p, f, 1.54035303933816099544e-4);
-    p = fma(p, f, 1.33335581464284434234e-3);
-    p = fma(p, f, 9.61812910762847716197e-3);
+    const double c = fmax(t, -100.0), big = c + 211106232532992.0, f = c - (big - 211106232532992.0);   // 1.5 * 2^47
+    double p = 9.61812910762847716197e-3;   // ln(2)^k / k!, k = 4 .. 0
     p = fma(p, f, 5.55041086648215799532e-2);
     p = fma(p, f, 2.40226506959100712334e-1);
     p = fma(p, f, 6.93147180559945309417e-1);
     p = fma(p, f, 1.0);
-    const long long b = __builtin_bit_cast(long long, p);
-    const unsigned hi = (unsigned)(b >> 32) + ((unsigned)(__builtin_bit_cast(long long, big) + bits) << 20);
+    const int n32 = (int)__builtin_bit_cast(long long, big);
+    const long long b = __builtin_bit_cast(long long, p * table[n32 & 31]);
+    const unsigned hi = (unsigned)(b >> 32) + ((unsigned)((n32 >> 5) + bits) << 20);
     const double w = __builtin_bit_cast(double, (long long)((u64)hi << 32 | (unsigned)b));   // <= 2^51
     const u64 n = __builtin_bit_cast(u64, w + 4503599627370496.0) & 0xfffffffffffffull;     // (to nearest)
     return t < -1074.0 ? 0 : n < 1 ? 1 : n;
   }
+  // The histogram's bin: 28 to a T, so that what falls into the last one lies 36.5 T or more below the maximum and weighs 1 or nothing.
+  // (by halves: the difference itself may be beyond fp32)
+  __device__ __forceinline__ float place(float v) const { return fmaf(v, -0.5f, half) * step; }
+  __device__ __forceinline__ int bin(float v) const { return (int)fminf(place(v), (float)(kBins - 1)); }
 };
 
-// A row's scores, 16 bytes at a time from the 16-byte boundary at or before the first: wave w of a workgroup has pieces (w per .. (w + 1) per - 1) of 64 vectors, a lane one of each
-template <typename T, int THREADS> struct TruncateRow {
-  static constexpr int kVec = 16 / (int)sizeof(T), kWaves = THREADS / 64;
+template <int THREADS> struct TruncateShared {
+  static constexpr int kMost = 2 * THREADS;   // scores of the list
+  u64 hist[kBins];
+  double table[32];
+  u64 part[THREADS / 64];
+  float lo[THREADS / 64], hi[THREADS / 64];
+  float list_x[kMost];   // in the row's order
+  int list_i[kMost];
+  float rank_x[kList];
+  int rank_i[kList];
+  u64 rank_w[kList];
+  u64 above;      // before the bin that holds the border
+  int bin, n;
+  Border border;
+  // what the waves before this one have of `part`, and all of them
+  __device__ __forceinline__ u64 before(u64& all) const {
+    const int lane = threadIdx.x & 63, wave = alike((int)(threadIdx.x >> 6));
+    const u64 own = lane < THREADS / 64 ? part[lane] : 0, up = wave_scan_u64(own);
+    all = lane_u64(up, 63);
+    return lane_u64(up - own, wave);
+  }
+};
+
+// A row's scores, 16 bytes at a time from the 16-byte boundary at or before the first: wave w of a workgroup has pieces (w per .. (w + 1) per - 1) of 64 vectors, a lane one of each.  The
+// first KEEP of a lane stay in LDS (where each lane reads only what it wrote).
+template <typename T, int THREADS, int KEEP> struct TruncateRow {
+  static constexpr int kVec = 16 / (int)sizeof(T);
   const T* x;
+  uint4* kept;
   int vocab, skew, per, first;   // per: vectors of a lane; first: this lane's first one
-  __device__ __forceinline__ TruncateRow(const TruncateArgs& a, int row) {
+  __device__ __forceinline__ TruncateRow(const TruncateArgs& a, int row, uint4* lds) {
     x = (const T*)a.x + (size_t)row * a.stride;
+    kept = lds + threadIdx.x;
     vocab = a.vocab;
     skew = (int)((uintptr_t)x & 15) / (int)sizeof(T);
     per = ((vocab + skew + kVec - 1) / kVec + THREADS - 1) / THREADS;
@@ -120,179 +151,284 @@ template <typename T, int THREADS> struct TruncateRow {
   }
   __device__ __forceinline__ int index(int c) const { return (first + 64 * c) * kVec - skew; }   // of vector c's first score
   __device__ __forceinline__ bool whole(int i) const { return i >= 0 && i + kVec <= vocab; }
-  // (-inf off the row)
-  __device__ __forceinline__ void load(int c, float (&v)[kVec]) const {
+  __device__ __forceinline__ uint4 fetch(int c) const {   // (-inf off the row)
     const int i = index(c);
-    if (whole(i)) {
-      const uint4 w = ldg16(x + i);
+    if (whole(i)) return ldg16(x + i);
+    // (an edge: score by score, each read where there is one)
+    auto one = [&](int e) -> unsigned {
+      const int at = min(max(i + e, 0), vocab - 1);
       if constexpr (sizeof(T) == 4) {
-        v[0] = __uint_as_float(w.x); v[1] = __uint_as_float(w.y); v[2] = __uint_as_float(w.z); v[3] = __uint_as_float(w.w);
+        const unsigned w = __float_as_uint(gload((const float*)x + at));
+        return at == i + e ? w : 0xff800000u;
       } else {
-        v[0] = __uint_as_float(w.x << 16); v[1] = __uint_as_float(w.x & 0xffff0000u); v[2] = __uint_as_float(w.y << 16); v[3] = __uint_as_float(w.y & 0xffff0000u);
-        v[4] = __uint_as_float(w.z << 16); v[5] = __uint_as_float(w.z & 0xffff0000u); v[6] = __uint_as_float(w.w << 16); v[7] = __uint_as_float(w.w & 0xffff0000u);
+        const unsigned w = gload((const bf16_t*)x + at);
+        return at == i + e ? w : 0xff80u;
       }
+    };
+    uint4 w;
+    if constexpr (sizeof(T) == 4) w = uint4{one(0), one(1), one(2), one(3)};
+    else w = uint4{one(0) | one(1) << 16, one(2) | one(3) << 16, one(4) | one(5) << 16, one(6) | one(7) << 16};
+    return w;
+  }
+  static __device__ __forceinline__ void unpack(const uint4& w, float (&v)[kVec]) {
+    if constexpr (sizeof(T) == 4) {
+      v[0] = __uint_as_float(w.x); v[1] = __uint_as_float(w.y); v[2] = __uint_as_float(w.z); v[3] = __uint_as_float(w.w);
     } else {
+      v[0] = __uint_as_float(w.x << 16); v[1] = __uint_as_float(w.x & 0xffff0000u); v[2] = __uint_as_float(w.y << 16); v[3] = __uint_as_float(w.y & 0xffff0000u);
+      v[4] = __uint_as_float(w.z << 16); v[5] = __uint_as_float(w.z & 0xffff0000u); v[6] = __uint_as_float(w.w << 16); v[7] = __uint_as_float(w.w & 0xffff0000u);
+    }
+  }
+  __device__ __forceinline__ uint4 again(int c) const { return c < KEEP ? kept[c * THREADS] : fetch(c); }
+  __device__ __forceinline__ void load(int c, float (&v)[kVec]) const { unpack(again(c), v); }
+  // the first time: f(scores) of each vector, eight on their way
+  template <typename F> __device__ __forceinline__ void take(const F& f) const {
+#pragma clang loop unroll(disable)
+    for (int c = 0; c < per; c += 8) {
+      uint4 w[8];
 #pragma unroll
-      for (int e = 0; e < kVec; ++e) v[e] = i + e >= 0 && i + e < vocab ? Store<T>::load(x + i + e) : -INFINITY;
+      for (int j = 0; j < 8; ++j)
+        if (c + j < per) w[j] = fetch(c + j);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if (c + j >= per) break;
+        if (c + j < KEEP) kept[(c + j) * THREADS] = w[j];
+        float v[kVec];
+        unpack(w[j], v);
+        f(v, j);
+      }
+    }
+  }
+  template <typename F> __device__ __forceinline__ void vectors(const F& f) const {   // f(vector, scores), the next two on their way
+    uint4 w = again(0), w1 = per > 1 ? again(1) : w;
+#pragma clang loop unroll(disable)
+    for (int c = 0; c < per; ++c) {
+      const uint4 w2 = c + 2 < per ? again(c + 2) : w1;
+      float v[kVec];
+      unpack(w, v);
+      f(c, v);
+      w = w1; w1 = w2;
     }
   }
   template <typename F> __device__ __forceinline__ void each(const F& f) const {   // f(score, index) over this thread's
-    for (int c = 0; c < per; ++c) {
-      float v[kVec];
-      load(c, v);
+    vectors([&](int c, const float (&v)[kVec]) {
 #pragma unroll
       for (int e = 0; e < kVec; ++e) f(v[e], index(c) + e);
-    }
+    });
   }
-};
-
-template <int THREADS> struct TruncateShared {
-  u64 hist[kBins];
-  u64 part[THREADS / 64];
-  float lo[THREADS / 64], hi[THREADS / 64];
-  float list_x[kList];
-  int list_i[kList];
-  u64 list_w[kList];
-  u64 above;      // before the bin that holds the border
-  int bin, n;
-  Border border;
-  float found_x;
-};
-
-// The least index whose f(score, index) up to it sum to want(sum of all) or more; thread by thread in the row's order, so the winning wave looks for it alone.  Left in
-// s.border: its score and index.
-template <typename T, int THREADS, typename F, typename W>
-__device__ __forceinline__ u64 truncate_find(TruncateShared<THREADS>& s, const TruncateRow<T, THREADS>& x, const F& f, const W& want) {
-  constexpr int kWaves = THREADS / 64, kVec = TruncateRow<T, THREADS>::kVec;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  u64 sum = 0;
-  x.each([&](float v, int i) { sum += f(v, i); });
-  sum = wave_sum_u64(sum);
-  __syncthreads();
-  if (lane == 0) s.part[wave] = sum;
-  __syncthreads();
-  u64 before = 0, all = 0;
+  // Weights of all, bin by bin; their sum goes with them.  What is in the last bin weighs 1 (or nothing) and is counted apart.
+  template <typename S> __device__ __forceinline__ void weigh_all(S& s, const Weigh& weigh) const {
+    unsigned tail = 0;
+    vectors([&](int, const float (&v)[kVec]) {
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    const u64 p = s.part[w];
-    if (w < wave) before += p;
-    all += p;
-  }
-  const u64 target = want(all);
-  if (before < target && before + sum >= target) {   // (one wave)
-    for (int c = 0; c < x.per; ++c) {
-      float v[kVec];
-      u64 e[kVec], own = 0;
-      x.load(c, v);
-#pragma unroll
-      for (int j = 0; j < kVec; ++j) { e[j] = f(v[j], x.index(c) + j); own += e[j]; }
-      const u64 up = wave_scan_u64(own), total = lane_u64(up, 63);
-      if (before + total < target) {
-        before += total;
-        continue;
+      for (int e = 0; e < kVec; ++e) {
+        const float at = weigh.place(v[e]);
+        if (at < (float)(kBins - 1)) atomicAdd(&s.hist[(int)at], weigh.of(weigh.power(v[e])));
+        else if (v[e] > -INFINITY) tail += weigh.power(v[e]) >= -1074.0;
       }
-      u64 at = before + up - own;
-      if (at < target && at + own >= target) {   // (one lane)
-#pragma unroll
-        for (int j = 0; j < kVec; ++j) {
-          if (at < target && at + e[j] >= target) s.border = Border{v[j], x.index(c) + j};
-          at += e[j];
-        }
-      }
-      break;
-    }
+    });
+    if (tail) atomicAdd(&s.hist[kBins - 1], (u64)tail);
   }
-  __syncthreads();
-  return all;
-}
-
-// The border of the least front of what `had` holds that sums to the target (its own part of it: `had` itself).  WEIGHTS: sums of weights, target part p of
-// all of them; else of ones, target k.
-template <bool WEIGHTS, typename T, int THREADS>
-__device__ __forceinline__ Border truncate_select(TruncateShared<THREADS>& s, const TruncateRow<T, THREADS>& x, const Weigh& weigh, const Border& had, float p, int k) {
-  constexpr int kWaves = THREADS / 64, kEach = kBins / THREADS;
-  const int t = threadIdx.x, wave = t >> 6, lane = t & 63;
-  auto one = [&](float v) -> u64 { return WEIGHTS ? weigh.of(weigh.power(v)) : 1; };
-  float lo = -INFINITY, hi = weigh.m;    // the scores among which the border lies
-  const float step = fminf(fmaxf((float)(weigh.rate * (16 * 0.69314718055994530942)), 1e-30f), 1e30f);
-  u64 above = 0, target = k;
-  for (bool top = true;; top = false) {
-    int shift = 0;
-    if (!top) shift = max(0, 32 - __clz(order_of(hi) - order_of(lo)) - 10);
-    auto bin_of = [&](float v) -> int {
-      return top ? (int)fminf((weigh.m - v) * step, (float)(kBins - 1)) : (int)((order_of(hi) - order_of(v)) >> shift);
-    };
-    auto here = [&](float v, int i) { return v >= lo && v <= hi && had.holds(v, i); };
-    __syncthreads();
+  // Those with pred(score) into the list, in their order, if they go there; how many there are.
+  template <typename S, typename P> __device__ __forceinline__ int gather(S& s, const P& pred) const {
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    int mine = 0;
+    u64 some = 0;   // vectors with one
+    vectors([&](int c, const float (&v)[kVec]) {
+      int n = 0;
 #pragma unroll
-    for (int j = 0; j < kEach; ++j) s.hist[t + j * THREADS] = 0;
-    if (t == 0) { s.n = 0; s.bin = -1; }
-    __syncthreads();
-    x.each([&](float v, int i) {
-      if (here(v, i)) atomicAdd(&s.hist[bin_of(v)], one(v));
+      for (int e = 0; e < kVec; ++e) n += __popcll(__ballot(pred(v[e])));
+      mine += n;
+      if (n) some |= (u64)1 << min(c, 63);
     });
     __syncthreads();
-    u64 own = 0;
-#pragma unroll
-    for (int j = 0; j < kEach; ++j) own += s.hist[t * kEach + j];
-    const u64 up = wave_scan_u64(own);
-    if (lane == 63) s.part[wave] = up;
+    if (lane == 0) s.part[wave] = mine;
     __syncthreads();
-    u64 at = above + up - own, all = 0;
+    u64 sum;
+    int at = (int)s.before(sum);
+    const int all = (int)sum;
+    if (all <= S::kMost) {
+#pragma clang loop unroll(disable)
+      for (int c = 0; c < per; ++c) {
+        if (!(some >> min(c, 63) & 1)) continue;
+        float v[kVec];
+        load(c, v);
+        int n = at;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      const u64 q = s.part[w];
-      if (w < wave) at += q;
-      all += q;
-    }
-    if (top) {
-      if constexpr (WEIGHTS) target = max(ceil_part(fmaxf(p, 0.f), all), (u64)1);
-      else if (all <= target) return had;   // (uniform: no more than k)
-    }
-    if (at < target && at + own >= target) {
-      for (int j = 0; j < kEach; ++j) {
-        const u64 h = s.hist[t * kEach + j];
-        if (at < target && at + h >= target) { s.bin = t * kEach + j; s.above = at; }
-        at += h;
+        for (int e = 0; e < kVec; ++e) {
+          const u64 b = __ballot(pred(v[e]));
+          n += __builtin_amdgcn_mbcnt_hi((unsigned)(b >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)b, 0));
+          at += __popcll(b);
+        }
+#pragma unroll
+        for (int e = 0; e < kVec; ++e)
+          if (pred(v[e])) { s.list_x[n] = v[e]; s.list_i[n] = index(c) + e; ++n; }
       }
     }
     __syncthreads();
-    const int bin = s.bin;
-    above = s.above;
+    return all;
+  }
+  // The least index whose f(score, index) up to it sum to want(sum of all) or more; the winning wave looks for it alone.  Left in s.border: its score and index.
+  template <typename S, typename F, typename W> __device__ __forceinline__ u64 find(S& s, const F& f, const W& want) const {
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    u64 sum = 0;
+    each([&](float v, int i) { sum += f(v, i); });
+    sum = wave_sum_u64(sum);
+    __syncthreads();
+    if (lane == 0) s.part[wave] = sum;
+    __syncthreads();
+    u64 all, before = s.before(all);
+    const u64 target = want(all);
+    if (before < target && before + sum >= target) {   // (one wave)
+#pragma clang loop unroll(disable)
+      for (int c = 0; c < per; ++c) {
+        float v[kVec];
+        u64 e[kVec], own = 0;
+        load(c, v);
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) { e[j] = f(v[j], index(c) + j); own += e[j]; }
+        const u64 up = wave_scan_u64(own), total = lane_u64(up, 63);
+        if (before + total < target) {
+          before += total;
+          continue;
+        }
+        u64 at = before + up - own;
+        if (at < target && at + own >= target) {   // (one lane)
+#pragma unroll
+          for (int j = 0; j < kVec; ++j) {
+            if (at < target && at + e[j] >= target) s.border = Border{v[j], index(c) + j};
+            at += e[j];
+          }
+        }
+        break;
+      }
+    }
+    __syncthreads();
+    return all;
+  }
+};
+
+// The same over the list, two scores a thread
+template <int THREADS> struct TruncateList {
+  float v[2];
+  int i[2];
+  __device__ __forceinline__ TruncateList(const TruncateShared<THREADS>& s, int n) {
+    const int t = threadIdx.x;
+    const float2 x = *(const float2*)&s.list_x[2 * t];
+    const int2 at = *(const int2*)&s.list_i[2 * t];
+    v[0] = 2 * t < n ? x.x : -INFINITY; v[1] = 2 * t + 1 < n ? x.y : -INFINITY;
+    i[0] = at.x; i[1] = at.y;
+  }
+  template <typename F> __device__ __forceinline__ void each(const F& f) const { f(v[0], i[0]); f(v[1], i[1]); }
+  template <typename S, typename F, typename W> __device__ __forceinline__ u64 find(S& s, const F& f, const W& want) const {
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const u64 e0 = f(v[0], i[0]), e1 = f(v[1], i[1]), up = wave_scan_u64(e0 + e1);
+    __syncthreads();
+    if (lane == 63) s.part[wave] = up;
+    __syncthreads();
+    u64 all, at = up - e0 - e1 + s.before(all);
+    const u64 target = want(all);
+    if (at < target && at + e0 + e1 >= target) s.border = at + e0 >= target ? Border{v[0], i[0]} : Border{v[1], i[1]};
+    __syncthreads();
+    return all;
+  }
+};
+
+template <int THREADS> __device__ __forceinline__ void truncate_clear(TruncateShared<THREADS>& s) {
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < kBins / THREADS; ++j) s.hist[threadIdx.x + j * THREADS] = 0;
+  if (threadIdx.x == 0) { s.n = 0; s.bin = -1; }
+  __syncthreads();
+}
+// The bin of the histogram where the sums from `above` on reach want(sum of all) (0: none does); left in s.bin and, what is before it, s.above.  The target.
+template <int THREADS, typename W> __device__ __forceinline__ u64 truncate_bin(TruncateShared<THREADS>& s, u64 above, const W& want) {
+  constexpr int kEach = kBins / THREADS;
+  const int t = threadIdx.x, wave = t >> 6, lane = t & 63;
+  __syncthreads();
+  u64 h[kEach], own = 0;
+#pragma unroll
+  for (int j = 0; j < kEach; ++j) own += h[j] = s.hist[t * kEach + j];
+  const u64 up = wave_scan_u64(own);
+  if (lane == 63) s.part[wave] = up;
+  __syncthreads();
+  u64 all, at = above + up - own + s.before(all);
+  const u64 target = want(all);
+  if (at < target && at + own >= target) {
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+      if (at < target && at + h[j] >= target) { s.bin = t * kEach + j; s.above = at; }
+      at += h[j];
+    }
+  }
+  __syncthreads();
+  return target;
+}
+
+// The border of the least front of what `had` holds that sums to the target, from the bin of the first histogram on that holds it.  Sums of weights, or of ones.
+template <int THREADS, typename X>
+__device__ __forceinline__ Border truncate_refine(TruncateShared<THREADS>& s, const X& x, const Weigh& weigh, bool weights, const Border& had, u64 target) {
+  const int t = threadIdx.x, wave = t >> 6, lane = t & 63;
+  auto one = [&](float v) -> u64 { return weights ? weigh.of(weigh.power(v)) : 1; };
+  float lo = -INFINITY, hi = weigh.m;    // the scores among which the border lies
+  int shift = -1;                        // below 0: the first histogram
+  auto bin_of = [&](float v) -> int { return shift < 0 ? weigh.bin(v) : (int)((order_of(hi) - order_of(v)) >> max(shift, 0)); };
+  auto here = [&](float v, int i) { return (int)(v >= lo) & (int)(v <= hi) & (int)had.holds(v, i); };
+#pragma clang loop unroll(disable)
+  for (;;) {
+    const int bin = alike(s.bin);
+    const u64 above = alike(s.above);
     // that bin's scores
     float least = INFINITY, most = -INFINITY;
     x.each([&](float v, int i) {
       if (here(v, i) && bin_of(v) == bin) {
         least = fminf(least, v); most = fmaxf(most, v);
         const int n = atomicAdd(&s.n, 1);
-        if (n < kList) { s.list_x[n] = v; s.list_i[n] = i; s.list_w[n] = one(v); }
+        if (n < kList) { s.rank_x[n] = v; s.rank_i[n] = i; s.rank_w[n] = one(v); }
       }
     });
     least = -wave_max(-least); most = wave_max(most);
     if (lane == 0) { s.lo[wave] = least; s.hi[wave] = most; }
     __syncthreads();
-    const int n = s.n;
+    const int n = alike(s.n);
     if (n <= kList) {
-      for (int r = t; r < n; r += THREADS) {
-        const float v = s.list_x[r];
-        const int i = s.list_i[r];
+      if (t < n) {
+        const Border b{s.rank_x[t], s.rank_i[t]};
+        const u64 w = s.rank_w[t];
         u64 up = above;
+#pragma clang loop unroll_count(4)
         for (int j = 0; j < n; ++j)
-          if (Border{v, i}.holds(s.list_x[j], s.list_i[j])) up += s.list_w[j];
-        if (up >= target && up - s.list_w[r] < target) s.border = Border{v, i};
+          if (b.holds(s.rank_x[j], s.rank_i[j])) up += s.rank_w[j];
+        if (up >= target && up - w < target) s.border = b;
       }
-      __syncthreads();
-      return s.border;
+      break;
     }
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) { least = fminf(least, s.lo[w]); most = fmaxf(most, s.hi[w]); }
-    lo = least; hi = most;
+    for (int w = 0; w < THREADS / 64; ++w) { least = fminf(least, s.lo[w]); most = fmaxf(most, s.hi[w]); }
+    lo = alike(least); hi = alike(most);
     if (lo == hi) {
-      const u64 each = one(lo), nth = (target - above + each - 1) / each;
-      truncate_find(s, x, [&](float v, int i) -> u64 { return v == lo && had.holds(v, i); }, [&](u64) { return nth; });
-      return s.border;
+      const u64 each = alike(one(lo)), nth = (target - above + each - 1) / each;
+      x.find(s, [&](float v, int i) -> u64 { return (int)(v == lo) & (int)had.holds(v, i); }, [&](u64) { return nth; });
+      break;
     }
+    shift = max(0, 32 - __clz(order_of(hi) - order_of(lo)) - 10);
+    truncate_clear(s);
+    x.each([&](float v, int i) {
+      if (here(v, i)) atomicAdd(&s.hist[bin_of(v)], one(v));
+    });
+    truncate_bin(s, above, [&](u64) { return target; });
   }
+  __syncthreads();
+  return Border{alike(s.border.x), alike(s.border.i)};
+}
+__device__ __forceinline__ u64 truncate_part(float p, u64 all) { return max(ceil_part(fmaxf(p, 0.f), all), (u64)1); }
+// The border of the first k of what `had` holds, or of its least front with part p of its weights.  k >= what x has: all of that.
+template <int THREADS, typename X>
+__device__ __forceinline__ Border truncate_select(TruncateShared<THREADS>& s, const X& x, const Weigh& weigh, bool weights, const Border& had, int k, float p) {
+  truncate_clear(s);
+  x.each([&](float v, int i) {
+    if (had.holds(v, i)) atomicAdd(&s.hist[weigh.bin(v)], weights ? weigh.of(weigh.power(v)) : (u64)1);
+  });
+  const u64 target = truncate_bin(s, 0, [&](u64 all) { return weights ? truncate_part(p, all) : min(all, (u64)k); });
+  return truncate_refine(s, x, weigh, weights, had, target);
 }
 
 // the sequence of packed row `row` (-1: none): the last one that starts there or before, found by each wave for itself: every 64th start at once, then those between two of them
@@ -306,35 +442,69 @@ __device__ __forceinline__ int truncate_owner(const TruncateArgs& a, int row) {
   return q >= 0 && a.row_start[q] <= row && row < a.row_start[q + 1] ? q : -1;
 }
 
-template <typename T, int THREADS, bool SAMPLE>
+template <typename T, int THREADS, int KEEP, bool SAMPLE>
 __global__ __launch_bounds__(THREADS) void k_truncate(TruncateArgs a) {
   __shared__ TruncateShared<THREADS> s;
-  constexpr int kWaves = THREADS / 64, kVec = 16 / (int)sizeof(T);
+  __shared__ uint4 kept[KEEP * THREADS];
+  using Row = TruncateRow<T, THREADS, KEEP>;
+  constexpr int kWaves = THREADS / 64, kVec = Row::kVec;
   const int row = blockIdx.x, t = threadIdx.x, wave = t >> 6, lane = t & 63;
   const int b = truncate_owner(a, row);
   if (b < 0) return;
-  const TruncateRow<T, THREADS> x(a, row);
+  const Row x(a, row, kept);
   const float temp = a.temperature ? a.temperature[b] : 1.f, top_p = a.top_p ? a.top_p[b] : 1.f, min_p = a.min_p ? a.min_p[b] : 0.f;
   const int top_k = a.top_k ? a.top_k[b] : 0;
-  float m = -INFINITY;
+  float most[2] = {-INFINITY, -INFINITY};   // of this thread's even and odd vectors
   bool bad = !(temp > 0.f && temp < INFINITY) || top_p != top_p || min_p != min_p;
-  x.each([&](float v, int) {
-    bad = bad || !(v < INFINITY);
-    m = fmaxf(m, v);
+  x.take([&](const float (&v)[kVec], int j) {
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) {
+      bad = bad || !(v[e] < INFINITY);
+      most[j & 1] = fmaxf(most[j & 1], v[e]);
+    }
   });
-  m = wave_max(m);
+  float m = wave_max(fmaxf(most[0], most[1]));
   if (lane == 0) s.hi[wave] = m;
+  if (t < 32) s.table[t] = exp2((double)t / 32);
   bad = __syncthreads_or(bad);
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) m = fmaxf(m, s.hi[w]);
   bad = bad || m == -INFINITY;   // no distribution
+  m = alike(m);
+  const double rate = 1.44269504088896340736 / (double)temp;
+  Weigh weigh{m, 0.5f * m, fminf((float)(rate * (56 * 0.69314718055994530942)), 1e30f), rate, -INFINITY, min(51, 62 - (32 - __clz(a.vocab))), s.table};
+  if (min_p > 0.f) weigh.least = log2((double)fminf(min_p, 1.f));
   Border border{bad ? INFINITY : -INFINITY, -1};
-  Weigh weigh{m, 1.44269504088896340736 / (double)temp, -INFINITY, min(51, 62 - (32 - __clz(a.vocab)))};
-  if (!bad) {
-    if (top_k > 0 && top_k < a.vocab) border = truncate_select<false>(s, x, weigh, border, 0.f, top_k);
-    if (top_p < 1.f) border = truncate_select<true>(s, x, weigh, border, top_p, 0);
-    if (min_p > 0.f) weigh.least = log2((double)fminf(min_p, 1.f));
+  constexpr int kMost = TruncateShared<THREADS>::kMost;
+  int n = INT_MAX;   // of the list, once that has all that stays
+  auto to_list = [&](float end) { n = alike(x.gather(s, [&](float v) { return weigh.place(v) < end; })); };
+#pragma clang loop unroll(disable)
+  for (int stage = 0; stage < 2; ++stage) {   // top_k, top_p
+    const bool weights = stage == 1, first = top_k > 0 && top_k < a.vocab;
+    if (bad || !(weights ? top_p < 1.f : first)) continue;
+    u64 target = 0;
+    if (!weights || !first) {   // (of the first k scores the list has all, or they do not go there)
+      truncate_clear(s);
+      if (weights) {
+        x.weigh_all(s, weigh);
+      } else if (top_k <= kMost) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+          if (most[j] > -INFINITY) atomicAdd(&s.hist[weigh.bin(most[j])], (u64)1);
+      }
+      target = alike(truncate_bin(s, 0, [&](u64 all) { return weights ? truncate_part(top_p, all) : all < (u64)top_k ? 0 : (u64)top_k; }));
+      const int bin = alike(s.bin);
+      if (target != 0 && bin < kBins - 1) to_list((float)(bin + 1));   // (the last bin's are not told from what is not there)
+      if (!weights) target = 0;
+    }
+    if (n <= kMost) {
+      const TruncateList<THREADS> list(s, n);
+      border = target != 0 ? truncate_refine(s, list, weigh, true, border, target) : truncate_select(s, list, weigh, weights, border, top_k, top_p);
+    } else {
+      border = target != 0 ? truncate_refine(s, x, weigh, true, border, target) : truncate_select(s, x, weigh, weights, border, top_k, top_p);
+    }
   }
+  if (SAMPLE && !bad && n == INT_MAX && border.i < 0 && min_p > 0.f) n = alike(x.gather(s, [&](float v) { return weigh.power(v) >= weigh.least; }));
   if constexpr (SAMPLE) {
     if (bad) {
       if (t == 0) {
@@ -344,14 +514,13 @@ __global__ __launch_bounds__(THREADS) void k_truncate(TruncateArgs a) {
       return;
     }
     const float u = a.u[row];
-    const u64 all = truncate_find(
-        s, x,
-        [&](float v, int i) -> u64 {
-          if (!border.holds(v, i)) return 0;
-          const double power = weigh.power(v);
-          return power >= weigh.least ? weigh.of(power) : 0;
-        },
-        [&](u64 z) { return !(u > 0.f) ? (u64)1 : u >= 1.f ? z : floor_part(u, z) + 1; });
+    auto stays = [&](float v, int i) -> u64 {
+      if (!border.holds(v, i)) return 0;
+      const double power = weigh.power(v);
+      return power >= weigh.least ? weigh.of(power) : 0;
+    };
+    auto want = [&](u64 z) { return !(u > 0.f) ? (u64)1 : u >= 1.f ? z : floor_part(u, z) + 1; };
+    const u64 all = n <= kMost ? TruncateList<THREADS>(s, n).find(s, stays, want) : x.find(s, stays, want);
     if (t == 0) {
       a.tokens[row] = s.border.i;
       if (a.log_probs) a.log_probs[row] = (float)((weigh.power(s.border.x) + (double)weigh.bits) * 0.69314718055994530942 - log((double)all));
@@ -359,39 +528,41 @@ __global__ __launch_bounds__(THREADS) void k_truncate(TruncateArgs a) {
   } else {
     T* out = (T*)a.out + (size_t)row * a.out_stride;
     const bool wide = (((uintptr_t)out ^ (uintptr_t)x.x) & 15) == 0;
-    for (int c = 0; c < x.per; ++c) {
-      float v[kVec];
-      x.load(c, v);
+    x.vectors([&](int c, const float (&v)[kVec]) {
       const int i = x.index(c);
+      unsigned w[kVec];
       // (selected without a branch: the compiler lost the -inf of a branch's other side)
 #pragma unroll
       for (int j = 0; j < kVec; ++j) {
-        const bool stays = border.holds(v[j], i + j) & (weigh.power(v[j]) >= weigh.least);
-        v[j] = __uint_as_float(stays ? __float_as_uint(v[j]) : 0xff800000u);
+        const int stays = (int)border.holds(v[j], i + j) & (int)(weigh.power(v[j]) >= weigh.least);
+        w[j] = stays ? __float_as_uint(v[j]) : 0xff800000u;
       }
       if (wide && x.whole(i)) {
-        uint4 w;
+        uint4 o;
         if constexpr (sizeof(T) == 4) {
-          w = uint4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+          o = uint4{w[0], w[1], w[2], w[3]};
         } else {   // (every value is a bf16 number)
-          auto two = [&](int j) { return __float_as_uint(v[j]) >> 16 | (__float_as_uint(v[j + 1]) & 0xffff0000u); };
-          w = uint4{two(0), two(2), two(4), two(6)};
+          auto two = [&](int j) { return w[j] >> 16 | w[j + 1]; };
+          o = uint4{two(0), two(2), two(4), two(6)};
         }
-        gstore((uint4*)(out + i), w);
+        gstore((uint4*)(out + i), o);
       } else {
 #pragma unroll
         for (int j = 0; j < kVec; ++j)
-          if (i + j >= 0 && i + j < a.vocab) Store<T>::store(out + i + j, v[j]);
+          if (i + j >= 0 && i + j < a.vocab) {
+            if constexpr (sizeof(T) == 4) gstore((unsigned*)out + i + j, w[j]);
+            else gstore((bf16_t*)out + i + j, (bf16_t)(w[j] >> 16));
+          }
       }
-    }
+    });
   }
 }
 
 template <bool SAMPLE> static void launch(int dtype, const TruncateArgs& a, hipStream_t s) {
   auto go = [&](auto type) {
     using T = decltype(type);
-    if (a.vocab <= 4096) k_truncate<T, 256, SAMPLE><<<a.rows, 256, 0, s>>>(a);
-    else k_truncate<T, 1024, SAMPLE><<<a.rows, 1024, 0, s>>>(a);
+    if (a.vocab <= 4096) k_truncate<T, 256, 4, SAMPLE><<<a.rows, 256, 0, s>>>(a);
+    else k_truncate<T, 1024, 8, SAMPLE><<<a.rows, 1024, 0, s>>>(a);
   };
   if (dtype == AD_BF16) go(bf16_t{});
   else go(float{});

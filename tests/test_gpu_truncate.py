@@ -112,6 +112,10 @@ def test_settings_at_their_ends():
     cut = dict(zip(("temperature", "top_k", "top_p", "min_p"), (f([g[i] for g in rows]) for i, f in enumerate((f32, i32, f32, f32)))))
     both(x, rng.random(n).astype(np.float32), rows, cut)
     both(x.to(torch.bfloat16), rng.random(n).astype(np.float32), rows, cut)
+    # temperatures as large and as small as the scores
+    x = torch.tensor(rng.standard_normal((8, vocab)) * np.array([1e38, 1e37, 1e32, 1e30, 1e-30, 1e-36, 1e-38, 1e-40])[:, None], dtype=torch.float32).cuda()
+    rows = [(t, 0, p, 0.0) for t, p in zip((3e38, 1e37, 1e32, 5e29, 1e-30, 1e-36, 1e-38, 1e-40), (0.9, 0.99, 1.0, 0.5, 0.9, 0.99, 0.9, 0.6))]
+    both(x, rng.random(8).astype(np.float32), rows, dict(temperature=f32([r[0] for r in rows]), top_p=f32([r[2] for r in rows])))
 
 
 @pytest.mark.parametrize("vocab", [40, 6000])
