@@ -83,6 +83,17 @@ __device__ __forceinline__ unsigned order_of(float v) {
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
+// 2^(j / 32)
+__device__ const double kPowers[32] = {
+    1.0, 1.0218971486541166, 1.0442737824274138, 1.0671404006768237,
+    1.0905077326652577, 1.1143867425958924, 1.1387886347566916, 1.1637248587775775,
+    1.189207115002721, 1.215247359980469, 1.241857812073484, 1.2690509571917332,
+    1.2968395546510096, 1.3252366431597413, 1.3542555469368927, 1.383909881963832,
+    1.4142135623730951, 1.4451808069770467, 1.4768261459394993, 1.5091644275934228,
+    1.5422108254079407, 1.5759808451078865, 1.6104903319492543, 1.645755478153965,
+    1.681792830507429, 1.718619298122478, 1.7562521603732995, 1.7947090750031072,
+    1.8340080864093424, 1.8741676341103, 1.9152065613971474, 1.9571441241754002};
+
 // A row's weights
 struct Weigh {
   float m, half, step;  // half: of m; step: of the histograms, bins two units of the scores
@@ -90,9 +101,9 @@ struct Weigh {
   int bits;             // S
   const double* table;  // 2^(j / 32)
   __device__ __forceinline__ double power(float v) const { return ((double)v - (double)m) * rate; }   // (the difference is exact; at temperatures near 0 a rounded product would not do)
-  // 2^(t + S) for t <= 0 in whole numbers: 2^f, |f| <= 1/64, by its series to f^4 (2e-12 relative), a table of the parts of 32, the whole part straight into the exponent
-  __device__ __forceinline__ u64 of(double t) const {
-    const double c = fmax(t, -100.0), big = c + 211106232532992.0, f = c - (big - 211106232532992.0);   // 1.5 * 2^47
+  // 2^(t + S) for -100 <= t <= 0 in whole numbers, 1 at least: 2^f, |f| <= 1/64, by its series to f^4 (2e-12 relative), a table of the parts of 32, the whole part straight into the exponent
+  __device__ __forceinline__ u64 near(double t) const {
+    const double big = t + 211106232532992.0, f = t - (big - 211106232532992.0);   // 1.5 * 2^47
     double p = 9.61812910762847716197e-3;   // ln(2)^k / k!, k = 4 .. 0
     p = fma(p, f, 5.55041086648215799532e-2);
     p = fma(p, f, 2.40226506959100712334e-1);
@@ -103,25 +114,26 @@ struct Weigh {
     const unsigned hi = (unsigned)(b >> 32) + ((unsigned)((n32 >> 5) + bits) << 20);
     const double w = __builtin_bit_cast(double, (long long)((u64)hi << 32 | (unsigned)b));   // <= 2^51
     const u64 n = __builtin_bit_cast(u64, w + 4503599627370496.0) & 0xfffffffffffffull;     // (to nearest)
-    return t < -1074.0 ? 0 : n < 1 ? 1 : n;
+    return n | (u64)(n == 0);
   }
+  __device__ __forceinline__ u64 of(double t) const { return t < -1074.0 ? 0 : near(fmax(t, -100.0)); }
   // The histogram's bin: 28 to a T, so that what falls into the last one lies 36.5 T or more below the maximum and weighs 1 or nothing.
   // (by halves: the difference itself may be beyond fp32)
   __device__ __forceinline__ float place(float v) const { return fmaf(v, -0.5f, half) * step; }
   __device__ __forceinline__ int bin(float v) const { return (int)fminf(place(v), (float)(kBins - 1)); }
 };
 
-template <int THREADS> struct TruncateShared {
-  static constexpr int kMost = 2 * THREADS;   // scores of the list
+template <int THREADS, int EACH> struct TruncateShared {
+  static constexpr int kMost = EACH * THREADS;   // scores of the list
   u64 hist[kBins];
   double table[32];
   u64 part[THREADS / 64];
   float lo[THREADS / 64], hi[THREADS / 64];
   float list_x[kMost];   // in the row's order
   int list_i[kMost];
-  float rank_x[kList];
-  int rank_i[kList];
-  u64 rank_w[kList];
+  uint4 rank[kList];     // score, index, weight
+  int order[kList];      // of the ranked: how many are before it,
+  u64 sum[kList];        // the weights up to it
   u64 above;      // before the bin that holds the border
   int bin, n;
   Border border;
@@ -222,7 +234,7 @@ template <typename T, int THREADS, int KEEP> struct TruncateRow {
 #pragma unroll
       for (int e = 0; e < kVec; ++e) {
         const float at = weigh.place(v[e]);
-        if (at < (float)(kBins - 1)) atomicAdd(&s.hist[(int)at], weigh.of(weigh.power(v[e])));
+        if (at < (float)(kBins - 1)) atomicAdd(&s.hist[(int)at], weigh.near(weigh.power(v[e])));
         else if (v[e] > -INFINITY) tail += weigh.power(v[e]) >= -1074.0;
       }
     });
@@ -236,12 +248,13 @@ template <typename T, int THREADS, int KEEP> struct TruncateRow {
     vectors([&](int c, const float (&v)[kVec]) {
       int n = 0;
 #pragma unroll
-      for (int e = 0; e < kVec; ++e) n += __popcll(__ballot(pred(v[e])));
+      for (int e = 0; e < kVec; ++e) n += pred(v[e]);
       mine += n;
-      if (n) some |= (u64)1 << min(c, 63);
+      if (__any(n)) some |= (u64)1 << min(c, 63);
     });
+    const u64 count = wave_sum_u64(mine);
     __syncthreads();
-    if (lane == 0) s.part[wave] = mine;
+    if (lane == 0) s.part[wave] = count;
     __syncthreads();
     u64 sum;
     int at = (int)s.before(sum);
@@ -307,33 +320,45 @@ template <typename T, int THREADS, int KEEP> struct TruncateRow {
   }
 };
 
-// The same over the list, two scores a thread
-template <int THREADS> struct TruncateList {
-  float v[2];
-  int i[2];
-  __device__ __forceinline__ TruncateList(const TruncateShared<THREADS>& s, int n) {
-    const int t = threadIdx.x;
-    const float2 x = *(const float2*)&s.list_x[2 * t];
-    const int2 at = *(const int2*)&s.list_i[2 * t];
-    v[0] = 2 * t < n ? x.x : -INFINITY; v[1] = 2 * t + 1 < n ? x.y : -INFINITY;
-    i[0] = at.x; i[1] = at.y;
+// The same over the list: wave w has its scores 64 EACH w .., a lane every 64th of them
+template <int THREADS, int EACH> struct TruncateList {
+  const TruncateShared<THREADS, EACH>& s;
+  int n, first, per;
+  __device__ __forceinline__ TruncateList(const TruncateShared<THREADS, EACH>& s, int n) : s(s), n(n), first((int)(threadIdx.x >> 6) * 64 * EACH + (int)(threadIdx.x & 63)) {
+    per = min(EACH, max(0, (n - alike(first) + 63) / 64));
   }
-  template <typename F> __device__ __forceinline__ void each(const F& f) const { f(v[0], i[0]); f(v[1], i[1]); }
+  __device__ __forceinline__ float at(int j) const { return first + 64 * j < n ? s.list_x[first + 64 * j] : -INFINITY; }
+  template <typename F> __device__ __forceinline__ void each(const F& f) const {
+#pragma clang loop unroll(disable)
+    for (int j = 0; j < per; ++j) f(at(j), s.list_i[first + 64 * j]);
+  }
   template <typename S, typename F, typename W> __device__ __forceinline__ u64 find(S& s, const F& f, const W& want) const {
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const u64 e0 = f(v[0], i[0]), e1 = f(v[1], i[1]), up = wave_scan_u64(e0 + e1);
+    u64 sum = 0;
+    each([&](float v, int i) { sum += f(v, i); });
+    sum = wave_sum_u64(sum);
     __syncthreads();
-    if (lane == 63) s.part[wave] = up;
+    if (lane == 0) s.part[wave] = sum;
     __syncthreads();
-    u64 all, at = up - e0 - e1 + s.before(all);
+    u64 all, before = s.before(all);
     const u64 target = want(all);
-    if (at < target && at + e0 + e1 >= target) s.border = at + e0 >= target ? Border{v[0], i[0]} : Border{v[1], i[1]};
+    if (before < target && before + sum >= target) {   // (one wave)
+#pragma clang loop unroll(disable)
+      for (int j = 0; j < per; ++j) {
+        const float v = at(j);
+        const int i = s.list_i[first + 64 * j];
+        const u64 own = f(v, i), up = wave_scan_u64(own);
+        if (before + up >= target && before + up - own < target) s.border = Border{v, i};
+        before += lane_u64(up, 63);
+        if (before >= target) break;
+      }
+    }
     __syncthreads();
     return all;
   }
 };
 
-template <int THREADS> __device__ __forceinline__ void truncate_clear(TruncateShared<THREADS>& s) {
+template <int THREADS, int EACH> __device__ __forceinline__ void truncate_clear(TruncateShared<THREADS, EACH>& s) {
   __syncthreads();
 #pragma unroll
   for (int j = 0; j < kBins / THREADS; ++j) s.hist[threadIdx.x + j * THREADS] = 0;
@@ -341,7 +366,7 @@ template <int THREADS> __device__ __forceinline__ void truncate_clear(TruncateSh
   __syncthreads();
 }
 // The bin of the histogram where the sums from `above` on reach want(sum of all) (0: none does); left in s.bin and, what is before it, s.above.  The target.
-template <int THREADS, typename W> __device__ __forceinline__ u64 truncate_bin(TruncateShared<THREADS>& s, u64 above, const W& want) {
+template <int THREADS, int EACH, typename W> __device__ __forceinline__ u64 truncate_bin(TruncateShared<THREADS, EACH>& s, u64 above, const W& want) {
   constexpr int kEach = kBins / THREADS;
   const int t = threadIdx.x, wave = t >> 6, lane = t & 63;
   __syncthreads();
@@ -364,9 +389,33 @@ template <int THREADS, typename W> __device__ __forceinline__ u64 truncate_bin(T
   return target;
 }
 
+// Ranks s.rank[0 .. n), n <= kList: how many come before each, and the sums of weights up to it, by all waves: each takes 64 of them and compares them with its share of all.
+template <int THREADS, int EACH> __device__ __forceinline__ void truncate_rank(TruncateShared<THREADS, EACH>& s, int n) {
+  const int t = threadIdx.x, lane = t & 63, wave = alike(t >> 6);
+  for (int i = t; i < n; i += THREADS) { s.order[i] = 0; s.sum[i] = 0; }
+  __syncthreads();
+  const int groups = (n + 63) / 64, shares = THREADS / 64 / groups, group = wave % groups, share = wave / groups, e = group * 64 + lane;
+  if (share < shares && e < n) {
+    const uint4 own = s.rank[e];
+    const Border b{__uint_as_float(own.x), (int)own.y};
+    int before = 0;
+    u64 up = 0;
+    const int end = (share + 1) * n / shares;
+#pragma clang loop unroll_count(4)
+    for (int j = share * n / shares; j < end; ++j) {
+      const uint4 r = s.rank[j];
+      if (b.holds(__uint_as_float(r.x), (int)r.y)) { ++before; up += (u64)r.w << 32 | r.z; }
+    }
+    atomicAdd(&s.order[e], before);   // (with itself)
+    atomicAdd(&s.sum[e], up);
+  }
+  __syncthreads();
+}
+__device__ __forceinline__ uint4 truncate_entry(float v, int i, u64 w) { return uint4{__float_as_uint(v), (unsigned)i, (unsigned)w, (unsigned)(w >> 32)}; }
+
 // The border of the least front of what `had` holds that sums to the target, from the bin of the first histogram on that holds it.  Sums of weights, or of ones.
-template <int THREADS, typename X>
-__device__ __forceinline__ Border truncate_refine(TruncateShared<THREADS>& s, const X& x, const Weigh& weigh, bool weights, const Border& had, u64 target) {
+template <int THREADS, int EACH, typename X>
+__device__ __forceinline__ Border truncate_refine(TruncateShared<THREADS, EACH>& s, const X& x, const Weigh& weigh, bool weights, const Border& had, u64 target) {
   const int t = threadIdx.x, wave = t >> 6, lane = t & 63;
   auto one = [&](float v) -> u64 { return weights ? weigh.of(weigh.power(v)) : 1; };
   float lo = -INFINITY, hi = weigh.m;    // the scores among which the border lies
@@ -383,7 +432,7 @@ __device__ __forceinline__ Border truncate_refine(TruncateShared<THREADS>& s, co
       if (here(v, i) && bin_of(v) == bin) {
         least = fminf(least, v); most = fmaxf(most, v);
         const int n = atomicAdd(&s.n, 1);
-        if (n < kList) { s.rank_x[n] = v; s.rank_i[n] = i; s.rank_w[n] = one(v); }
+        if (n < kList) s.rank[n] = truncate_entry(v, i, one(v));
       }
     });
     least = -wave_max(-least); most = wave_max(most);
@@ -391,14 +440,11 @@ __device__ __forceinline__ Border truncate_refine(TruncateShared<THREADS>& s, co
     __syncthreads();
     const int n = alike(s.n);
     if (n <= kList) {
+      truncate_rank(s, n);
       if (t < n) {
-        const Border b{s.rank_x[t], s.rank_i[t]};
-        const u64 w = s.rank_w[t];
-        u64 up = above;
-#pragma clang loop unroll_count(4)
-        for (int j = 0; j < n; ++j)
-          if (b.holds(s.rank_x[j], s.rank_i[j])) up += s.rank_w[j];
-        if (up >= target && up - w < target) s.border = b;
+        const uint4 r = s.rank[t];
+        const u64 up = above + s.sum[t];
+        if (up >= target && up - ((u64)r.w << 32 | r.z) < target) s.border = Border{__uint_as_float(r.x), (int)r.y};
       }
       break;
     }
@@ -421,8 +467,8 @@ __device__ __forceinline__ Border truncate_refine(TruncateShared<THREADS>& s, co
 }
 __device__ __forceinline__ u64 truncate_part(float p, u64 all) { return max(ceil_part(fmaxf(p, 0.f), all), (u64)1); }
 // The border of the first k of what `had` holds, or of its least front with part p of its weights.  k >= what x has: all of that.
-template <int THREADS, typename X>
-__device__ __forceinline__ Border truncate_select(TruncateShared<THREADS>& s, const X& x, const Weigh& weigh, bool weights, const Border& had, int k, float p) {
+template <int THREADS, int EACH, typename X>
+__device__ __forceinline__ Border truncate_select(TruncateShared<THREADS, EACH>& s, const X& x, const Weigh& weigh, bool weights, const Border& had, int k, float p) {
   truncate_clear(s);
   x.each([&](float v, int i) {
     if (had.holds(v, i)) atomicAdd(&s.hist[weigh.bin(v)], weights ? weigh.of(weigh.power(v)) : (u64)1);
@@ -442,10 +488,37 @@ __device__ __forceinline__ int truncate_owner(const TruncateArgs& a, int row) {
   return q >= 0 && a.row_start[q] <= row && row < a.row_start[q + 1] ? q : -1;
 }
 
-template <typename T, int THREADS, int KEEP, bool SAMPLE>
+// The border over a list of n <= kList scores, all at once: of the first k of them; of those, the front with `target` of the weights (0: with part p of theirs).
+template <int THREADS, int EACH>
+__device__ __forceinline__ Border truncate_short(TruncateShared<THREADS, EACH>& s, int n, const Weigh& weigh, int k, float p, u64 target) {
+  const int t = threadIdx.x;
+  if (t < n) {
+    const float v = s.list_x[t];
+    s.rank[t] = truncate_entry(v, s.list_i[t], weigh.of(weigh.power(v)));
+  }
+  truncate_rank(s, n);
+  k = min(k, n);
+  const bool mine = t < n;
+  const uint4 r = mine ? s.rank[t] : uint4{0, 0, 0, 0};
+  const int place = mine ? s.order[t] : INT_MAX;   // (from 1)
+  const u64 up = mine ? s.sum[t] : 0;
+  const Border b{__uint_as_float(r.x), (int)r.y};
+  if (place == k) { s.border = b; s.above = up; }
+  __syncthreads();
+  if (p >= 1.f) return Border{alike(s.border.x), alike(s.border.i)};
+  if (target == 0) target = truncate_part(p, alike(s.above));
+  __syncthreads();
+  if (place <= k && up >= target && up - ((u64)r.w << 32 | r.z) < target) s.border = b;
+  __syncthreads();
+  return Border{alike(s.border.x), alike(s.border.i)};
+}
+
+// KEEP: vectors of a lane that stay in LDS; EACH: scores of a thread that the list has room for
+template <typename T, int THREADS, int KEEP, int EACH, bool SAMPLE>
 __global__ __launch_bounds__(THREADS) void k_truncate(TruncateArgs a) {
-  __shared__ TruncateShared<THREADS> s;
-  __shared__ uint4 kept[KEEP * THREADS];
+  __shared__ TruncateShared<THREADS, EACH> s;
+  __shared__ uint4 kept[KEEP ? KEEP * THREADS : 1];
+  using List = TruncateList<THREADS, EACH>;
   using Row = TruncateRow<T, THREADS, KEEP>;
   constexpr int kWaves = THREADS / 64, kVec = Row::kVec;
   const int row = blockIdx.x, t = threadIdx.x, wave = t >> 6, lane = t & 63;
@@ -454,6 +527,8 @@ __global__ __launch_bounds__(THREADS) void k_truncate(TruncateArgs a) {
   const Row x(a, row, kept);
   const float temp = a.temperature ? a.temperature[b] : 1.f, top_p = a.top_p ? a.top_p[b] : 1.f, min_p = a.min_p ? a.min_p[b] : 0.f;
   const int top_k = a.top_k ? a.top_k[b] : 0;
+  const double rate = 1.44269504088896340736 / (double)temp;
+  if (t < 32) s.table[t] = kPowers[t];
   float most[2] = {-INFINITY, -INFINITY};   // of this thread's even and odd vectors
   bool bad = !(temp > 0.f && temp < INFINITY) || top_p != top_p || min_p != min_p;
   x.take([&](const float (&v)[kVec], int j) {
@@ -465,17 +540,15 @@ __global__ __launch_bounds__(THREADS) void k_truncate(TruncateArgs a) {
   });
   float m = wave_max(fmaxf(most[0], most[1]));
   if (lane == 0) s.hi[wave] = m;
-  if (t < 32) s.table[t] = exp2((double)t / 32);
   bad = __syncthreads_or(bad);
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) m = fmaxf(m, s.hi[w]);
   bad = bad || m == -INFINITY;   // no distribution
   m = alike(m);
-  const double rate = 1.44269504088896340736 / (double)temp;
   Weigh weigh{m, 0.5f * m, fminf((float)(rate * (56 * 0.69314718055994530942)), 1e30f), rate, -INFINITY, min(51, 62 - (32 - __clz(a.vocab))), s.table};
   if (min_p > 0.f) weigh.least = log2((double)fminf(min_p, 1.f));
   Border border{bad ? INFINITY : -INFINITY, -1};
-  constexpr int kMost = TruncateShared<THREADS>::kMost;
+  constexpr int kMost = EACH * THREADS;
   int n = INT_MAX;   // of the list, once that has all that stays
   auto to_list = [&](float end) { n = alike(x.gather(s, [&](float v) { return weigh.place(v) < end; })); };
 #pragma clang loop unroll(disable)
@@ -497,8 +570,12 @@ __global__ __launch_bounds__(THREADS) void k_truncate(TruncateArgs a) {
       if (target != 0 && bin < kBins - 1) to_list((float)(bin + 1));   // (the last bin's are not told from what is not there)
       if (!weights) target = 0;
     }
+    if (n <= kList) {
+      border = truncate_short(s, n, weigh, first ? top_k : INT_MAX, top_p, target);
+      break;   // (both at once)
+    }
     if (n <= kMost) {
-      const TruncateList<THREADS> list(s, n);
+      const List list(s, n);
       border = target != 0 ? truncate_refine(s, list, weigh, true, border, target) : truncate_select(s, list, weigh, weights, border, top_k, top_p);
     } else {
       border = target != 0 ? truncate_refine(s, x, weigh, true, border, target) : truncate_select(s, x, weigh, weights, border, top_k, top_p);
@@ -520,7 +597,7 @@ __global__ __launch_bounds__(THREADS) void k_truncate(TruncateArgs a) {
       return power >= weigh.least ? weigh.of(power) : 0;
     };
     auto want = [&](u64 z) { return !(u > 0.f) ? (u64)1 : u >= 1.f ? z : floor_part(u, z) + 1; };
-    const u64 all = n <= kMost ? TruncateList<THREADS>(s, n).find(s, stays, want) : x.find(s, stays, want);
+    const u64 all = n <= kMost ? List(s, n).find(s, stays, want) : x.find(s, stays, want);
     if (t == 0) {
       a.tokens[row] = s.border.i;
       if (a.log_probs) a.log_probs[row] = (float)((weigh.power(s.border.x) + (double)weigh.bits) * 0.69314718055994530942 - log((double)all));
@@ -561,8 +638,10 @@ __global__ __launch_bounds__(THREADS) void k_truncate(TruncateArgs a) {
 template <bool SAMPLE> static void launch(int dtype, const TruncateArgs& a, hipStream_t s) {
   auto go = [&](auto type) {
     using T = decltype(type);
-    if (a.vocab <= 4096) k_truncate<T, 256, 4, SAMPLE><<<a.rows, 256, 0, s>>>(a);
-    else k_truncate<T, 1024, 8, SAMPLE><<<a.rows, 1024, 0, s>>>(a);
+    constexpr int kVec = 16 / (int)sizeof(T);
+    if (a.vocab <= 1024 * kVec) k_truncate<T, 256, 4, 2, SAMPLE><<<a.rows, 256, 0, s>>>(a);
+    else if (a.vocab <= 10 * 1024 * kVec) k_truncate<T, 1024, 8, 2, SAMPLE><<<a.rows, 1024, 0, s>>>(a);
+    else k_truncate<T, 1024, 0, 16, SAMPLE><<<a.rows, 1024, 0, s>>>(a);
   };
   if (dtype == AD_BF16) go(bf16_t{});
   else go(float{});
