@@ -147,25 +147,14 @@ template <int DH> __device__ __forceinline__ void kv8_fetch(Kv8Bytes<DH>& x, con
   x.scale = scales[blk];
 }
 
-// The state of rows row0 .. last of a (sequence, head) over a split's blocks of this wave, two blocks on their way while one is worked on.
-template <int DH, int R, int FMT, bool CLOSED>
-__device__ __forceinline__ void kv8_wave(Kv8State<DH, R>& st, const unsigned char* cache, const Kv8Attend& a, const Kv8Dims& dm, const Kv8Seq& sq, size_t bh, int h,
-                                         int row0, int last, int own_lo, int own_hi, int blk0, int blk1, int wave) {
+// The rows row0 .. last of a (sequence, head) before their first key: queries (of a scale below 0 negated), nothing summed; pos: position of this lane's row (rows past the last one repeat it)
+template <int DH, int R>
+__device__ __forceinline__ void kv8_start(Kv8State<DH, R>& st, const Kv8Attend& a, const Kv8Seq& sq, int h, int row0, int last, int (&pos)[R]) {
   const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
-  const unsigned char* blocks = cache + bh * dm.blocks * (2 * kKv8Block * DH);
-  const float2* scales = (const float2*)(cache + dm.scales) + bh * dm.blocks;
-  const int whole = min(blk1, own_lo), end = min(blk1, own_hi);
-  int blk = blk0 + wave;
-  constexpr int kAhead = 2;
-  Kv8Bytes<DH> x[kAhead + 1];
-#pragma unroll
-  for (int n = 0; n < kAhead; ++n)
-    if (blk + 4 * n < whole) kv8_fetch(x[n], blocks, scales, blk + 4 * n, lane);
-  int pos[R];   // position of this lane's row (closed: the length; rows past the last one repeat it)
 #pragma unroll
   for (int rt = 0; rt < R; ++rt) {
     const int m = min(row0 + 16 * rt + r, last), i = m / a.group, hq = h * a.group + m % a.group;
-    pos[rt] = CLOSED ? sq.base : sq.base + i;
+    pos[rt] = sq.base + i;
     const bf16_t* qp = a.q + (size_t)(sq.row0 + i) * a.q_stride + (size_t)hq * DH + 8 * g;
 #pragma unroll
     for (int s = 0; s < DH / 32; ++s) {
@@ -179,6 +168,28 @@ __device__ __forceinline__ void kv8_wave(Kv8State<DH, R>& st, const unsigned cha
     for (int c = 0; c < DH / 16; ++c) st.o[rt][c] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   st.inf = kv8_inf();
+}
+
+// The state of rows row0 .. last of a (sequence, head) over a split's blocks of this wave, two blocks on their way while one is worked on.
+template <int DH, int R, int FMT, bool CLOSED>
+__device__ __forceinline__ void kv8_wave(Kv8State<DH, R>& st, const unsigned char* cache, const Kv8Attend& a, const Kv8Dims& dm, const Kv8Seq& sq, size_t bh, int h,
+                                         int row0, int last, int own_lo, int own_hi, int blk0, int blk1, int wave) {
+  const int lane = threadIdx.x & 63, g = lane >> 4;
+  const unsigned char* blocks = cache + bh * dm.blocks * (2 * kKv8Block * DH);
+  const float2* scales = (const float2*)(cache + dm.scales) + bh * dm.blocks;
+  const int whole = min(blk1, own_lo), end = min(blk1, own_hi);
+  int blk = blk0 + wave;
+  constexpr int kAhead = 2;
+  Kv8Bytes<DH> x[kAhead + 1];
+#pragma unroll
+  for (int n = 0; n < kAhead; ++n)
+    if (blk + 4 * n < whole) kv8_fetch(x[n], blocks, scales, blk + 4 * n, lane);
+  int pos[R];
+  kv8_start<DH, R>(st, a, sq, h, row0, last, pos);
+  if (CLOSED) {
+#pragma unroll
+    for (int rt = 0; rt < R; ++rt) pos[rt] = sq.base;
+  }
   const float scale = fabsf(a.scale);
   auto take = [&](auto mask, const Kv8Bytes<DH>& x, int blk) {
     auto kf = [&](int kt, int s) { return kv8_operand<FMT>(kt == 0 ? uint2{x.k[s].x, x.k[s].y} : uint2{x.k[s].z, x.k[s].w}, 1.f); };

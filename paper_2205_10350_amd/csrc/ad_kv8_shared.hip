@@ -4,6 +4,8 @@
 //   m = max(m1, m2), l = l1 2^(m1 - m) + l2 2^(m2 - m), o = (o1 2^(m1 - m) + o2 2^(m2 - m)) / l.
 // A text's part takes the rows of all of its continuations together, which lie next to each other, as the rows of one sequence over a closed cache: its keys are fetched once for 32
 // rows (of the query heads that share a head among them) instead of once for every continuation.  Both parts are one launch, cut into splits of the keys; a second joins the splits of a row, the text's first.
+// Where a text has 64 continuations (times the query heads that share a head) or more, a workgroup takes 128 of its rows, 32 a wave: all waves go over the same keys, whose operands they unpack
+// together, once, into LDS.  Else the waves take every fourth block of keys each for the same rows, as over one cache.
 // A row's sums depend on the caches' sizes, the query heads and the row's own tokens alone.
 #include <hip/hip_runtime.h>
 
@@ -48,29 +50,35 @@ template <typename F> __device__ __forceinline__ int shared_owner(int n, int at,
   return g;
 }
 
+// workgroup -> ((split, row tile), (sequence, head)), as in the attention over one cache; whether it has one
+template <typename O, typename F>
+__device__ __forceinline__ bool kv8_where(int at, const Kv8Deal& deal, int n_seq, int heads, const O& owner, const F& first, int& b, int& h, int& tile, int& split) {
+  if (deal.packed) {
+    const int rest = at / heads;
+    h = at % heads;
+    tile = rest % deal.pieces; split = rest / deal.pieces;
+    b = owner(tile);
+    if (b < 0) return false;
+    tile -= first(b);
+    return tile >= 0;
+  }
+  const int pairs = n_seq * heads, pair = at % pairs, rest = at / pairs;
+  tile = rest % deal.pieces; split = rest / deal.pieces;
+  b = pair / heads; h = pair % heads;
+  return true;
+}
+
 template <int DH, int FMT>
 __global__ __launch_bounds__(256, kv8_waves(DH, 2)) void k_kv8_attend_shared(const unsigned char* __restrict__ cache, Kv8Attend a, Kv8Dims dm, Kv8Shared sh, Kv8Dims ds) {
   __shared__ float Os[4][16 * (DH + 4)];
   __shared__ float Ms[4][16][2];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const bool text = blockIdx.x < sh.blocks;
-  const int at = text ? blockIdx.x : blockIdx.x - sh.blocks;
-  const Kv8Deal& deal = text ? sh.tiles : a.tiles;
-  // workgroup -> ((split, row tile), (sequence, head)), as in the attention over one cache
   int b, h, tile, split;
-  if (deal.packed) {
-    const int rest = at / dm.heads;
-    h = at % dm.heads;
-    tile = rest % deal.pieces; split = rest / deal.pieces;
-    b = text ? shared_owner(sh.texts.n, tile, [&](int g) { return shared_first(a.rows, sh.texts, sh.tiles, g); }) : kv8_owner(a.rows, a.tiles, tile);
-    if (b < 0) return;
-    tile -= text ? shared_first(a.rows, sh.texts, sh.tiles, b) : kv8_first(a.rows, a.tiles, b);
-    if (tile < 0) return;
-  } else {
-    const int pairs = (text ? sh.texts.n : a.rows.n_seq) * dm.heads, pair = at % pairs, rest = at / pairs;
-    tile = rest % deal.pieces; split = rest / deal.pieces;
-    b = pair / dm.heads; h = pair % dm.heads;
-  }
+  if (!kv8_where(text ? blockIdx.x : blockIdx.x - sh.blocks, text ? sh.tiles : a.tiles, text ? sh.texts.n : a.rows.n_seq, dm.heads,
+                 [&](int at) { return text ? shared_owner(sh.texts.n, at, [&](int g) { return shared_first(a.rows, sh.texts, sh.tiles, g); }) : kv8_owner(a.rows, a.tiles, at); },
+                 [&](int b) { return text ? shared_first(a.rows, sh.texts, sh.tiles, b) : kv8_first(a.rows, a.tiles, b); }, b, h, tile, split))
+    return;
   const Kv8Seq sq = text ? shared_seq(a.rows, sh.texts, b, ds) : kv8_seq(a.rows, b, dm.capacity);
   const int m_rows = sq.n * a.group, row0 = tile * 32;
   if (row0 >= m_rows) return;
@@ -88,6 +96,112 @@ __global__ __launch_bounds__(256, kv8_waves(DH, 2)) void k_kv8_attend_shared(con
   };
   if (last - row0 < 16) go(std::integral_constant<int, 1>{});
   else go(std::integral_constant<int, 2>{});
+}
+
+// A text's blocks blk0 .. blk1 - 1 for the rows row0 .. last of this wave (none: it only unpacks): one block after the other through LDS, where all waves put its operands, in the order that a wave
+// reads them in; kAhead blocks on their way from memory.
+template <int DH, int FMT>
+__device__ __forceinline__ void kv8_text(Kv8State<DH, 2>& st, uint4* lds, const unsigned char* blocks, const float2* scales, const Kv8Attend& a, int length, int blk0, int blk1, bool rows) {
+  constexpr int kOps = DH / 8, kMine = DH >= 64 ? DH / 64 : 1, kAhead = 3;   // operands of a block, 1 KB each; a thread's 16 bytes of a block's 2 DH / 32 chunks
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), g = lane >> 4;
+  const bool unpacks = DH >= 64 || wave < 2;
+  const float scale = fabsf(a.scale);
+  uint4 x[kAhead][kMine];
+  float2 sc[kAhead];
+  auto fetch = [&](int n, int blk) {
+    blk = min(blk, blk1 - 1);   // (past the last one: again, unused)
+    const unsigned char* p = blocks + (size_t)blk * (2 * kKv8Block * DH) + t * 16;
+    if (unpacks) {
+#pragma unroll
+      for (int j = 0; j < kMine; ++j) x[n][j] = ldg16(p + j * 4096);
+    }
+    sc[n] = scales[blk];
+  };
+#pragma unroll
+  for (int n = 0; n < kAhead; ++n) fetch(n, blk0 + n);
+  auto work = [&](int n, int blk) {
+    uint4* buf = lds + (blk & 1) * kOps * 64;
+    if (unpacks) {
+#pragma unroll
+      for (int j = 0; j < kMine; ++j) {
+        const int chunk = wave + 4 * j;
+        const float f = chunk >= DH / 32 ? sc[n].y : 1.f;   // (e4m3: the values' scale)
+        buf[(2 * chunk) * 64 + lane] = __builtin_bit_cast(uint4, kv8_operand<FMT>(uint2{x[n][j].x, x[n][j].y}, f));
+        buf[(2 * chunk + 1) * 64 + lane] = __builtin_bit_cast(uint4, kv8_operand<FMT>(uint2{x[n][j].z, x[n][j].w}, f));
+      }
+    }
+    const float2 now = sc[n];
+    fetch(n, blk + kAhead);
+    __syncthreads();   // (one a block: the other buffer's readers are past it)
+    if (!rows) return;
+    auto kf = [&](int kt, int s) { return __builtin_bit_cast(bf16x8, buf[(2 * s + kt) * 64 + lane]); };
+    auto vf = [&](int c) { return __builtin_bit_cast(bf16x8, buf[(DH / 16 + c) * 64 + lane]); };
+    if ((blk + 1) * kKv8Block <= length) {
+      kv8_block<DH, 2, false, FMT == AD_KV_I8>(st, kf, vf, now.x * scale, now.y, [](int) { return 0xffu; });
+    } else {
+      unsigned bits = 0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) bits |= (blk * kKv8Block + kv8_key(g, j) < length ? 1u : 0u) << j;
+      kv8_block<DH, 2, true, FMT == AD_KV_I8>(st, kf, vf, now.x * scale, now.y, [&](int) { return bits; });
+    }
+  };
+  for (int blk = blk0; blk < blk1; blk += kAhead) {
+#pragma unroll
+    for (int n = 0; n < kAhead; ++n) {
+      if (blk + n >= blk1) break;
+      work(n, blk + n);
+    }
+  }
+}
+
+// As k_kv8_attend_shared, with 128 rows of a text a workgroup and 16 of a sequence.
+template <int DH, int FMT>
+__global__ __launch_bounds__(256, DH == 128 ? 2 : 3) void k_kv8_attend_many(const unsigned char* __restrict__ cache, Kv8Attend a, Kv8Dims dm, Kv8Shared sh, Kv8Dims ds) {
+  constexpr int kStage = 2 * (DH / 8) * 64 * 16, kMerge = 4 * 16 * (DH + 4) * 4 + 4 * 16 * 2 * 4;
+  __shared__ __align__(16) unsigned char lds[kStage > kMerge ? kStage : kMerge];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (blockIdx.x >= sh.blocks) {
+    int b, h, tile, split;
+    if (!kv8_where(blockIdx.x - sh.blocks, a.tiles, a.rows.n_seq, dm.heads, [&](int at) { return kv8_owner(a.rows, a.tiles, at); }, [&](int b) { return kv8_first(a.rows, a.tiles, b); }, b, h, tile, split)) return;
+    const Kv8Seq sq = kv8_seq(a.rows, b, dm.capacity);
+    const int m_rows = sq.n * a.group, row0 = tile * 16;
+    if (row0 >= m_rows) return;
+    const int last = min(row0 + 16, m_rows) - 1, own_lo = (sq.base + row0 / a.group) / kKv8Block, own_hi = (sq.base + last / a.group) / kKv8Block;
+    const int blk0 = split * a.split_blocks, blk1 = blk0 + a.split_blocks;
+    if (blk0 >= own_hi + 1) return;
+    Kv8State<DH, 1> st;
+    kv8_wave<DH, 1, FMT, false>(st, cache, a, dm, sq, (size_t)b * dm.heads + h, h, row0, last, own_lo, own_hi, blk0, blk1, wave);
+    float(*Os)[16 * (DH + 4)] = (float(*)[16 * (DH + 4)])lds;
+    kv8_merge<DH, 1>(st, Os, (float(*)[16][2])(lds + 4 * 16 * (DH + 4) * 4), a, dm, sq, h, row0, last, sh.n_split + split, wave);
+    return;
+  }
+  int b, h, tile, split;
+  auto first = [&](int g) { return shared_first(a.rows, sh.texts, sh.tiles, g); };
+  if (!kv8_where(blockIdx.x, sh.tiles, sh.texts.n, dm.heads, [&](int at) { return shared_owner(sh.texts.n, at, first); }, first, b, h, tile, split)) return;
+  const Kv8Seq sq = shared_seq(a.rows, sh.texts, b, ds);
+  const int m_rows = sq.n * a.group, row0 = tile * 128 + wave * 32;
+  if (tile * 128 >= m_rows) return;
+  const int blk0 = split * sh.split_blocks, blk1 = min(blk0 + sh.split_blocks, (sq.base + kKv8Block - 1) / kKv8Block);
+  if (blk0 >= blk1) return;
+  const bool rows = row0 < m_rows;
+  const int last = min(row0 + 32, m_rows) - 1;
+  const size_t bh = (size_t)b * dm.heads + h;
+  Kv8State<DH, 2> st;
+  int pos[2];
+  kv8_start<DH, 2>(st, a, sq, h, rows ? row0 : m_rows - 1, rows ? last : m_rows - 1, pos);
+  kv8_text<DH, FMT>(st, (uint4*)lds, sh.cache + bh * ds.blocks * (2 * kKv8Block * DH), (const float2*)(sh.cache + ds.scales) + bh * ds.blocks, a, sq.base, blk0, blk1, rows);
+  if (!rows) return;
+  const int lane = threadIdx.x & 63, g = lane >> 4;
+#pragma unroll
+  for (int rt = 0; rt < 2; ++rt) {
+    const float l = kv8_rows_sum(st.l[rt]);
+    const int m = row0 + 16 * rt + (lane & 15);
+    if (m > last) continue;
+    const size_t at = ((size_t)(sq.row0 + m / a.group) * (dm.heads * a.group) + h * a.group + m % a.group) * a.n_split + split;
+#pragma unroll
+    for (int c = 0; c < DH / 16; ++c) gstore((f32x4*)(a.part_o + at * DH + 16 * c + 4 * g), st.o[rt][c]);
+    if (g == 0) gstore((float2*)(a.part_ml + at * 2), float2{st.m[rt], l});
+  }
 }
 
 // The splits of a (row, query head), a wave each: the text's, then the sequence's own.
@@ -118,11 +232,14 @@ __global__ __launch_bounds__(256) void k_kv8_join_shared(Kv8Attend a, Kv8Deal on
   gstore((uint2*)(a.out + (size_t)row * a.out_stride + (size_t)hq * DH + col), uint2{f2bf_pair(o.x * inv, o.y * inv), f2bf_pair(o.z * inv, o.w * inv)});
 }
 
-// Keys of a split of a text: by the caches' sizes and the query heads alone, so that a row's sums do not depend on a call.
+// What goes by the caches' sizes and the query heads alone, so that a row's sums do not depend on a call: whether a workgroup takes 128 rows of a text, and the keys of a split of it.
+static size_t text_fan(const Kv8Dims& d, const Kv8Dims& texts, int group) { return (size_t)((d.n_seq + texts.n_seq - 1) / texts.n_seq) * group; }
+static bool text_many(const Kv8Dims& d, const Kv8Dims& texts, int group) { return text_fan(d, texts, group) >= 64; }
 static int text_split_keys(const Kv8Dims& d, const Kv8Dims& texts, int group) {
-  const size_t rows = (size_t)((d.n_seq + texts.n_seq - 1) / texts.n_seq) * group, parts = (size_t)texts.n_seq * d.heads * ((rows + 31) / 32);
-  size_t keys = 512;
-  while (keys < 8192 && keys * 2048 < parts * texts.capacity) keys *= 2;
+  const bool many = text_many(d, texts, group);
+  const size_t rows = text_fan(d, texts, group) * (many ? 1 : std::min(d.k_max, 8)), parts = (size_t)texts.n_seq * d.heads * (many ? (rows + 127) / 128 : (rows + 31) / 32);
+  size_t keys = many ? 1024 : 512;
+  while (keys < 8192 && keys * 1024 < parts * texts.capacity) keys *= 2;
   return (int)keys;
 }
 static int splits(int capacity, int max_keys, int keys) { return (std::min(max_keys, capacity) + keys - 1) / keys; }
@@ -133,21 +250,22 @@ size_t kv8_attend_shared_bytes(const Kv8Dims& d, const Kv8Dims& texts, int q_hea
   const size_t n = own_splits(d, max_keys) + text_splits(d, texts, q_heads / d.heads, max_text_keys), parts = (size_t)rows * q_heads * n;
   return n == 1 ? 0 : ml_bytes(parts) + parts * d.width * 4;
 }
-static Kv8Deal tiles_of(const Kv8Rows& r, int group) { return kv8_deal(r, group, 5, 1, (((size_t)r.max_rows * group - 1) >> 5) + 1); }
+static Kv8Deal tiles_of(const Kv8Rows& r, int group, int shift) { return kv8_deal(r, group, shift, 1, (((size_t)r.max_rows * group - 1) >> shift) + 1); }   // of 2^shift rows
+static Kv8Deal own_tiles(const Kv8Rows& r, int group, bool many) { return tiles_of(r, group, many ? 4 : 5); }
 static size_t of_all(const Kv8Deal& d, size_t n_seq) { return d.packed ? d.pieces : d.pieces * n_seq; }
-static Kv8Deal text_tiles(const Kv8Rows& r, const Kv8Texts& x, int group) {
+static Kv8Deal text_tiles(const Kv8Rows& r, const Kv8Texts& x, int group, bool many) {
   Kv8Rows t = r;
   t.n_seq = x.n; t.max_rows = std::min(x.max_rows, r.rows);
-  return tiles_of(t, group);
+  return tiles_of(t, group, many ? 7 : 5);
 }
 static size_t text_blocks(const Kv8Dims& d, const Kv8Dims& texts, const Kv8Rows& r, const Kv8Texts& x, int group, int max_text_keys) {
-  return x.max_rows == 0 ? 0 : of_all(text_tiles(r, x, group), x.n) * d.heads * text_splits(d, texts, group, max_text_keys);
+  return x.max_rows == 0 ? 0 : of_all(text_tiles(r, x, group, text_many(d, texts, group)), x.n) * d.heads * text_splits(d, texts, group, max_text_keys);
 }
-static size_t own_blocks(const Kv8Dims& d, const Kv8Rows& r, int group, int max_keys) { return of_all(tiles_of(r, group), r.n_seq) * d.heads * own_splits(d, max_keys); }
+static size_t own_blocks(const Kv8Dims& d, const Kv8Rows& r, int group, bool many, int max_keys) { return of_all(own_tiles(r, group, many), r.n_seq) * d.heads * own_splits(d, max_keys); }
 // (a launch takes less than 2^32 lanes along x: 2^24 workgroups of 256)
 bool kv8_attend_shared_fits(const Kv8Dims& d, const Kv8Dims& texts, const Kv8Rows& r, const Kv8Texts& x, int q_heads, int max_keys, int max_text_keys) {
   const int group = q_heads / d.heads;
-  return text_blocks(d, texts, r, x, group, max_text_keys) + own_blocks(d, r, group, max_keys) < (1u << 24) && (size_t)kv8_deal(r, 1, 0, 0, r.max_rows).pieces * q_heads < (1u << 26);
+  return text_blocks(d, texts, r, x, group, max_text_keys) + own_blocks(d, r, group, text_many(d, texts, group), max_keys) < (1u << 24) && (size_t)kv8_deal(r, 1, 0, 0, r.max_rows).pieces * q_heads < (1u << 26);
 }
 
 void launch_kv8_attend_shared(const Kv8Dims& d, const void* cache, const Kv8Dims& texts, const void* text_cache, const void* q, size_t q_stride, void* out, size_t out_stride,
@@ -156,22 +274,24 @@ void launch_kv8_attend_shared(const Kv8Dims& d, const void* cache, const Kv8Dims
   a.q = (const bf16_t*)q; a.out = (bf16_t*)out; a.q_stride = q_stride; a.out_stride = out_stride;
   a.rows = r; a.group = q_heads / d.heads; a.scale = scale * kLog2e;
   a.split_blocks = kv8_split_keys(d) / kKv8Block;
-  a.tiles = tiles_of(r, a.group);
+  const bool many = text_many(d, texts, a.group);
+  a.tiles = own_tiles(r, a.group, many);
   Kv8Shared sh;
   sh.cache = (const unsigned char*)text_cache; sh.texts = x;
   sh.split_blocks = text_split_keys(d, texts, a.group) / kKv8Block;
   sh.n_split = text_splits(d, texts, a.group, max_text_keys);
-  sh.tiles = text_tiles(r, x, a.group);
+  sh.tiles = text_tiles(r, x, a.group, many);
   sh.blocks = (unsigned)text_blocks(d, texts, r, x, a.group, max_text_keys);
   a.n_split = sh.n_split + own_splits(d, max_keys);
   const size_t parts = (size_t)r.rows * q_heads * a.n_split;
   a.part_ml = (float*)ws;
   a.part_o = (float*)((char*)ws + ml_bytes(parts));
-  const unsigned blocks = sh.blocks + (unsigned)own_blocks(d, r, a.group, max_keys);
+  const unsigned blocks = sh.blocks + (unsigned)own_blocks(d, r, a.group, many, max_keys);
   const Kv8Deal one = kv8_deal(r, 1, 0, 0, r.max_rows);
   const dim3 rows((unsigned)(((size_t)one.pieces * q_heads + 3) / 4), one.packed ? 1 : r.n_seq);
   kv8_dispatch(d, [&](auto width, auto fmt) {
-    k_kv8_attend_shared<width.value, fmt.value><<<blocks, 256, 0, s>>>((const unsigned char*)cache, a, d, sh, texts);
+    if (many) k_kv8_attend_many<width.value, fmt.value><<<blocks, 256, 0, s>>>((const unsigned char*)cache, a, d, sh, texts);
+    else k_kv8_attend_shared<width.value, fmt.value><<<blocks, 256, 0, s>>>((const unsigned char*)cache, a, d, sh, texts);
     if (a.n_split > 1) k_kv8_join_shared<width.value><<<rows, 256, 0, s>>>(a, one, d, sh, texts);
   });
 }

@@ -11,7 +11,7 @@
 // One workgroup a row, which it keeps in LDS as far as it goes there.  A border is found by a histogram of the scores in steps of T / 28 below the maximum; what lies up to the bin that holds the
 // border is gathered, in its order, into a list in LDS, where everything else is done: of the bin that holds the border equal parts of the floating point numbers between its
 // least and its largest, until few enough are left to be ranked by comparing each with each, or all are equal and their indices decide.  With top_k no histogram of the row is needed: the
-// k-th largest of the largest scores of each thread's even and odd vectors bounds the border from below.  What does not go into the list is done the same way over the row.
+// k-th largest of the largest scores of 2048 parts of the row bounds the border from below.  What does not go into the list is done the same way over the row.
 #include <hip/hip_runtime.h>
 #include <limits.h>
 #include <math.h>
@@ -529,16 +529,22 @@ __global__ __launch_bounds__(THREADS) void k_truncate(TruncateArgs a) {
   const int top_k = a.top_k ? a.top_k[b] : 0;
   const double rate = 1.44269504088896340736 / (double)temp;
   if (t < 32) s.table[t] = kPowers[t];
-  float most[2] = {-INFINITY, -INFINITY};   // of this thread's even and odd vectors
+  constexpr int kLargest = THREADS >= 1024 ? 2 : THREADS >= 512 ? 4 : 8;
+  float most[kLargest];   // of every kLargest-th of this thread's vectors
+#pragma unroll
+  for (int j = 0; j < kLargest; ++j) most[j] = -INFINITY;
   bool bad = !(temp > 0.f && temp < INFINITY) || top_p != top_p || min_p != min_p;
   x.take([&](const float (&v)[kVec], int j) {
 #pragma unroll
     for (int e = 0; e < kVec; ++e) {
       bad = bad || !(v[e] < INFINITY);
-      most[j & 1] = fmaxf(most[j & 1], v[e]);
+      most[j % kLargest] = fmaxf(most[j % kLargest], v[e]);
     }
   });
-  float m = wave_max(fmaxf(most[0], most[1]));
+  float m = most[0];
+#pragma unroll
+  for (int j = 1; j < kLargest; ++j) m = fmaxf(m, most[j]);
+  m = wave_max(m);
   if (lane == 0) s.hi[wave] = m;
   bad = __syncthreads_or(bad);
 #pragma unroll
@@ -562,7 +568,7 @@ __global__ __launch_bounds__(THREADS) void k_truncate(TruncateArgs a) {
         x.weigh_all(s, weigh);
       } else if (top_k <= kMost) {
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+        for (int j = 0; j < kLargest; ++j)
           if (most[j] > -INFINITY) atomicAdd(&s.hist[weigh.bin(most[j])], (u64)1);
       }
       target = alike(truncate_bin(s, 0, [&](u64 all) { return weights ? truncate_part(top_p, all) : all < (u64)top_k ? 0 : (u64)top_k; }));

@@ -283,6 +283,12 @@ CASES = [
     ("i8", 128, 2, 10, [3], [1056], [40, 0, 600], [2, 7, 1], False),
     ("e4m3", 64, 1, 16, [1, 1], [2112, 32], [0, 0], [3, 1], False),
     ("e4m3", 64, 1, 2, [40], [544], list(range(40)), [1] * 39 + [5], False),
+    # (64 or more rows of a head to a text: workgroups of 128 rows)
+    ("i8", 128, 1, 16, [6, 5], [1300, 40], [0, 70, 3, 31, 32, 33, 5, 9, 64, 1, 100], [1, 2, 9, 1, 3, 1, 1, 20, 1, 1, 4], True),
+    ("e4m3", 128, 2, 32, [5], [2144], [7, 0, 40, 1, 90], [3, 1, 1, 8, 1], False),
+    ("e4m3", 32, 2, 64, [1, 0, 5], [33, 64, 3001], [0, 9, 31, 500, 2, 64], [2, 1, 3, 1, 1, 5], True),
+    ("i8", 32, 1, 64, [2, 1], [1088, 0], [0, 35, 8], [5, 1, 2], False),
+    ("i8", 64, 2, 128, [2, 1], [1500, 31], [0, 35, 8], [3, 1, 2], True),
 ]
 
 
