@@ -4,9 +4,14 @@
 //   m = max(m1, m2), l = l1 2^(m1 - m) + l2 2^(m2 - m), o = (o1 2^(m1 - m) + o2 2^(m2 - m)) / l.
 // A text's part takes the rows of all of its continuations together, which lie next to each other, as the rows of one sequence over a closed cache: its keys are fetched once for 32
 // rows (of the query heads that share a head among them) instead of once for every continuation.  Both parts are one launch, cut into splits of the keys; a second joins the splits of a row, the text's first.
-// Where a text has 64 continuations (times the query heads that share a head) or more, a workgroup takes 128 of its rows, 32 a wave: all waves go over the same keys, whose operands they unpack
+// Where a text has 32 continuations (times the query heads that share a head) or more, a workgroup takes 128 of its rows, 32 a wave: all waves go over the same keys, whose operands they unpack
 // together, once, into LDS.  Else the waves take every fourth block of keys each for the same rows, as over one cache.
 // A row's sums depend on the caches' sizes, the query heads and the row's own tokens alone.
+//
+// Four texts of 8000 tokens, 16 heads of width 64, e4m3, us a replay with a workgroup of 32 rows / of 128, by continuations of each and rows of a continuation: 4 x 1 21.5 / 27.9, 10 x 1 21.4 / 28.3,
+// 10 x 8 34.7 / 37.1, 16 x 1 23.0 / 29.2, 16 x 8 46.0 / 43.5, 32 x 1 34.9 / 30.5, 32 x 8 79.9 / 69.5, 64 x 1 56.0 / 44.8, 64 x 25 382 / 376 (210 GFLOP, 560 TFLOP/s); in i8 32 x 8 95.7 / 78.8.
+// What bounds it with many rows: vector instructions, 176 (32 of them exponentials, at a quarter of the rate) for 36 matrix instructions over 32 rows and 64 keys, busy two thirds of the time; the
+// partial results of the splits (one text of 8192 tokens, 96 continuations of 8 rows: 27 MB written and read, 11 us of 58 for the join).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -98,66 +103,142 @@ __global__ __launch_bounds__(256, kv8_waves(DH, 2)) void k_kv8_attend_shared(con
   else go(std::integral_constant<int, 2>{});
 }
 
-// A text's blocks blk0 .. blk1 - 1 for the rows row0 .. last of this wave (none: it only unpacks): one block after the other through LDS, where all waves put its operands, in the order that a wave
-// reads them in; kAhead blocks on their way from memory.
+// kv8_block of NB blocks at once, half the reductions and looks at the reference where there are two.  f[j]: block j's operands in LDS; c1, cv: its scales, of the keys times that of the scores and of
+// the values (VSCALE); bits: of the eight keys of this lane that rows see (MASK; all see the same).  The denominator of e4m3 is a product of the rounded probabilities with ones, l[rt][0] the
+// whole row's; of i8, whose values' scale is in the rounded ones, this lane's part in st.l.
+template <int DH, int NB, bool MASK, bool VSCALE>
+__device__ __forceinline__ void kv8_text_blocks(Kv8State<DH, 2>& st, f32x4 (&l)[2], const uint4* const (&f)[NB], const float (&c1)[NB], const float (&cv)[NB], unsigned bits) {
+  const int lane = threadIdx.x & 63;
+  auto of = [&](int j, int op) { return __builtin_bit_cast(bf16x8, f[j][op * 64 + lane]); };
+  f32x4 sc[2][2 * NB];   // [row tile][16 keys]
+#pragma unroll
+  for (int kt = 0; kt < 2 * NB; ++kt) {
+#pragma unroll
+    for (int rt = 0; rt < 2; ++rt) sc[rt][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int s = 0; s < DH / 32; ++s) {
+      const bf16x8 a = of(kt / 2, 2 * s + kt % 2);
+#pragma unroll
+      for (int rt = 0; rt < 2; ++rt) sc[rt][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, st.q[rt][s], sc[rt][kt], 0, 0, 0);
+    }
+  }
+  bf16x8 pf[NB][2];   // [block][row tile]
+#pragma unroll
+  for (int rt = 0; rt < 2; ++rt) {
+    auto larger = [&](float a, float b) { return kv8_max(a, b, st.inf); };
+    auto score = [&](int j, int i) { return !MASK || ((bits >> i) & 1) ? sc[rt][2 * j + (i >> 2)][i & 3] : -INFINITY; };
+    auto most = [&](int j) {
+      return larger(larger(larger(score(j, 0), score(j, 1)), larger(score(j, 2), score(j, 3))), larger(larger(score(j, 4), score(j, 5)), larger(score(j, 6), score(j, 7)))) * c1[j];
+    };
+    float top = most(0);
+    if constexpr (NB == 2) top = larger(top, most(1));
+    top = kv8_rows_max(top, st.inf);
+    const bool step = top > st.m[rt] + kStep;
+    if (__builtin_expect(__any(step), 0)) {
+      const float to = step ? top : st.m[rt];
+      const float by = __builtin_amdgcn_exp2f(st.m[rt] - (to == -INFINITY ? 0.f : to));
+      st.m[rt] = to;
+      if constexpr (VSCALE) st.l[rt] *= by;
+      else l[rt][0] *= by;
+#pragma unroll
+      for (int c = 0; c < DH / 16; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) st.o[rt][c][i] *= by;
+    }
+    const float off = st.m[rt] == -INFINITY ? 0.f : st.m[rt];
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+      float x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = !MASK || ((bits >> i) & 1) ? __builtin_amdgcn_exp2f(fmaf(sc[rt][2 * j + (i >> 2)][i & 3], c1[j], -off)) : 0.f;
+      if constexpr (VSCALE) {
+        st.l[rt] += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] *= cv[j];
+      }
+      pf[j][rt] = __builtin_bit_cast(bf16x8, uint4{f2bf_pair(x[0], x[1]), f2bf_pair(x[2], x[3]), f2bf_pair(x[4], x[5]), f2bf_pair(x[6], x[7])});   // (roundings as kv8_block's)
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < NB; ++j) {
+    if constexpr (!VSCALE) {
+      const bf16x8 ones = __builtin_bit_cast(bf16x8, uint4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
+#pragma unroll
+      for (int rt = 0; rt < 2; ++rt) l[rt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[j][rt], l[rt], 0, 0, 0);
+    }
+#pragma unroll
+    for (int c = 0; c < DH / 16; ++c) {
+      const bf16x8 a = of(j, DH / 16 + c);
+#pragma unroll
+      for (int rt = 0; rt < 2; ++rt) st.o[rt][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, pf[j][rt], st.o[rt][c], 0, 0, 0);
+    }
+  }
+}
+
+// A text's blocks blk0 .. blk1 - 1 for the rows of this wave (none: it only unpacks): two blocks after the other through LDS, where all waves put their operands, in the order that a wave
+// reads them in; the next two are on their way from memory.
 template <int DH, int FMT>
-__device__ __forceinline__ void kv8_text(Kv8State<DH, 2>& st, uint4* lds, const unsigned char* blocks, const float2* scales, const Kv8Attend& a, int length, int blk0, int blk1, bool rows) {
-  constexpr int kOps = DH / 8, kMine = DH >= 64 ? DH / 64 : 1, kAhead = 3;   // operands of a block, 1 KB each; a thread's 16 bytes of a block's 2 DH / 32 chunks
+__device__ __forceinline__ void kv8_text(Kv8State<DH, 2>& st, f32x4 (&l)[2], uint4* lds, const unsigned char* blocks, const float2* scales, float scale, int length, int blk0, int blk1, bool rows) {
+  constexpr int kOps = DH / 8, kMine = DH >= 64 ? DH / 64 : 1;   // operands of a block, 1 KB each; a thread's 16 bytes of a block's 2 DH / 32 chunks
+  constexpr bool kV = FMT == AD_KV_I8;
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), g = lane >> 4;
   const bool unpacks = DH >= 64 || wave < 2;
-  const float scale = fabsf(a.scale);
-  uint4 x[kAhead][kMine];
-  float2 sc[kAhead];
-  auto fetch = [&](int n, int blk) {
-    blk = min(blk, blk1 - 1);   // (past the last one: again, unused)
-    const unsigned char* p = blocks + (size_t)blk * (2 * kKv8Block * DH) + t * 16;
-    if (unpacks) {
+  uint4 x[2][kMine];
+  float2 sc[2];
+  float c1[2], cv[2];
+  auto fetch = [&](int blk) {
 #pragma unroll
-      for (int j = 0; j < kMine; ++j) x[n][j] = ldg16(p + j * 4096);
-    }
-    sc[n] = scales[blk];
-  };
+    for (int n = 0; n < 2; ++n) {
+      const int at = min(blk + n, blk1 - 1);   // (past the last one: again, unused)
+      const unsigned char* p = blocks + (size_t)at * (2 * kKv8Block * DH) + t * 16;
+      if (unpacks) {
 #pragma unroll
-  for (int n = 0; n < kAhead; ++n) fetch(n, blk0 + n);
-  auto work = [&](int n, int blk) {
-    uint4* buf = lds + (blk & 1) * kOps * 64;
-    if (unpacks) {
-#pragma unroll
-      for (int j = 0; j < kMine; ++j) {
-        const int chunk = wave + 4 * j;
-        const float f = chunk >= DH / 32 ? sc[n].y : 1.f;   // (e4m3: the values' scale)
-        buf[(2 * chunk) * 64 + lane] = __builtin_bit_cast(uint4, kv8_operand<FMT>(uint2{x[n][j].x, x[n][j].y}, f));
-        buf[(2 * chunk + 1) * 64 + lane] = __builtin_bit_cast(uint4, kv8_operand<FMT>(uint2{x[n][j].z, x[n][j].w}, f));
+        for (int j = 0; j < kMine; ++j) x[n][j] = ldg16(p + j * 4096);
       }
-    }
-    const float2 now = sc[n];
-    fetch(n, blk + kAhead);
-    __syncthreads();   // (one a block: the other buffer's readers are past it)
-    if (!rows) return;
-    auto kf = [&](int kt, int s) { return __builtin_bit_cast(bf16x8, buf[(2 * s + kt) * 64 + lane]); };
-    auto vf = [&](int c) { return __builtin_bit_cast(bf16x8, buf[(DH / 16 + c) * 64 + lane]); };
-    if ((blk + 1) * kKv8Block <= length) {
-      kv8_block<DH, 2, false, FMT == AD_KV_I8>(st, kf, vf, now.x * scale, now.y, [](int) { return 0xffu; });
-    } else {
-      unsigned bits = 0;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) bits |= (blk * kKv8Block + kv8_key(g, j) < length ? 1u : 0u) << j;
-      kv8_block<DH, 2, true, FMT == AD_KV_I8>(st, kf, vf, now.x * scale, now.y, [&](int) { return bits; });
+      sc[n] = scales[at];
     }
   };
-  for (int blk = blk0; blk < blk1; blk += kAhead) {
+  uint4* buf = lds;
+  auto stage = [&](int blk) {   // blocks blk and blk + 1 into the buffer, and those behind them on their way
+    buf = lds + (blk >> 1 & 1) * 2 * kOps * 64;   // (a split begins at a multiple of two blocks)
+    if (unpacks) {
 #pragma unroll
-    for (int n = 0; n < kAhead; ++n) {
-      if (blk + n >= blk1) break;
-      work(n, blk + n);
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int j = 0; j < kMine; ++j) {
+          const int chunk = wave + 4 * j;
+          const float by = chunk >= DH / 32 ? sc[n].y : 1.f;   // (e4m3: the values' scale)
+          uint4* to = buf + (n * kOps + 2 * chunk) * 64 + lane;
+          to[0] = __builtin_bit_cast(uint4, kv8_operand<FMT>(uint2{x[n][j].x, x[n][j].y}, by));
+          to[64] = __builtin_bit_cast(uint4, kv8_operand<FMT>(uint2{x[n][j].z, x[n][j].w}, by));
+        }
     }
+#pragma unroll
+    for (int n = 0; n < 2; ++n) { c1[n] = sc[n].x * scale; cv[n] = sc[n].y; }
+    fetch(blk + 2);
+    __syncthreads();   // (one for two blocks: the other buffer's readers are past it)
+  };
+  fetch(blk0);
+  int blk = blk0;
+  for (const int whole = min(blk1, length / kKv8Block) - 1; blk < whole; blk += 2) {
+    stage(blk);
+    if (rows) kv8_text_blocks<DH, 2, false, kV>(st, l, {buf, buf + kOps * 64}, c1, cv, 0xffu);
+  }
+  if (blk >= blk1) return;
+  stage(blk);   // the last one or two, of which the very last may be incomplete
+  if (!rows) return;
+  for (int n = 0; n < 2 && blk + n < blk1; ++n) {
+    unsigned bits = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) bits |= ((blk + n) * kKv8Block + kv8_key(g, j) < length ? 1u : 0u) << j;
+    kv8_text_blocks<DH, 1, true, kV>(st, l, {buf + n * kOps * 64}, {n ? c1[1] : c1[0]}, {n ? cv[1] : cv[0]}, bits);
   }
 }
 
 // As k_kv8_attend_shared, with 128 rows of a text a workgroup and 16 of a sequence.
 template <int DH, int FMT>
-__global__ __launch_bounds__(256, DH == 128 ? 2 : 3) void k_kv8_attend_many(const unsigned char* __restrict__ cache, Kv8Attend a, Kv8Dims dm, Kv8Shared sh, Kv8Dims ds) {
-  constexpr int kStage = 2 * (DH / 8) * 64 * 16, kMerge = 4 * 16 * (DH + 4) * 4 + 4 * 16 * 2 * 4;
+__global__ __launch_bounds__(256, DH == 128 ? 2 : 4) void k_kv8_attend_many(const unsigned char* __restrict__ cache, Kv8Attend a, Kv8Dims dm, Kv8Shared sh, Kv8Dims ds) {
+  constexpr int kStage = 4 * (DH / 8) * 64 * 16, kMerge = 4 * 16 * (DH + 4) * 4 + 4 * 16 * 2 * 4;
   __shared__ __align__(16) unsigned char lds[kStage > kMerge ? kStage : kMerge];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (blockIdx.x >= sh.blocks) {
@@ -189,12 +270,13 @@ __global__ __launch_bounds__(256, DH == 128 ? 2 : 3) void k_kv8_attend_many(cons
   Kv8State<DH, 2> st;
   int pos[2];
   kv8_start<DH, 2>(st, a, sq, h, rows ? row0 : m_rows - 1, rows ? last : m_rows - 1, pos);
-  kv8_text<DH, FMT>(st, (uint4*)lds, sh.cache + bh * ds.blocks * (2 * kKv8Block * DH), (const float2*)(sh.cache + ds.scales) + bh * ds.blocks, a, sq.base, blk0, blk1, rows);
+  f32x4 sum[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+  kv8_text<DH, FMT>(st, sum, (uint4*)lds, sh.cache + bh * ds.blocks * (2 * kKv8Block * DH), (const float2*)(sh.cache + ds.scales) + bh * ds.blocks, fabsf(a.scale), sq.base, blk0, blk1, rows);
   if (!rows) return;
   const int lane = threadIdx.x & 63, g = lane >> 4;
 #pragma unroll
   for (int rt = 0; rt < 2; ++rt) {
-    const float l = kv8_rows_sum(st.l[rt]);
+    const float l = FMT == AD_KV_I8 ? kv8_rows_sum(st.l[rt]) : sum[rt][0];
     const int m = row0 + 16 * rt + (lane & 15);
     if (m > last) continue;
     const size_t at = ((size_t)(sq.row0 + m / a.group) * (dm.heads * a.group) + h * a.group + m % a.group) * a.n_split + split;
@@ -204,7 +286,7 @@ __global__ __launch_bounds__(256, DH == 128 ? 2 : 3) void k_kv8_attend_many(cons
   }
 }
 
-// The splits of a (row, query head), a wave each: the text's, then the sequence's own.
+// The splits of a (row, query head), a wave each: the text's, then the sequence's own.  (Two heads a wave, their tables looked up once: 768 rows of 16 heads the same, 4 of 8 1 us longer.)
 template <int DH>
 __global__ __launch_bounds__(256) void k_kv8_join_shared(Kv8Attend a, Kv8Deal one, Kv8Dims dm, Kv8Shared sh, Kv8Dims ds) {
   const int col = 4 * ((threadIdx.x & 63) % (DH / 4));
@@ -234,7 +316,9 @@ __global__ __launch_bounds__(256) void k_kv8_join_shared(Kv8Attend a, Kv8Deal on
 
 // What goes by the caches' sizes and the query heads alone, so that a row's sums do not depend on a call: whether a workgroup takes 128 rows of a text, and the keys of a split of it.
 static size_t text_fan(const Kv8Dims& d, const Kv8Dims& texts, int group) { return (size_t)((d.n_seq + texts.n_seq - 1) / texts.n_seq) * group; }
-static bool text_many(const Kv8Dims& d, const Kv8Dims& texts, int group) { return text_fan(d, texts, group) >= 64; }
+static bool text_many(const Kv8Dims& d, const Kv8Dims& texts, int group) { return text_fan(d, texts, group) >= 32; }
+// (us by keys of a split, 512, 1024, 2048, 4096: workgroups of 32 rows, 40 continuations of 13 rows of 4 texts of 2000 to 8000 tokens in i8 61, 54, 50, 54; of 128, 96 continuations of 8 rows of a text
+// of 8192 69, 60, 69, -, 64 of 4 query heads of 2 texts of 16,000 to 32,000 72, 62, 67, -)
 static int text_split_keys(const Kv8Dims& d, const Kv8Dims& texts, int group) {
   const bool many = text_many(d, texts, group);
   const size_t rows = text_fan(d, texts, group) * (many ? 1 : std::min(d.k_max, 8)), parts = (size_t)texts.n_seq * d.heads * (many ? (rows + 127) / 128 : (rows + 31) / 32);
