@@ -83,40 +83,55 @@ __device__ __forceinline__ unsigned order_of(float v) {
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-// 2^(j / 32)
-__device__ const double kPowers[32] = {
-    1.0, 1.0218971486541166, 1.0442737824274138, 1.0671404006768237,
-    1.0905077326652577, 1.1143867425958924, 1.1387886347566916, 1.1637248587775775,
-    1.189207115002721, 1.215247359980469, 1.241857812073484, 1.2690509571917332,
-    1.2968395546510096, 1.3252366431597413, 1.3542555469368927, 1.383909881963832,
-    1.4142135623730951, 1.4451808069770467, 1.4768261459394993, 1.5091644275934228,
-    1.5422108254079407, 1.5759808451078865, 1.6104903319492543, 1.645755478153965,
-    1.681792830507429, 1.718619298122478, 1.7562521603732995, 1.7947090750031072,
-    1.8340080864093424, 1.8741676341103, 1.9152065613971474, 1.9571441241754002};
+// 2^(-j / 128)
+__device__ const double kPowers[128] = {
+    1.0, 0.9945994234836332, 0.9892280131939755, 0.9838856116165879, 0.9785720620877001, 0.9732872087896166,
+    0.9680308967461472, 0.9628029718180625, 0.9576032806985737, 0.9524316709088371, 0.9472879907934828, 0.9421720895161673,
+    0.93708381705515, 0.9320230241988945, 0.9269895625416927, 0.921983284479313, 0.9170040432046712, 0.9120516927035267,
+    0.9071260877501994, 0.902227083903312, 0.8973545375015536, 0.8925083056594675, 0.8876882462632606, 0.8828942179666364,
+    0.8781260801866497, 0.8733836930995845, 0.8686669176368531, 0.8639756154809188, 0.859309649061239, 0.8546688815502315,
+    0.8500531768592617, 0.8454623996346526, 0.8408964152537145, 0.8363550898207983, 0.8318382901633682, 0.8273458838280972,
+    0.8228777390769825, 0.8184337248834822, 0.8140137109286739, 0.8096175675974319, 0.8052451659746271, 0.8008963778413467,
+    0.7965710756711335, 0.7922691326262469, 0.7879904225539432, 0.7837348199827765, 0.7795022001189185, 0.7752924388425,
+    0.7711054127039704, 0.766940998920478, 0.7627990753722692, 0.7586795205991074, 0.7545822137967114, 0.7505070348132128,
+    0.7464538641456324, 0.7424225829363762, 0.7384130729697497, 0.7344252166684909, 0.7304588970903235, 0.7265139979245263,
+    0.7225904034885233, 0.7186879987244912, 0.714806669195985, 0.7109463010845828, 0.7071067811865476, 0.7032879969095077,
+    0.6994898362691556, 0.6957121878859631, 0.691954940981916, 0.6882179853772651, 0.6845012114872953, 0.6808045103191124,
+    0.6771277734684463, 0.6734708931164729, 0.6698337620266515, 0.6662162735415808, 0.6626183215798707, 0.659039800633032,
+    0.6554806057623822, 0.6519406325959679, 0.6484197773255048, 0.6449179367033329, 0.6414350080393891, 0.637970889198196,
+    0.6345254785958666, 0.6310986751971254, 0.6276903785123455, 0.6243004885946024, 0.620928906036742, 0.6175755319684667,
+    0.614240268053435, 0.6109230164863788, 0.6076236799902345, 0.6043421618132908, 0.6010783657263515, 0.5978321960199137,
+    0.5946035575013605, 0.5913923554921705, 0.5881984958251406, 0.5850218848416251, 0.5818624293887887, 0.5787200368168756,
+    0.5755946149764913, 0.5724860722159021, 0.5693943173783458, 0.5663192597993596, 0.5632608093041209, 0.5602188762048034,
+    0.5571933712979462, 0.5541842058618394, 0.5511912916539204, 0.5482145409081884, 0.5452538663326288, 0.5423091811066546,
+    0.5393803988785599, 0.5364674337629878, 0.5335702003384118, 0.530688613644631, 0.5278225891802786, 0.5249720429003436,
+    0.5221368912137069, 0.5193170509806894, 0.5165124395106142, 0.5137229745593819, 0.5109485743270583, 0.5081891574554765,
+    0.5054446430258502, 0.5027149505564014};
 
 // A row's weights
 struct Weigh {
   float m, half, step;  // half: of m; step: of the histograms, bins two units of the scores
-  double rate, least;   // least: 2's exponent of min_p (-inf: none)
+  double rate, most;    // 128 log2(e) / T; the most that a score of min_p's weight lies below the maximum (inf: no min_p)
   int bits;             // S
-  const double* table;  // 2^(j / 32)
-  __device__ __forceinline__ double power(float v) const { return ((double)v - (double)m) * rate; }   // (the difference is exact; at temperatures near 0 a rounded product would not do)
-  // 2^(t + S) for -100 <= t <= 0 in whole numbers, 1 at least: 2^f, |f| <= 1/64, by its series to f^4 (2e-12 relative), a table of the parts of 32, the whole part straight into the exponent
+  const double* table;  // kPowers
+  // 128 times the power of two that a score's weight lies below the maximum's 1 (the difference is exact; at temperatures near 0 a difference of rounded products would not do)
+  __device__ __forceinline__ double below(float v) const { return ((double)m - (double)v) * rate; }
+  static constexpr double kNothing = 1074.0 * 128;   // what lies further below has no double
+  // The weight 2^(S - t / 128), 0 <= t <= 12800, in whole numbers, 1 at least: 2^(-f / 128), 0 <= f < 1, by a polynomial (1 at 0 and off by 3.3e-13 at most: least maximum error), the other 127 parts by
+  // a table, the whole part straight into the exponent, and the product rounded to a whole number as it is added to 2^52.
   __device__ __forceinline__ u64 near(double t) const {
-    const double big = t + 211106232532992.0, f = t - (big - 211106232532992.0);   // 1.5 * 2^47
-    double p = 9.61812910762847716197e-3;   // ln(2)^k / k!, k = 4 .. 0
-    p = fma(p, f, 5.55041086648215799532e-2);
-    p = fma(p, f, 2.40226506959100712334e-1);
-    p = fma(p, f, 6.93147180559945309417e-1);
+    const int n = (int)t;
+    const double f = __builtin_amdgcn_fract(t);
+    double p = -2.6397700221988634e-08;
+    p = fma(p, f, 1.466222257317361e-05);
+    p = fma(p, f, -0.005415212341565815);
     p = fma(p, f, 1.0);
-    const int n32 = (int)__builtin_bit_cast(long long, big);
-    const long long b = __builtin_bit_cast(long long, p * table[n32 & 31]);
-    const unsigned hi = (unsigned)(b >> 32) + ((unsigned)((n32 >> 5) + bits) << 20);
-    const double w = __builtin_bit_cast(double, (long long)((u64)hi << 32 | (unsigned)b));   // <= 2^51
-    const u64 n = __builtin_bit_cast(u64, w + 4503599627370496.0) & 0xfffffffffffffull;     // (to nearest)
-    return n | (u64)(n == 0);
+    const long long b = __builtin_bit_cast(long long, table[n & 127]);
+    const unsigned hi = (unsigned)(b >> 32) + ((unsigned)(bits - (n >> 7)) << 20);
+    const u64 w = __builtin_bit_cast(u64, fma(p, __builtin_bit_cast(double, (long long)((u64)hi << 32 | (unsigned)b)), 4503599627370496.0)) & 0xfffffffffffffull;   // (<= 2^51)
+    return w | (u64)(w == 0);
   }
-  __device__ __forceinline__ u64 of(double t) const { return t < -1074.0 ? 0 : near(fmax(t, -100.0)); }
+  __device__ __forceinline__ u64 of(double t) const { return t > kNothing ? 0 : near(fmin(t, 12800.0)); }
   // The histogram's bin: 28 to a T, so that what falls into the last one lies 36.5 T or more below the maximum and weighs 1 or nothing.
   // (by halves: the difference itself may be beyond fp32)
   __device__ __forceinline__ float place(float v) const { return fmaf(v, -0.5f, half) * step; }
@@ -126,14 +141,15 @@ struct Weigh {
 template <int THREADS, int EACH> struct TruncateShared {
   static constexpr int kMost = EACH * THREADS;   // scores of the list
   u64 hist[kBins];
-  double table[32];
+  double table[128];
   u64 part[THREADS / 64];
   float lo[THREADS / 64], hi[THREADS / 64];
   float list_x[kMost];   // in the row's order
   int list_i[kMost];
   uint4 rank[kList];     // score, index, weight
-  int order[kList];      // of the ranked: how many are before it,
-  u64 sum[kList];        // the weights up to it
+  // of the ranked, where the histogram was: the weights up to it, how many are before it
+  __device__ __forceinline__ u64& sum(int i) { return hist[i]; }
+  __device__ __forceinline__ int& order(int i) { return ((int*)(hist + kList))[i]; }
   u64 above;      // before the bin that holds the border
   int bin, n;
   Border border;
@@ -162,6 +178,14 @@ template <typename T, int THREADS, int KEEP> struct TruncateRow {
     first = (int)(threadIdx.x >> 6) * per * 64 + (int)(threadIdx.x & 63);
   }
   __device__ __forceinline__ int index(int c) const { return (first + 64 * c) * kVec - skew; }   // of vector c's first score
+  // the same row as another wave has it
+  __device__ __forceinline__ TruncateRow of_wave(int wave) const {
+    TruncateRow x = *this;
+    const int lane = threadIdx.x & 63;
+    x.first = wave * per * 64 + lane;
+    x.kept = kept - threadIdx.x + wave * 64 + lane;
+    return x;
+  }
   __device__ __forceinline__ bool whole(int i) const { return i >= 0 && i + kVec <= vocab; }
   __device__ __forceinline__ uint4 fetch(int c) const {   // (-inf off the row)
     const int i = index(c);
@@ -230,12 +254,22 @@ template <typename T, int THREADS, int KEEP> struct TruncateRow {
   // Weights of all, bin by bin; their sum goes with them.  What is in the last bin weighs 1 (or nothing) and is counted apart.
   template <typename S> __device__ __forceinline__ void weigh_all(S& s, const Weigh& weigh) const {
     unsigned tail = 0;
+    // (weights of four scores at once, without a branch: a score's is a chain of ten steps in 64 bits)
     vectors([&](int, const float (&v)[kVec]) {
 #pragma unroll
-      for (int e = 0; e < kVec; ++e) {
-        const float at = weigh.place(v[e]);
-        if (at < (float)(kBins - 1)) atomicAdd(&s.hist[(int)at], weigh.near(weigh.power(v[e])));
-        else if (v[e] > -INFINITY) tail += weigh.power(v[e]) >= -1074.0;
+      for (int h = 0; h < kVec; h += 4) {
+        u64 w[4];
+        float at[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const double t = weigh.below(v[h + e]);
+          w[e] = weigh.near(t);   // (meant for those that are not in the last bin)
+          at[e] = weigh.place(v[h + e]);
+          tail += (int)(at[e] >= (float)(kBins - 1)) & (int)(t <= Weigh::kNothing);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (at[e] < (float)(kBins - 1)) atomicAdd(&s.hist[(int)at[e]], w[e]);
       }
     });
     if (tail) atomicAdd(&s.hist[kBins - 1], (u64)tail);
@@ -280,43 +314,95 @@ template <typename T, int THREADS, int KEEP> struct TruncateRow {
     __syncthreads();
     return all;
   }
-  // The least index whose f(score, index) up to it sum to want(sum of all) or more; the winning wave looks for it alone.  Left in s.border: its score and index.
-  template <typename S, typename F, typename W> __device__ __forceinline__ u64 find(S& s, const F& f, const W& want) const {
+  // f(scores' weights, those that do not stay 0) of each vector that has one that stays; weight(score) of four at once, without a branch
+  template <typename P, typename G> __device__ __forceinline__ bool weights(int c, const float (&v)[kVec], const P& stays, const G& weight, u64 (&e)[kVec]) const {
+    bool in[kVec];
+    int some = 0;
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) { in[j] = stays(v[j], index(c) + j); some |= (int)in[j]; }
+    if (!__any(some)) return false;
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) {
+      const u64 w = weight(v[j]);
+      e[j] = in[j] ? w : 0;
+    }
+    return true;
+  }
+  // The least index up to which the weights of those that stay sum to want(sum of all) or more.  Left in s.border: its score and index.
+  template <typename S, typename P, typename G, typename W> __device__ __forceinline__ u64 find(S& s, const P& stays, const G& weight, const W& want) const {
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     u64 sum = 0;
-    each([&](float v, int i) { sum += f(v, i); });
+    vectors([&](int c, const float (&v)[kVec]) {
+      u64 e[kVec];
+      if (!weights(c, v, stays, weight, e)) return;
+#pragma unroll
+      for (int j = 0; j < kVec; ++j) sum += e[j];
+    });
     sum = wave_sum_u64(sum);
     __syncthreads();
     if (lane == 0) s.part[wave] = sum;
     __syncthreads();
     u64 all, before = s.before(all);
     const u64 target = want(all);
-    if (before < target && before + sum >= target) {   // (one wave)
-#pragma clang loop unroll(disable)
-      for (int c = 0; c < per; ++c) {
+    if (lane == 0 && before < target && before + sum >= target) { s.bin = wave; s.above = before; }
+    __syncthreads();
+    const TruncateRow x = of_wave(alike(s.bin));
+    before = alike(s.above);
+    // every wave takes some of the winner's vectors (64 at a time, whose sums lie where the histogram was), then each looks for the one that holds the target
+    for (int c0 = 0;; c0 += 64) {
+      const int n = min(per - c0, 64);
+      for (int c = wave; c < n; c += THREADS / 64) {
         float v[kVec];
         u64 e[kVec], own = 0;
-        load(c, v);
+        x.load(c0 + c, v);
+        if (x.weights(c0 + c, v, stays, weight, e)) {
 #pragma unroll
-        for (int j = 0; j < kVec; ++j) { e[j] = f(v[j], index(c) + j); own += e[j]; }
-        const u64 up = wave_scan_u64(own), total = lane_u64(up, 63);
-        if (before + total < target) {
-          before += total;
-          continue;
+          for (int j = 0; j < kVec; ++j) own += e[j];
         }
-        u64 at = before + up - own;
-        if (at < target && at + own >= target) {   // (one lane)
+        own = wave_sum_u64(own);
+        if (lane == 0) s.hist[c] = own;
+      }
+      __syncthreads();
+      const u64 own = lane < n ? s.hist[lane] : 0, up = wave_scan_u64(own);
+      const u64 here = __ballot(before + up >= target);
+      if (here != 0) {
+        const int c = __ffsll(here) - 1;
+        if (c % (THREADS / 64) == wave) {
+          u64 at = before + lane_u64(up, c) - lane_u64(own, c);
+          float v[kVec];
+          u64 e[kVec], mine = 0;
+          x.load(c0 + c, v);
+          if (x.weights(c0 + c, v, stays, weight, e)) {
 #pragma unroll
-          for (int j = 0; j < kVec; ++j) {
-            if (at < target && at + e[j] >= target) s.border = Border{v[j], index(c) + j};
-            at += e[j];
+            for (int j = 0; j < kVec; ++j) mine += e[j];
+            at += wave_scan_u64(mine) - mine;
+            if (at < target && at + mine >= target) {   // (one lane)
+#pragma unroll
+              for (int j = 0; j < kVec; ++j) {
+                if (at < target && at + e[j] >= target) s.border = Border{v[j], x.index(c0 + c) + j};
+                at += e[j];
+              }
+            }
           }
         }
         break;
       }
+      before += lane_u64(up, 63);
+      if (c0 + 64 >= per) break;   // (not reached: the winner has it)
+      __syncthreads();
     }
     __syncthreads();
     return all;
+  }
+  // weight(score) of those that stay into the histogram's bin(score)
+  template <typename S, typename P, typename G, typename B> __device__ __forceinline__ void into(S& s, const P& stays, const G& weight, const B& bin) const {
+    vectors([&](int c, const float (&v)[kVec]) {
+      u64 e[kVec];
+      if (!weights(c, v, stays, weight, e)) return;
+#pragma unroll
+      for (int j = 0; j < kVec; ++j)
+        if (e[j]) atomicAdd(&s.hist[bin(v[j])], e[j]);
+    });
   }
 };
 
@@ -332,10 +418,15 @@ template <int THREADS, int EACH> struct TruncateList {
 #pragma clang loop unroll(disable)
     for (int j = 0; j < per; ++j) f(at(j), s.list_i[first + 64 * j]);
   }
-  template <typename S, typename F, typename W> __device__ __forceinline__ u64 find(S& s, const F& f, const W& want) const {
+  template <typename S, typename P, typename G, typename B> __device__ __forceinline__ void into(S& s, const P& stays, const G& weight, const B& bin) const {
+    each([&](float v, int i) {
+      if (stays(v, i)) atomicAdd(&s.hist[bin(v)], weight(v));
+    });
+  }
+  template <typename S, typename P, typename G, typename W> __device__ __forceinline__ u64 find(S& s, const P& stays, const G& weight, const W& want) const {
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     u64 sum = 0;
-    each([&](float v, int i) { sum += f(v, i); });
+    each([&](float v, int i) { sum += stays(v, i) ? weight(v) : 0; });
     sum = wave_sum_u64(sum);
     __syncthreads();
     if (lane == 0) s.part[wave] = sum;
@@ -347,7 +438,7 @@ template <int THREADS, int EACH> struct TruncateList {
       for (int j = 0; j < per; ++j) {
         const float v = at(j);
         const int i = s.list_i[first + 64 * j];
-        const u64 own = f(v, i), up = wave_scan_u64(own);
+        const u64 own = stays(v, i) ? weight(v) : 0, up = wave_scan_u64(own);
         if (before + up >= target && before + up - own < target) s.border = Border{v, i};
         before += lane_u64(up, 63);
         if (before >= target) break;
@@ -392,7 +483,7 @@ template <int THREADS, int EACH, typename W> __device__ __forceinline__ u64 trun
 // Ranks s.rank[0 .. n), n <= kList: how many come before each, and the sums of weights up to it, by all waves: each takes 64 of them and compares them with its share of all.
 template <int THREADS, int EACH> __device__ __forceinline__ void truncate_rank(TruncateShared<THREADS, EACH>& s, int n) {
   const int t = threadIdx.x, lane = t & 63, wave = alike(t >> 6);
-  for (int i = t; i < n; i += THREADS) { s.order[i] = 0; s.sum[i] = 0; }
+  for (int i = t; i < n; i += THREADS) { s.order(i) = 0; s.sum(i) = 0; }
   __syncthreads();
   const int groups = (n + 63) / 64, shares = THREADS / 64 / groups, group = wave % groups, share = wave / groups, e = group * 64 + lane;
   if (share < shares && e < n) {
@@ -406,8 +497,8 @@ template <int THREADS, int EACH> __device__ __forceinline__ void truncate_rank(T
       const uint4 r = s.rank[j];
       if (b.holds(__uint_as_float(r.x), (int)r.y)) { ++before; up += (u64)r.w << 32 | r.z; }
     }
-    atomicAdd(&s.order[e], before);   // (with itself)
-    atomicAdd(&s.sum[e], up);
+    atomicAdd(&s.order(e), before);   // (with itself)
+    atomicAdd(&s.sum(e), up);
   }
   __syncthreads();
 }
@@ -417,11 +508,11 @@ __device__ __forceinline__ uint4 truncate_entry(float v, int i, u64 w) { return 
 template <int THREADS, int EACH, typename X>
 __device__ __forceinline__ Border truncate_refine(TruncateShared<THREADS, EACH>& s, const X& x, const Weigh& weigh, bool weights, const Border& had, u64 target) {
   const int t = threadIdx.x, wave = t >> 6, lane = t & 63;
-  auto one = [&](float v) -> u64 { return weights ? weigh.of(weigh.power(v)) : 1; };
+  auto one = [&](float v) -> u64 { return weights ? weigh.of(weigh.below(v)) : 1; };
   float lo = -INFINITY, hi = weigh.m;    // the scores among which the border lies
   int shift = -1;                        // below 0: the first histogram
   auto bin_of = [&](float v) -> int { return shift < 0 ? weigh.bin(v) : (int)((order_of(hi) - order_of(v)) >> max(shift, 0)); };
-  auto here = [&](float v, int i) { return (int)(v >= lo) & (int)(v <= hi) & (int)had.holds(v, i); };
+  auto here = [&](float v, int i) -> bool { return (int)(v >= lo) & (int)(v <= hi) & (int)had.holds(v, i); };
 #pragma clang loop unroll(disable)
   for (;;) {
     const int bin = alike(s.bin);
@@ -443,23 +534,20 @@ __device__ __forceinline__ Border truncate_refine(TruncateShared<THREADS, EACH>&
       truncate_rank(s, n);
       if (t < n) {
         const uint4 r = s.rank[t];
-        const u64 up = above + s.sum[t];
+        const u64 up = above + s.sum(t);
         if (up >= target && up - ((u64)r.w << 32 | r.z) < target) s.border = Border{__uint_as_float(r.x), (int)r.y};
       }
       break;
     }
-    for (int w = 0; w < THREADS / 64; ++w) { least = fminf(least, s.lo[w]); most = fmaxf(most, s.hi[w]); }
-    lo = alike(least); hi = alike(most);
+    lo = alike(-wave_max(-s.lo[lane % (THREADS / 64)])); hi = alike(wave_max(s.hi[lane % (THREADS / 64)]));
     if (lo == hi) {
       const u64 each = alike(one(lo)), nth = (target - above + each - 1) / each;
-      x.find(s, [&](float v, int i) -> u64 { return (int)(v == lo) & (int)had.holds(v, i); }, [&](u64) { return nth; });
+      x.find(s, [&](float v, int i) -> bool { return (int)(v == lo) & (int)had.holds(v, i); }, [&](float) -> u64 { return 1; }, [&](u64) { return nth; });
       break;
     }
     shift = max(0, 32 - __clz(order_of(hi) - order_of(lo)) - 10);
     truncate_clear(s);
-    x.each([&](float v, int i) {
-      if (here(v, i)) atomicAdd(&s.hist[bin_of(v)], one(v));
-    });
+    x.into(s, here, one, bin_of);
     truncate_bin(s, above, [&](u64) { return target; });
   }
   __syncthreads();
@@ -470,9 +558,7 @@ __device__ __forceinline__ u64 truncate_part(float p, u64 all) { return max(ceil
 template <int THREADS, int EACH, typename X>
 __device__ __forceinline__ Border truncate_select(TruncateShared<THREADS, EACH>& s, const X& x, const Weigh& weigh, bool weights, const Border& had, int k, float p) {
   truncate_clear(s);
-  x.each([&](float v, int i) {
-    if (had.holds(v, i)) atomicAdd(&s.hist[weigh.bin(v)], weights ? weigh.of(weigh.power(v)) : (u64)1);
-  });
+  x.into(s, [&](float v, int i) { return had.holds(v, i); }, [&](float v) { return weights ? weigh.of(weigh.below(v)) : (u64)1; }, [&](float v) { return weigh.bin(v); });
   const u64 target = truncate_bin(s, 0, [&](u64 all) { return weights ? truncate_part(p, all) : min(all, (u64)k); });
   return truncate_refine(s, x, weigh, weights, had, target);
 }
@@ -494,14 +580,14 @@ __device__ __forceinline__ Border truncate_short(TruncateShared<THREADS, EACH>& 
   const int t = threadIdx.x;
   if (t < n) {
     const float v = s.list_x[t];
-    s.rank[t] = truncate_entry(v, s.list_i[t], weigh.of(weigh.power(v)));
+    s.rank[t] = truncate_entry(v, s.list_i[t], weigh.of(weigh.below(v)));
   }
   truncate_rank(s, n);
   k = min(k, n);
   const bool mine = t < n;
   const uint4 r = mine ? s.rank[t] : uint4{0, 0, 0, 0};
-  const int place = mine ? s.order[t] : INT_MAX;   // (from 1)
-  const u64 up = mine ? s.sum[t] : 0;
+  const int place = mine ? s.order(t) : INT_MAX;   // (from 1)
+  const u64 up = mine ? s.sum(t) : 0;
   const Border b{__uint_as_float(r.x), (int)r.y};
   if (place == k) { s.border = b; s.above = up; }
   __syncthreads();
@@ -527,8 +613,12 @@ __global__ __launch_bounds__(THREADS) void k_truncate(TruncateArgs a) {
   const Row x(a, row, kept);
   const float temp = a.temperature ? a.temperature[b] : 1.f, top_p = a.top_p ? a.top_p[b] : 1.f, min_p = a.min_p ? a.min_p[b] : 0.f;
   const int top_k = a.top_k ? a.top_k[b] : 0;
-  const double rate = 1.44269504088896340736 / (double)temp;
-  if (t < 32) s.table[t] = kPowers[t];
+  const double rate = 128 * 1.44269504088896340736 / (double)temp;
+  if (t < 128) s.table[t] = kPowers[t];
+  bool clear = true;   // the histogram
+#pragma unroll
+  for (int j = 0; j < kBins / THREADS; ++j) s.hist[t + j * THREADS] = 0;
+  if (t == 0) { s.n = 0; s.bin = -1; }
   constexpr int kLargest = THREADS >= 1024 ? 2 : THREADS >= 512 ? 4 : 8;
   float most[kLargest];   // of every kLargest-th of this thread's vectors
 #pragma unroll
@@ -545,25 +635,26 @@ __global__ __launch_bounds__(THREADS) void k_truncate(TruncateArgs a) {
 #pragma unroll
   for (int j = 1; j < kLargest; ++j) m = fmaxf(m, most[j]);
   m = wave_max(m);
-  if (lane == 0) s.hi[wave] = m;
-  bad = __syncthreads_or(bad);
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) m = fmaxf(m, s.hi[w]);
+  bad = __any(bad);
+  if (lane == 0) { s.hi[wave] = m; s.lo[wave] = bad ? 1.f : 0.f; }
+  __syncthreads();
+  m = wave_max(s.hi[lane % kWaves]);
+  bad = __any(s.lo[lane % kWaves] != 0.f);
   bad = bad || m == -INFINITY;   // no distribution
   m = alike(m);
-  Weigh weigh{m, 0.5f * m, fminf((float)(rate * (56 * 0.69314718055994530942)), 1e30f), rate, -INFINITY, min(51, 62 - (32 - __clz(a.vocab))), s.table};
-  if (min_p > 0.f) weigh.least = log2((double)fminf(min_p, 1.f));
+  Weigh weigh{m, 0.5f * m, fminf((float)(rate * (56 * 0.69314718055994530942 / 128)), 1e30f), rate, INFINITY, min(51, 62 - (32 - __clz(a.vocab))), s.table};
+  if (min_p > 0.f) weigh.most = -128.0 * log2((double)fminf(min_p, 1.f));
   Border border{bad ? INFINITY : -INFINITY, -1};
   constexpr int kMost = EACH * THREADS;
   int n = INT_MAX;   // of the list, once that has all that stays
-  auto to_list = [&](float end) { n = alike(x.gather(s, [&](float v) { return weigh.place(v) < end; })); };
 #pragma clang loop unroll(disable)
   for (int stage = 0; stage < 2; ++stage) {   // top_k, top_p
     const bool weights = stage == 1, first = top_k > 0 && top_k < a.vocab;
     if (bad || !(weights ? top_p < 1.f : first)) continue;
     u64 target = 0;
     if (!weights || !first) {   // (of the first k scores the list has all, or they do not go there)
-      truncate_clear(s);
+      if (!clear) truncate_clear(s);
+      clear = false;
       if (weights) {
         x.weigh_all(s, weigh);
       } else if (top_k <= kMost) {
@@ -573,7 +664,18 @@ __global__ __launch_bounds__(THREADS) void k_truncate(TruncateArgs a) {
       }
       target = alike(truncate_bin(s, 0, [&](u64 all) { return weights ? truncate_part(top_p, all) : all < (u64)top_k ? 0 : (u64)top_k; }));
       const int bin = alike(s.bin);
-      if (target != 0 && bin < kBins - 1) to_list((float)(bin + 1));   // (the last bin's are not told from what is not there)
+      // What is in the bins up to the border's goes into the list (the last bin's are not told from what is not there), or, where that has no room for it, what is in the border's alone.
+      if (target != 0 && bin < kBins - 1) {
+        const float begin = (float)bin, end = begin + 1.f;
+        n = alike(x.gather(s, [&](float v) { return weigh.place(v) < end; }));
+        if (weights && n > kMost) {
+          const int among = alike(x.gather(s, [&](float v) { return weigh.place(v) >= begin && weigh.place(v) < end; }));
+          if (among <= kMost) {
+            border = truncate_refine(s, List(s, among), weigh, true, border, target);
+            break;
+          }
+        }
+      }
       if (!weights) target = 0;
     }
     if (n <= kList) {
@@ -587,7 +689,7 @@ __global__ __launch_bounds__(THREADS) void k_truncate(TruncateArgs a) {
       border = target != 0 ? truncate_refine(s, x, weigh, true, border, target) : truncate_select(s, x, weigh, weights, border, top_k, top_p);
     }
   }
-  if (SAMPLE && !bad && n == INT_MAX && border.i < 0 && min_p > 0.f) n = alike(x.gather(s, [&](float v) { return weigh.power(v) >= weigh.least; }));
+  if (SAMPLE && !bad && n == INT_MAX && border.i < 0 && min_p > 0.f) n = alike(x.gather(s, [&](float v) { return weigh.below(v) <= weigh.most; }));
   if constexpr (SAMPLE) {
     if (bad) {
       if (t == 0) {
@@ -597,16 +699,13 @@ __global__ __launch_bounds__(THREADS) void k_truncate(TruncateArgs a) {
       return;
     }
     const float u = a.u[row];
-    auto stays = [&](float v, int i) -> u64 {
-      if (!border.holds(v, i)) return 0;
-      const double power = weigh.power(v);
-      return power >= weigh.least ? weigh.of(power) : 0;
-    };
+    auto stays = [&](float v, int i) -> bool { return (int)border.holds(v, i) & (int)(weigh.below(v) <= weigh.most); };
+    auto weight = [&](float v) { return weigh.of(weigh.below(v)); };
     auto want = [&](u64 z) { return !(u > 0.f) ? (u64)1 : u >= 1.f ? z : floor_part(u, z) + 1; };
-    const u64 all = n <= kMost ? List(s, n).find(s, stays, want) : x.find(s, stays, want);
+    const u64 all = n <= kMost ? List(s, n).find(s, stays, weight, want) : x.find(s, stays, weight, want);
     if (t == 0) {
       a.tokens[row] = s.border.i;
-      if (a.log_probs) a.log_probs[row] = (float)((weigh.power(s.border.x) + (double)weigh.bits) * 0.69314718055994530942 - log((double)all));
+      if (a.log_probs) a.log_probs[row] = (float)(((double)weigh.bits - weigh.below(s.border.x) / 128) * 0.69314718055994530942 - log((double)all));
     }
   } else {
     T* out = (T*)a.out + (size_t)row * a.out_stride;
@@ -617,7 +716,7 @@ __global__ __launch_bounds__(THREADS) void k_truncate(TruncateArgs a) {
       // (selected without a branch: the compiler lost the -inf of a branch's other side)
 #pragma unroll
       for (int j = 0; j < kVec; ++j) {
-        const int stays = (int)border.holds(v[j], i + j) & (int)(weigh.power(v[j]) >= weigh.least);
+        const int stays = (int)border.holds(v[j], i + j) & (int)(weigh.below(v[j]) <= weigh.most);
         w[j] = stays ? __float_as_uint(v[j]) : 0xff800000u;
       }
       if (wide && x.whole(i)) {
@@ -646,8 +745,7 @@ template <bool SAMPLE> static void launch(int dtype, const TruncateArgs& a, hipS
     using T = decltype(type);
     constexpr int kVec = 16 / (int)sizeof(T);
     if (a.vocab <= 1024 * kVec) k_truncate<T, 256, 4, 2, SAMPLE><<<a.rows, 256, 0, s>>>(a);
-    else if (a.vocab <= 10 * 1024 * kVec) k_truncate<T, 1024, 8, 2, SAMPLE><<<a.rows, 1024, 0, s>>>(a);
-    else k_truncate<T, 1024, 0, 16, SAMPLE><<<a.rows, 1024, 0, s>>>(a);
+    else k_truncate<T, 1024, 8, 2, SAMPLE><<<a.rows, 1024, 0, s>>>(a);
   };
   if (dtype == AD_BF16) go(bf16_t{});
   else go(float{});
