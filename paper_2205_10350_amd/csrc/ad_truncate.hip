@@ -274,18 +274,24 @@ template <typename T, int THREADS, int KEEP> struct TruncateRow {
     });
     if (tail) atomicAdd(&s.hist[kBins - 1], (u64)tail);
   }
-  // Those with pred(score) into the list, in their order, if they go there; how many there are.
-  template <typename S, typename P> __device__ __forceinline__ int gather(S& s, const P& pred) const {
+  // Those with pred(score) into the list, in their order, if they go there; how many there are.  may(score) of the largest of every eighth vector: whether one of these may have one.
+  template <typename S, typename M, typename P> __device__ __forceinline__ int gather(S& s, const float (&most)[8], const M& may, const P& pred) const {
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    int mine = 0;
+    int mine = 0, groups = 0;
     u64 some = 0;   // vectors with one
-    vectors([&](int c, const float (&v)[kVec]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) groups |= __any(may(most[j])) ? 1 << j : 0;
+#pragma clang loop unroll(disable)
+    for (int c = 0; c < per; ++c) {
+      if (!(groups >> (c & 7) & 1)) continue;
+      float v[kVec];
+      load(c, v);
       int n = 0;
 #pragma unroll
       for (int e = 0; e < kVec; ++e) n += pred(v[e]);
       mine += n;
       if (__any(n)) some |= (u64)1 << min(c, 63);
-    });
+    }
     const u64 count = wave_sum_u64(mine);
     __syncthreads();
     if (lane == 0) s.part[wave] = count;
@@ -619,21 +625,28 @@ __global__ __launch_bounds__(THREADS) void k_truncate(TruncateArgs a) {
 #pragma unroll
   for (int j = 0; j < kBins / THREADS; ++j) s.hist[t + j * THREADS] = 0;
   if (t == 0) { s.n = 0; s.bin = -1; }
-  constexpr int kLargest = THREADS >= 1024 ? 2 : THREADS >= 512 ? 4 : 8;
-  float most[kLargest];   // of every kLargest-th of this thread's vectors
+  float most[8];   // of every eighth of this thread's vectors
 #pragma unroll
-  for (int j = 0; j < kLargest; ++j) most[j] = -INFINITY;
+  for (int j = 0; j < 8; ++j) most[j] = -INFINITY;
   bool bad = !(temp > 0.f && temp < INFINITY) || top_p != top_p || min_p != min_p;
   x.take([&](const float (&v)[kVec], int j) {
 #pragma unroll
     for (int e = 0; e < kVec; ++e) {
       bad = bad || !(v[e] < INFINITY);
-      most[j % kLargest] = fmaxf(most[j % kLargest], v[e]);
+      most[j] = fmaxf(most[j], v[e]);
     }
   });
-  float m = most[0];
+  constexpr int kLargest = THREADS >= 1024 ? 2 : 8;
+  float largest[kLargest];   // of 2048 parts of the row
 #pragma unroll
-  for (int j = 1; j < kLargest; ++j) m = fmaxf(m, most[j]);
+  for (int j = 0; j < kLargest; ++j) {
+    largest[j] = most[j];
+#pragma unroll
+    for (int i = j + kLargest; i < 8; i += kLargest) largest[j] = fmaxf(largest[j], most[i]);
+  }
+  float m = largest[0];
+#pragma unroll
+  for (int j = 1; j < kLargest; ++j) m = fmaxf(m, largest[j]);
   m = wave_max(m);
   bad = __any(bad);
   if (lane == 0) { s.hi[wave] = m; s.lo[wave] = bad ? 1.f : 0.f; }
@@ -660,16 +673,17 @@ __global__ __launch_bounds__(THREADS) void k_truncate(TruncateArgs a) {
       } else if (top_k <= kMost) {
 #pragma unroll
         for (int j = 0; j < kLargest; ++j)
-          if (most[j] > -INFINITY) atomicAdd(&s.hist[weigh.bin(most[j])], (u64)1);
+          if (largest[j] > -INFINITY) atomicAdd(&s.hist[weigh.bin(largest[j])], (u64)1);
       }
       target = alike(truncate_bin(s, 0, [&](u64 all) { return weights ? truncate_part(top_p, all) : all < (u64)top_k ? 0 : (u64)top_k; }));
       const int bin = alike(s.bin);
       // What is in the bins up to the border's goes into the list (the last bin's are not told from what is not there), or, where that has no room for it, what is in the border's alone.
       if (target != 0 && bin < kBins - 1) {
         const float begin = (float)bin, end = begin + 1.f;
-        n = alike(x.gather(s, [&](float v) { return weigh.place(v) < end; }));
+        auto near = [&](float v) { return weigh.place(v) < end; };
+        n = alike(x.gather(s, most, near, near));
         if (weights && n > kMost) {
-          const int among = alike(x.gather(s, [&](float v) { return weigh.place(v) >= begin && weigh.place(v) < end; }));
+          const int among = alike(x.gather(s, most, near, [&](float v) { return weigh.place(v) >= begin && weigh.place(v) < end; }));
           if (among <= kMost) {
             border = truncate_refine(s, List(s, among), weigh, true, border, target);
             break;
@@ -689,7 +703,10 @@ __global__ __launch_bounds__(THREADS) void k_truncate(TruncateArgs a) {
       border = target != 0 ? truncate_refine(s, x, weigh, true, border, target) : truncate_select(s, x, weigh, weights, border, top_k, top_p);
     }
   }
-  if (SAMPLE && !bad && n == INT_MAX && border.i < 0 && min_p > 0.f) n = alike(x.gather(s, [&](float v) { return weigh.below(v) <= weigh.most; }));
+  if (SAMPLE && !bad && n == INT_MAX && border.i < 0 && min_p > 0.f) {
+    auto stays = [&](float v) { return weigh.below(v) <= weigh.most; };
+    n = alike(x.gather(s, most, stays, stays));
+  }
   if constexpr (SAMPLE) {
     if (bad) {
       if (t == 0) {
