@@ -236,8 +236,11 @@ int ad_truncate_scores(const void* logits, int32_t dtype, int64_t logits_stride,
   if (out_stride < vocab) return refuse("ad_truncate_scores: row stride below vocab");
   const size_t size = dtype == AD_F32 ? 4 : 2;
   if ((uintptr_t)out & (size - 1)) return refuse("ad_truncate_scores: out not aligned to its type");
+  // rows that lie between the scores' rows overlap them nowhere
+  const int64_t apart = (int64_t)(((intptr_t)out - (intptr_t)logits) / (intptr_t)size), between = logits_stride ? (apart % logits_stride + logits_stride) % logits_stride : 0;
+  const bool interleaved = out_stride == logits_stride && between >= vocab && between + vocab <= logits_stride;
   if (out == logits ? out_stride != logits_stride && rows > 1
-                    : (uintptr_t)out < (uintptr_t)logits + ((size_t)logits_stride * (rows - 1) + vocab) * size && (uintptr_t)logits < (uintptr_t)out + ((size_t)out_stride * (rows - 1) + vocab) * size)
+                    : !interleaved && (uintptr_t)out < (uintptr_t)logits + ((size_t)logits_stride * (rows - 1) + vocab) * size && (uintptr_t)logits < (uintptr_t)out + ((size_t)out_stride * (rows - 1) + vocab) * size)
     return refuse("ad_truncate_scores: out must be the scores themselves, with their stride, or not overlap them");
   TruncateArgs a{};
   a.x = logits; a.stride = (size_t)logits_stride; a.vocab = vocab; a.n_seq = n_seq; a.rows = rows; a.row_start = row_start;

@@ -4,7 +4,7 @@
 // least number whose weights sum to p of theirs or more (one at least); of them those with w >= min_p.  So what stays is a front of that order: everything before a border
 // (score, index).  The drawn token is the least index whose weights up to it, of what stays, exceed u of all of that.
 //
-// Weights are whole numbers of 2^-S, S = min(51, 62 - log2 of the vocabulary): w is rounded to nearest and to 1 at least (what a double has no number for is 0), and all of a
+// Weights are whole numbers of 2^-S, S = min(51, 62 - the bits of the vocabulary): w is rounded to nearest and to 1 at least (what a double has no number for is 0), and all of a
 // row sum to less than 2^63.  Whole sums are exact, so neither atomics nor the launch's shape change a border or a token, and p Z and u Z are compared exactly.  What rounding moves a border by,
 // 2^-S a token, is some 10^-12 of the sum at most: a drawn number falls there once in 10^8 draws.
 //

@@ -212,11 +212,15 @@ class Kv8Cache:
 
         def call(stream):
             nonlocal out
-            if out is None:
-                out = torch.empty((rows, heads, c.head_width), dtype=self._bf16, device=self.device)
-            op, os, orows = _rows(out, "out", i, self._bf16, heads, c.head_width)
-            if orows != rows:
-                _refuse("out must have as many rows as q")
+            if out is None and qs == heads * c.head_width:
+                out = torch.empty_like(q)
+                op, os = out.data_ptr(), qs
+            else:
+                if out is None:
+                    out = torch.empty((rows, heads, c.head_width), dtype=self._bf16, device=self.device)
+                op, os, orows = _rows(out, "out", i, self._bf16, heads, c.head_width)
+                if orows != rows:
+                    _refuse("out must have as many rows as q")
             sizes = heads, rows, keys, text_keys, shared.cfg.n_seq, shared.cfg.capacity
             need = self._need.get(sizes)
             if need is None:

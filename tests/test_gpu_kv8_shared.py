@@ -350,8 +350,9 @@ def test_the_text_in_the_same_cache():
         assert np.all(np.abs(f64(got[r]) - ref) <= tol) and np.all(np.abs(f64(want[r]) - ref) <= tol)
 
 
-def test_scores_of_all_sizes_and_other_scales():
-    p = Problem("i8", 64, 1, 2, [2], [300], [40, 60], [4, 4], True)
+@pytest.mark.parametrize("fmt,q_heads", [("i8", 2), ("i8", 32), ("e4m3", 32)])     # (the latter: workgroups of 128 rows)
+def test_scores_of_all_sizes_and_other_scales(fmt, q_heads):
+    p = Problem(fmt, 64, 1, q_heads, [2], [300], [40, 60], [4, 4], True)
     p.q[1] = 0
     p.q[2] *= -40
     p.q[5] *= 30
@@ -359,11 +360,12 @@ def test_scores_of_all_sizes_and_other_scales():
         p.check(p.go(scale=scale), scale=scale)
 
 
-def test_tokens_that_are_not_finite_spoil_what_sees_them_and_nothing_else():
-    clean = Problem("e4m3", 64, 1, 1, [2, 2], [96, 64], [10, 40, 5, 50], [2, 2, 2, 2], True)
+@pytest.mark.parametrize("fmt,q_heads", [("e4m3", 1), ("e4m3", 32), ("i8", 32)])
+def test_tokens_that_are_not_finite_spoil_what_sees_them_and_nothing_else(fmt, q_heads):
+    clean = Problem(fmt, 64, 1, q_heads, [2, 2], [96, 64], [10, 40, 5, 50], [2, 2, 2, 2], True)
     want = clean.go()
     for where in ("text", "own"):
-        p = Problem("e4m3", 64, 1, 1, [2, 2], [96, 64], [10, 40, 5, 50], [2, 2, 2, 2], True)
+        p = Problem(fmt, 64, 1, q_heads, [2, 2], [96, 64], [10, 40, 5, 50], [2, 2, 2, 2], True)
         if where == "text":
             p.tv[0, 50, 0, 3] = INF
             feed(p.shared, p.tk, p.tv, p.text, 96)

@@ -319,5 +319,10 @@ def test_refused():
     wide = torch.zeros((3, 16), device="cuda")
     with pytest.raises(ad.AdError, match="overlap"):
         ad.truncate_scores(wide[:, :10], out=wide[:, 4:14])
+    # rows between the scores' rows do not
+    fused = torch.randn((3, 2, 10), device="cuda")
+    k = i32([2, 3, 1])
+    assert torch.equal(ad.truncate_scores(fused[:, 1], top_k=k, out=fused[:, 0]), ad.truncate_scores(fused[:, 1], top_k=k))
+    assert torch.equal(ad.truncate_scores(fused[:, 0], top_k=k, out=fused[:, 1]), ad.truncate_scores(fused[:, 0], top_k=k))
     empty = ad.sample_tokens(x[:0], u[:0])
     assert empty.shape == (0,) and ad.truncate_scores(x[:0]).shape == (0, 10)
