@@ -4,7 +4,7 @@
 // moved within the bf16 ring, from the slot that it has in one cache to the one that it has in the other.  All entries of a call are read before any is written: a
 // workgroup takes the same bytes of the same block and head of all entries at once, holds them in registers, waits, and writes them; what one workgroup reads no other
 // writes.  Bound by memory, a byte read and a byte written for a value: 139 MB of 16 sequences, 16 heads, to another cache in 50 to 60 us, 67 MB of 16 sequences of width 128 within one in 28, 4.7 to 5 TB/s;
-three copies of 301 tokens 4.7 us, a launch and two waits for memory.
+// three copies of 301 tokens 4.7 us, a launch and two waits for memory.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
