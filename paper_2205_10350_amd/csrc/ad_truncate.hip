@@ -730,12 +730,16 @@ __global__ __launch_bounds__(THREADS) void k_truncate(TruncateArgs a) {
     x.vectors([&](int c, const float (&v)[kVec]) {
       const int i = x.index(c);
       unsigned w[kVec];
+      int heavy[kVec];
+#pragma unroll
+      for (int j = 0; j < kVec; ++j) heavy[j] = 1;
+      if (min_p > 0.f) {
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) heavy[j] = weigh.below(v[j]) <= weigh.most;
+      }
       // (selected without a branch: the compiler lost the -inf of a branch's other side)
 #pragma unroll
-      for (int j = 0; j < kVec; ++j) {
-        const int stays = (int)border.holds(v[j], i + j) & (int)(weigh.below(v[j]) <= weigh.most);
-        w[j] = stays ? __float_as_uint(v[j]) : 0xff800000u;
-      }
+      for (int j = 0; j < kVec; ++j) w[j] = ((int)border.holds(v[j], i + j) & heavy[j]) != 0 ? __float_as_uint(v[j]) : 0xff800000u;
       if (wide && x.whole(i)) {
         uint4 o;
         if constexpr (sizeof(T) == 4) {
