@@ -91,28 +91,28 @@ __device__ __forceinline__ unsigned order_of(float v) {
 
 // 2^(-j / 128)
 __device__ const double kPowers[128] = {
-    1.0, 0.9945994234836332, 0.9892280131939755, 0.9838856116165879, 0.9785720620877001, 0.9732872087896166,
-    0.9680308967461472, 0.9628029718180625, 0.9576032806985737, 0.9524316709088371, 0.9472879907934828, 0.9421720895161673,
-    0.93708381705515, 0.9320230241988945, 0.9269895625416927, 0.921983284479313, 0.9170040432046712, 0.9120516927035267,
-    0.9071260877501994, 0.902227083903312, 0.8973545375015536, 0.8925083056594675, 0.8876882462632606, 0.8828942179666364,
-    0.8781260801866497, 0.8733836930995845, 0.8686669176368531, 0.8639756154809188, 0.859309649061239, 0.8546688815502315,
-    0.8500531768592617, 0.8454623996346526, 0.8408964152537145, 0.8363550898207983, 0.8318382901633682, 0.8273458838280972,
-    0.8228777390769825, 0.8184337248834822, 0.8140137109286739, 0.8096175675974319, 0.8052451659746271, 0.8008963778413467,
-    0.7965710756711335, 0.7922691326262469, 0.7879904225539432, 0.7837348199827765, 0.7795022001189185, 0.7752924388425,
-    0.7711054127039704, 0.766940998920478, 0.7627990753722692, 0.7586795205991074, 0.7545822137967114, 0.7505070348132128,
-    0.7464538641456324, 0.7424225829363762, 0.7384130729697497, 0.7344252166684909, 0.7304588970903235, 0.7265139979245263,
-    0.7225904034885233, 0.7186879987244912, 0.714806669195985, 0.7109463010845828, 0.7071067811865476, 0.7032879969095077,
-    0.6994898362691556, 0.6957121878859631, 0.691954940981916, 0.6882179853772651, 0.6845012114872953, 0.6808045103191124,
-    0.6771277734684463, 0.6734708931164729, 0.6698337620266515, 0.6662162735415808, 0.6626183215798707, 0.659039800633032,
-    0.6554806057623822, 0.6519406325959679, 0.6484197773255048, 0.6449179367033329, 0.6414350080393891, 0.637970889198196,
-    0.6345254785958666, 0.6310986751971254, 0.6276903785123455, 0.6243004885946024, 0.620928906036742, 0.6175755319684667,
-    0.614240268053435, 0.6109230164863788, 0.6076236799902345, 0.6043421618132908, 0.6010783657263515, 0.5978321960199137,
-    0.5946035575013605, 0.5913923554921705, 0.5881984958251406, 0.5850218848416251, 0.5818624293887887, 0.5787200368168756,
-    0.5755946149764913, 0.5724860722159021, 0.5693943173783458, 0.5663192597993596, 0.5632608093041209, 0.5602188762048034,
-    0.5571933712979462, 0.5541842058618394, 0.5511912916539204, 0.5482145409081884, 0.5452538663326288, 0.5423091811066546,
-    0.5393803988785599, 0.5364674337629878, 0.5335702003384118, 0.530688613644631, 0.5278225891802786, 0.5249720429003436,
-    0.5221368912137069, 0.5193170509806894, 0.5165124395106142, 0.5137229745593819, 0.5109485743270583, 0.5081891574554765,
-    0.5054446430258502, 0.5027149505564014};
+    1.0, 0x1.fd3c22b8f71f1p-1, 0x1.fa7c1819e90d8p-1, 0x1.f7bfdad9cbe14p-1, 0x1.f50765b6e4540p-1, 0x1.f252b376bba97p-1,
+    0x1.efa1bee615a27p-1, 0x1.ecf482d8e67f1p-1, 0x1.ea4afa2a490dap-1, 0x1.e7a51fbc74c83p-1, 0x1.e502ee78b3ff6p-1, 0x1.e264614f5a129p-1,
+    0x1.dfc97337b9b5fp-1, 0x1.dd321f301b460p-1, 0x1.da9e603db3285p-1, 0x1.d80e316c98398p-1, 0x1.d5818dcfba487p-1, 0x1.d2f87080d89f2p-1,
+    0x1.d072d4a07897cp-1, 0x1.cdf0b555dc3fap-1, 0x1.cb720dcef9069p-1, 0x1.c8f6d9406e7b5p-1, 0x1.c67f12e57d14bp-1, 0x1.c40ab5fffd07ap-1,
+    0x1.c199bdd85529cp-1, 0x1.bf2c25bd71e09p-1, 0x1.bcc1e904bc1d2p-1, 0x1.ba5b030a1064ap-1, 0x1.b7f76f2fb5e47p-1, 0x1.b59728de5593ap-1,
+    0x1.b33a2b84f15fbp-1, 0x1.b0e07298db666p-1, 0x1.ae89f995ad3adp-1, 0x1.ac36bbfd3f37ap-1, 0x1.a9e6b5579fdbfp-1, 0x1.a799e1330b358p-1,
+    0x1.a5503b23e255dp-1, 0x1.a309bec4a2d33p-1, 0x1.a0c667b5de565p-1, 0x1.9e86319e32323p-1, 0x1.9c49182a3f090p-1, 0x1.9a0f170ca07bap-1,
+    0x1.97d829fde4e50p-1, 0x1.95a44cbc8520fp-1, 0x1.93737b0cdc5e5p-1, 0x1.9145b0b91ffc6p-1, 0x1.8f1ae99157736p-1, 0x1.8cf3216b5448cp-1,
+    0x1.8ace5422aa0dbp-1, 0x1.88ac7d98a6699p-1, 0x1.868d99b4492edp-1, 0x1.8471a4623c7adp-1, 0x1.82589994cce13p-1, 0x1.80427543e1a12p-1,
+    0x1.7e2f336cf4e62p-1, 0x1.7c1ed0130c132p-1, 0x1.7a11473eb0187p-1, 0x1.780694fde5d3fp-1, 0x1.75feb564267c9p-1, 0x1.73f9a48a58174p-1,
+    0x1.71f75e8ec5f74p-1, 0x1.6ff7df9519484p-1, 0x1.6dfb23c651a2fp-1, 0x1.6c012750bdabfp-1, 0x1.6a09e667f3bcdp-1, 0x1.68155d44ca973p-1,
+    0x1.6623882552225p-1, 0x1.6434634ccc320p-1, 0x1.6247eb03a5585p-1, 0x1.605e1b976dc09p-1, 0x1.5e76f15ad2148p-1, 0x1.5c9268a5946b7p-1,
+    0x1.5ab07dd485429p-1, 0x1.58d12d497c7fdp-1, 0x1.56f4736b527dap-1, 0x1.551a4ca5d920fp-1, 0x1.5342b569d4f82p-1, 0x1.516daa2cf6642p-1,
+    0x1.4f9b2769d2ca7p-1, 0x1.4dcb299fddd0dp-1, 0x1.4bfdad5362a27p-1, 0x1.4a32af0d7d3dep-1, 0x1.486a2b5c13cd0p-1, 0x1.46a41ed1d0057p-1,
+    0x1.44e086061892dp-1, 0x1.431f5d950a897p-1, 0x1.4160a21f72e2ap-1, 0x1.3fa4504ac801cp-1, 0x1.3dea64c123422p-1, 0x1.3c32dc313a8e5p-1,
+    0x1.3a7db34e59ff7p-1, 0x1.38cae6d05d866p-1, 0x1.371a7373aa9cbp-1, 0x1.356c55f929ff1p-1, 0x1.33c08b26416ffp-1, 0x1.32170fc4cd831p-1,
+    0x1.306fe0a31b715p-1, 0x1.2ecafa93e2f56p-1, 0x1.2d285a6e4030bp-1, 0x1.2b87fd0dad990p-1, 0x1.29e9df51fdee1p-1, 0x1.284dfe1f56381p-1,
+    0x1.26b4565e27cddp-1, 0x1.251ce4fb2a63fp-1, 0x1.2387a6e756238p-1, 0x1.21f49917ddc96p-1, 0x1.2063b88628cd6p-1, 0x1.1ed5022fcd91dp-1,
+    0x1.1d4873168b9aap-1, 0x1.1bbe084045cd4p-1, 0x1.1a35beb6fcb75p-1, 0x1.18af9388c8deap-1, 0x1.172b83c7d517bp-1, 0x1.15a98c8a58e51p-1,
+    0x1.1429aaea92de0p-1, 0x1.12abdc06c31ccp-1, 0x1.11301d0125b51p-1, 0x1.0fb66affed31bp-1, 0x1.0e3ec32d3d1a2p-1, 0x1.0cc922b7247f7p-1,
+    0x1.0b5586cf9890fp-1, 0x1.09e3ecac6f383p-1, 0x1.0874518759bc8p-1, 0x1.0706b29ddf6dep-1, 0x1.059b0d3158574p-1, 0x1.04315e86e7f85p-1,
+    0x1.02c9a3e778061p-1, 0x1.0163da9fb3335p-1};
 
 // A row's weights
 struct Weigh {
@@ -358,7 +358,7 @@ template <typename T, int THREADS, int KEEP> struct TruncateRow {
     const u64 target = want(all);
     if (lane == 0 && before < target && before + sum >= target) { s.bin = wave; s.above = before; }
     __syncthreads();
-    const TruncateRow x = of_wave(alike(s.bin));
+    const TruncateRow x = of_wave(min(max(alike(s.bin), 0), THREADS / 64 - 1));
     before = alike(s.above);
     // every wave takes some of the winner's vectors (64 at a time, whose sums lie where the histogram was), then each looks for the one that holds the target
     for (int c0 = 0;; c0 += 64) {
