@@ -171,7 +171,8 @@ __device__ __forceinline__ void kv8_start(Kv8State<DH, R>& st, const Kv8Attend& 
 }
 
 // The state of rows row0 .. last of a (sequence, head) over a split's blocks of this wave, two blocks on their way while one is worked on.
-template <int DH, int R, int FMT, bool CLOSED>
+// (START false: the state goes on from other keys of the same rows)
+template <int DH, int R, int FMT, bool CLOSED, bool START = true>
 __device__ __forceinline__ void kv8_wave(Kv8State<DH, R>& st, const unsigned char* cache, const Kv8Attend& a, const Kv8Dims& dm, const Kv8Seq& sq, size_t bh, int h,
                                          int row0, int last, int own_lo, int own_hi, int blk0, int blk1, int wave) {
   const int lane = threadIdx.x & 63, g = lane >> 4;
@@ -185,7 +186,12 @@ __device__ __forceinline__ void kv8_wave(Kv8State<DH, R>& st, const unsigned cha
   for (int n = 0; n < kAhead; ++n)
     if (blk + 4 * n < whole) kv8_fetch(x[n], blocks, scales, blk + 4 * n, lane);
   int pos[R];
-  kv8_start<DH, R>(st, a, sq, h, row0, last, pos);
+  if constexpr (START) {
+    kv8_start<DH, R>(st, a, sq, h, row0, last, pos);
+  } else {
+#pragma unroll
+    for (int rt = 0; rt < R; ++rt) pos[rt] = sq.base + min(row0 + 16 * rt + (lane & 15), last) / a.group;
+  }
   if (CLOSED) {
 #pragma unroll
     for (int rt = 0; rt < R; ++rt) pos[rt] = sq.base;

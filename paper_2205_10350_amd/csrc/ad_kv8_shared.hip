@@ -5,7 +5,8 @@
 // A text's part takes the rows of all of its continuations together, which lie next to each other, as the rows of one sequence over a closed cache: its keys are fetched once for 32
 // rows (of the query heads that share a head among them) instead of once for every continuation.  Both parts are one launch, cut into splits of the keys; a second joins the splits of a row, the text's first.
 // Where a text has 32 continuations (times the query heads that share a head) or more, a workgroup takes 128 of its rows, 32 a wave: all waves go over the same keys, whose operands they unpack
-// together, once, into LDS.  Else the waves take every fourth block of keys each for the same rows, as over one cache.
+// together, once, into LDS.  Else the waves take every fourth block of keys each for the same rows, as over one cache.  Where texts are short and continuations few, all of it is one launch: a workgroup takes
+// 16 rows of a continuation over the text and its own tokens.
 // A row's sums depend on the caches' sizes, the query heads and the row's own tokens alone.
 //
 // Four texts of 8000 tokens, 16 heads of width 64, e4m3, us a replay with a workgroup of 32 rows / of 128, by continuations of each and rows of a continuation: 4 x 1 21.5 / 27.9, 10 x 1 21.4 / 28.3,
@@ -286,6 +287,30 @@ __global__ __launch_bounds__(256, DH == 128 ? 2 : 4) void k_kv8_attend_many(cons
   }
 }
 
+// Short texts and sequences, one split of each and few continuations: a workgroup takes 16 rows of a sequence over its text and its own tokens, and is done.
+template <int DH, int FMT>
+__global__ __launch_bounds__(256, kv8_waves(DH, 1)) void k_kv8_attend_short(const unsigned char* __restrict__ cache, Kv8Attend a, Kv8Dims dm, Kv8Shared sh, Kv8Dims ds) {
+  __shared__ float Os[4][16 * (DH + 4)];
+  __shared__ float Ms[4][16][2];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int b, h, tile, split;
+  if (!kv8_where(blockIdx.x, a.tiles, a.rows.n_seq, dm.heads, [&](int at) { return kv8_owner(a.rows, a.tiles, at); }, [&](int b) { return kv8_first(a.rows, a.tiles, b); }, b, h, tile, split)) return;
+  Kv8Seq sq = kv8_seq(a.rows, b, dm.capacity), text{sq.row0, sq.n, 0};
+  const int g = __builtin_amdgcn_readfirstlane(shared_owner(sh.texts.n, b, [&](int g) { return sh.texts.seq_start[g]; }));
+  if (g >= 0 && b < sh.texts.seq_start[g + 1]) {
+    const Kv8Seq t = shared_seq(a.rows, sh.texts, g, ds);
+    text.base = min(t.base, sh.split_blocks * kKv8Block);
+    sq.n = sq.row0 < t.row0 ? 0 : min(sq.n, t.row0 + t.n - sq.row0);   // (beyond the bound on a text's rows: left as they were)
+  }
+  const int m_rows = sq.n * a.group, row0 = tile * 16;
+  if (row0 >= m_rows) return;
+  const int last = min(row0 + 16, m_rows) - 1;
+  Kv8State<DH, 1> st;
+  kv8_wave<DH, 1, FMT, true>(st, sh.cache, a, ds, text, (size_t)max(g, 0) * ds.heads + h, h, row0, last, text.base / kKv8Block, (text.base + kKv8Block - 1) / kKv8Block, 0, sh.split_blocks, wave);
+  kv8_wave<DH, 1, FMT, false, false>(st, cache, a, dm, sq, (size_t)b * dm.heads + h, h, row0, last, (sq.base + row0 / a.group) / kKv8Block, (sq.base + last / a.group) / kKv8Block, 0, a.split_blocks, wave);
+  kv8_merge<DH, 1>(st, Os, Ms, a, dm, sq, h, row0, last, 0, wave);
+}
+
 // The splits of a (row, query head), a wave each: the text's, then the sequence's own.  (Two heads a wave, their tables looked up once: 768 rows of 16 heads the same, 4 of 8 1 us longer.)
 template <int DH>
 __global__ __launch_bounds__(256) void k_kv8_join_shared(Kv8Attend a, Kv8Deal one, Kv8Dims dm, Kv8Shared sh, Kv8Dims ds) {
@@ -326,30 +351,38 @@ static int text_split_keys(const Kv8Dims& d, const Kv8Dims& texts, int group) {
   while (keys < 8192 && keys * 1024 < parts * texts.capacity) keys *= 2;
   return (int)keys;
 }
+// Short texts and few continuations: each continuation's workgroups read the text for themselves.  (Four texts, 16 heads of width 64, continuations with up to 300 tokens, us a replay in one launch / in two, by
+// continuations of a text, rows and tokens of a text: 2 x 1, 512 6.9 / 9.5, 1024 8.4 / 9.5, 2048 11.2 / 10.6; 8 x 1, 512 8.5 / 10.6, 1024 11.6 / 11.5; 8 x 8, 1024 12.2 / 14.9; 16 x 1, 512 11.9 / 13.7, 1024
+// 16.5 / 14.9; 16 x 8, 1024 17.3 / 23.4; 31 x 1, 512 19.6 / 19.8; 31 x 8, 512 20.0 / 32.7; 64 x 1, 512 33.7 / 27.2.)
+static bool text_short(const Kv8Dims& d, const Kv8Dims& texts, int group) {
+  return !text_many(d, texts, group) && texts.capacity <= 1024 && text_fan(d, texts, group) * texts.capacity <= 16384 && kv8_split_keys(d) >= d.capacity;
+}
 static int splits(int capacity, int max_keys, int keys) { return (std::min(max_keys, capacity) + keys - 1) / keys; }
 static int own_splits(const Kv8Dims& d, int max_keys) { return std::max(1, splits(d.capacity, max_keys, kv8_split_keys(d))); }
 static int text_splits(const Kv8Dims& d, const Kv8Dims& texts, int group, int max_keys) { return splits(texts.capacity, max_keys, text_split_keys(d, texts, group)); }
 static size_t ml_bytes(size_t parts) { return (parts * 2 * 4 + 255) / 256 * 256; }
 size_t kv8_attend_shared_bytes(const Kv8Dims& d, const Kv8Dims& texts, int q_heads, int rows, int max_keys, int max_text_keys) {
+  if (text_short(d, texts, q_heads / d.heads)) return 0;
   const size_t n = own_splits(d, max_keys) + text_splits(d, texts, q_heads / d.heads, max_text_keys), parts = (size_t)rows * q_heads * n;
   return n == 1 ? 0 : ml_bytes(parts) + parts * d.width * 4;
 }
 static Kv8Deal tiles_of(const Kv8Rows& r, int group, int shift) { return kv8_deal(r, group, shift, 1, (((size_t)r.max_rows * group - 1) >> shift) + 1); }   // of 2^shift rows
-static Kv8Deal own_tiles(const Kv8Rows& r, int group, bool many) { return tiles_of(r, group, many ? 4 : 5); }
+static Kv8Deal own_tiles(const Kv8Rows& r, int group, bool small) { return tiles_of(r, group, small ? 4 : 5); }
 static size_t of_all(const Kv8Deal& d, size_t n_seq) { return d.packed ? d.pieces : d.pieces * n_seq; }
 static Kv8Deal text_tiles(const Kv8Rows& r, const Kv8Texts& x, int group, bool many) {
   Kv8Rows t = r;
   t.n_seq = x.n; t.max_rows = std::min(x.max_rows, r.rows);
   return tiles_of(t, group, many ? 7 : 5);
 }
+static bool small_tiles(const Kv8Dims& d, const Kv8Dims& texts, int group) { return text_many(d, texts, group) || text_short(d, texts, group); }   // 16 rows of a sequence
 static size_t text_blocks(const Kv8Dims& d, const Kv8Dims& texts, const Kv8Rows& r, const Kv8Texts& x, int group, int max_text_keys) {
-  return x.max_rows == 0 ? 0 : of_all(text_tiles(r, x, group, text_many(d, texts, group)), x.n) * d.heads * text_splits(d, texts, group, max_text_keys);
+  return x.max_rows == 0 || text_short(d, texts, group) ? 0 : of_all(text_tiles(r, x, group, text_many(d, texts, group)), x.n) * d.heads * text_splits(d, texts, group, max_text_keys);
 }
-static size_t own_blocks(const Kv8Dims& d, const Kv8Rows& r, int group, bool many, int max_keys) { return of_all(own_tiles(r, group, many), r.n_seq) * d.heads * own_splits(d, max_keys); }
+static size_t own_blocks(const Kv8Dims& d, const Kv8Rows& r, int group, bool small, int max_keys) { return of_all(own_tiles(r, group, small), r.n_seq) * d.heads * own_splits(d, max_keys); }
 // (a launch takes less than 2^32 lanes along x: 2^24 workgroups of 256)
 bool kv8_attend_shared_fits(const Kv8Dims& d, const Kv8Dims& texts, const Kv8Rows& r, const Kv8Texts& x, int q_heads, int max_keys, int max_text_keys) {
   const int group = q_heads / d.heads;
-  return text_blocks(d, texts, r, x, group, max_text_keys) + own_blocks(d, r, group, text_many(d, texts, group), max_keys) < (1u << 24) && (size_t)kv8_deal(r, 1, 0, 0, r.max_rows).pieces * q_heads < (1u << 26);
+  return text_blocks(d, texts, r, x, group, max_text_keys) + own_blocks(d, r, group, small_tiles(d, texts, group), max_keys) < (1u << 24) && (size_t)kv8_deal(r, 1, 0, 0, r.max_rows).pieces * q_heads < (1u << 26);
 }
 
 void launch_kv8_attend_shared(const Kv8Dims& d, const void* cache, const Kv8Dims& texts, const void* text_cache, const void* q, size_t q_stride, void* out, size_t out_stride,
@@ -358,23 +391,25 @@ void launch_kv8_attend_shared(const Kv8Dims& d, const void* cache, const Kv8Dims
   a.q = (const bf16_t*)q; a.out = (bf16_t*)out; a.q_stride = q_stride; a.out_stride = out_stride;
   a.rows = r; a.group = q_heads / d.heads; a.scale = scale * kLog2e;
   a.split_blocks = kv8_split_keys(d) / kKv8Block;
-  const bool many = text_many(d, texts, a.group);
-  a.tiles = own_tiles(r, a.group, many);
+  const bool many = text_many(d, texts, a.group), one_launch = text_short(d, texts, a.group), small = small_tiles(d, texts, a.group);
+  a.tiles = own_tiles(r, a.group, small);
   Kv8Shared sh;
   sh.cache = (const unsigned char*)text_cache; sh.texts = x;
   sh.split_blocks = text_split_keys(d, texts, a.group) / kKv8Block;
   sh.n_split = text_splits(d, texts, a.group, max_text_keys);
   sh.tiles = text_tiles(r, x, a.group, many);
   sh.blocks = (unsigned)text_blocks(d, texts, r, x, a.group, max_text_keys);
-  a.n_split = sh.n_split + own_splits(d, max_keys);
+  a.n_split = one_launch ? 1 : sh.n_split + own_splits(d, max_keys);
+  if (one_launch) sh.split_blocks = (std::min(max_text_keys, texts.capacity) + kKv8Block - 1) / kKv8Block;
   const size_t parts = (size_t)r.rows * q_heads * a.n_split;
   a.part_ml = (float*)ws;
   a.part_o = (float*)((char*)ws + ml_bytes(parts));
-  const unsigned blocks = sh.blocks + (unsigned)own_blocks(d, r, a.group, many, max_keys);
+  const unsigned blocks = sh.blocks + (unsigned)own_blocks(d, r, a.group, small, max_keys);
   const Kv8Deal one = kv8_deal(r, 1, 0, 0, r.max_rows);
   const dim3 rows((unsigned)(((size_t)one.pieces * q_heads + 3) / 4), one.packed ? 1 : r.n_seq);
   kv8_dispatch(d, [&](auto width, auto fmt) {
-    if (many) k_kv8_attend_many<width.value, fmt.value><<<blocks, 256, 0, s>>>((const unsigned char*)cache, a, d, sh, texts);
+    if (one_launch) k_kv8_attend_short<width.value, fmt.value><<<blocks, 256, 0, s>>>((const unsigned char*)cache, a, d, sh, texts);
+    else if (many) k_kv8_attend_many<width.value, fmt.value><<<blocks, 256, 0, s>>>((const unsigned char*)cache, a, d, sh, texts);
     else k_kv8_attend_shared<width.value, fmt.value><<<blocks, 256, 0, s>>>((const unsigned char*)cache, a, d, sh, texts);
     if (a.n_split > 1) k_kv8_join_shared<width.value><<<rows, 256, 0, s>>>(a, one, d, sh, texts);
   });

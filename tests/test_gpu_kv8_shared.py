@@ -277,6 +277,7 @@ CASES = [
     # format, width, heads, query heads, sequences of each text, lengths of the texts, own tokens, rows, closed
     ("e4m3", 64, 2, 2, [3, 1], [64, 96], [0, 1, 40, 33], [1, 1, 1, 1], False),
     ("i8", 64, 2, 2, [2, 0, 3], [700, 5, 33], [0, 31, 32, 100, 7], [25, 1, 9, 3, 40], True),
+    ("i8", 64, 2, 2, [2, 0, 3], [1700, 5, 33], [0, 31, 32, 100, 7], [25, 1, 9, 3, 40], True),
     ("e4m3", 32, 3, 6, [1, 4], [1, 1030], [5, 600, 0, 64, 2], [33, 1, 2, 1, 70], True),
     ("i8", 32, 1, 1, [6], [1600], [1, 2, 3, 4, 5, 6], [8] * 6, False),
     ("e4m3", 128, 1, 4, [2, 2], [520, 0], [3, 30, 0, 77], [1, 2, 5, 1], True),

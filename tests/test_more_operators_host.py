@@ -66,7 +66,7 @@ def test_copy_refuses():
 def test_attend_shared_refuses():
     L = ad.lib()
 
-    def go(c=cfg(), cache=P, s=cfg(n_seq=3, capacity=1000, closed=1), shared=FAR, q=P, qs=256, heads=4, start=P, length=P, first=P, texts=P, rows=8, most=8, keys=100, together=8,
+    def go(c=cfg(), cache=P, s=cfg(n_seq=3, capacity=2000, closed=1), shared=FAR, q=P, qs=256, heads=4, start=P, length=P, first=P, texts=P, rows=8, most=8, keys=100, together=8,
            text_keys=1000, scale=0.125, out=P, os=256, ws=P, size=1 << 40):
         return L.ad_kv8_attend_shared(C.byref(c), cache, C.byref(s), shared, q, qs, heads, start, length, first, texts, rows, most, keys, together, text_keys, scale, out, os, ws, size, None)
     for bad in (dict(c=cfg(closed=1)), dict(s=cfg(n_heads=2)), dict(s=cfg(head_width=128)), dict(s=cfg(format=ad.AD_KV_I8)), dict(s=cfg(n_seq=0)), dict(cache=None), dict(shared=None),
@@ -75,10 +75,11 @@ def test_attend_shared_refuses():
                 dict(keys=-1), dict(text_keys=-1), dict(scale=math.nan), dict(scale=math.inf), dict(ws=None), dict(ws=P + 64)):
         assert go(**bad) == ad.AD_EINVAL, bad
         assert message()
-    need = L.ad_kv8_attend_shared_bytes(C.byref(cfg()), C.byref(cfg(n_seq=3, capacity=1000, closed=1)), 4, 8, 100, 1000)
+    need = L.ad_kv8_attend_shared_bytes(C.byref(cfg()), C.byref(cfg(n_seq=3, capacity=2000, closed=1)), 4, 8, 100, 1000)
     # 1000 keys of the texts are two splits of 512, the own 100 one: 8 rows x 4 heads x 3 parts of 64 + 2 numbers
     assert need == 8 * 4 * 3 * 64 * 4 + 8 * 4 * 3 * 8
     assert go(size=need - 1) == ad.AD_ENOMEM
+    assert L.ad_kv8_attend_shared_bytes(C.byref(cfg()), C.byref(cfg(n_seq=3, capacity=1000)), 4, 8, 100, 1000) == 0       # short texts: one launch
     assert go(rows=0, most=0, together=0) == ad.AD_OK
     wide = cfg(n_seq=1, n_heads=256, k_max=65536, capacity=1 << 17)
     assert go(c=wide, s=wide, heads=65536, qs=65536 * 64, os=65536 * 64, rows=65536, most=65536, together=65536, size=1 << 62) == ad.AD_EINVAL and "workgroups" in message()
