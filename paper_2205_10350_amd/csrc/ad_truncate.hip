@@ -586,29 +586,77 @@ __device__ __forceinline__ int truncate_owner(const TruncateArgs& a, int row) {
   return q >= 0 && a.row_start[q] <= row && row < a.row_start[q + 1] ? q : -1;
 }
 
-// The border over a list of n <= kList scores, all at once: of the first k of them; of those, the front with `target` of the weights (0: with part p of theirs).
-template <int THREADS, int EACH>
-__device__ __forceinline__ Border truncate_short(TruncateShared<THREADS, EACH>& s, int n, const Weigh& weigh, int k, float p, u64 target) {
-  const int t = threadIdx.x;
+__device__ __forceinline__ u64 pick(bool p, u64 a, u64 b) { return p ? a : b; }
+// A list of n <= kList scores, all at once: ranked by all waves, the rest by the first one alone, four neighbours a lane, so without a barrier.  The border of the first k of them; of those, of the front
+// with `target` of the weights (0: with part p of theirs); left in s.border.  SAMPLE: then of what stays, and weighs enough for min_p, the least index up to which weights sum to want(sum of all) or more:
+// draw(its score, its index, the sum of all), by one lane.
+template <bool SAMPLE, int THREADS, int EACH, typename W, typename D>
+__device__ __forceinline__ void truncate_short(TruncateShared<THREADS, EACH>& s, int n, const Weigh& weigh, int k, float p, u64 target, const W& want, const D& draw) {
+  const int t = threadIdx.x, lane = t & 63;
   if (t < n) {
     const float v = s.list_x[t];
     s.rank[t] = truncate_entry(v, s.list_i[t], weigh.of(weigh.below(v)));
   }
   truncate_rank(s, n);
+  if (t >= 64) return;
   k = min(k, n);
-  const bool mine = t < n;
-  const uint4 r = mine ? s.rank[t] : uint4{0, 0, 0, 0};
-  const int place = mine ? s.order(t) : INT_MAX;   // (from 1)
-  const u64 up = mine ? s.sum(t) : 0;
-  const Border b{__uint_as_float(r.x), (int)r.y};
-  if (place == k) { s.border = b; s.above = up; }
-  __syncthreads();
-  if (p >= 1.f) return Border{alike(s.border.x), alike(s.border.i)};
-  if (target == 0) target = truncate_part(p, alike(s.above));
-  __syncthreads();
-  if (place <= k && up >= target && up - ((u64)r.w << 32 | r.z) < target) s.border = b;
-  __syncthreads();
-  return Border{alike(s.border.x), alike(s.border.i)};
+  uint4 r[4];
+  int place[4];   // (from 1)
+  u64 up[4], w[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int at = 4 * lane + j;
+    const bool mine = at < n;
+    r[j] = s.rank[min(at, n - 1)];
+    place[j] = mine ? s.order(min(at, n - 1)) : INT_MAX;
+    up[j] = s.sum(min(at, n - 1));
+    w[j] = (u64)r[j].w << 32 | r[j].z;
+  }
+  // the one of all lanes' for which f(j): its place and the weights up to it, its score and index
+  struct { int place; u64 up; Border b; } found;
+  auto only = [&](auto f) {
+    int at = -1;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) at = f(j) ? j : at;
+    const int src = max(__ffsll(__ballot(at >= 0)) - 1, 0);
+    int pl = place[0];
+    u64 u = up[0];
+    unsigned x = r[0].x, i = r[0].y;
+#pragma unroll
+    for (int j = 1; j < 4; ++j) {
+      pl = at == j ? place[j] : pl;
+      u = pick(at == j, up[j], u);
+      x = at == j ? r[j].x : x;
+      i = at == j ? r[j].y : i;
+    }
+    found.place = __builtin_amdgcn_readlane(pl, src);
+    found.up = lane_u64(u, src);
+    found.b = Border{__uint_as_float((unsigned)__builtin_amdgcn_readlane((int)x, src)), __builtin_amdgcn_readlane((int)i, src)};
+  };
+  only([&](int j) { return place[j] == k; });
+  if (p < 1.f) {
+    if (target == 0) target = truncate_part(p, found.up);
+    only([&](int j) { return place[j] <= k && up[j] >= target && up[j] - w[j] < target; });
+  }
+  if constexpr (!SAMPLE) {
+    if (lane == 0) s.border = found.b;
+  } else {
+    u64 e[4], own = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int stays = (int)(place[j] <= found.place) & (int)(weigh.below(__uint_as_float(r[j].x)) <= weigh.most);
+      own += e[j] = stays ? w[j] : 0;
+    }
+    const u64 sums = wave_scan_u64(own), all = lane_u64(sums, 63), to = want(all);
+    u64 at = sums - own;
+    if (at < to && at + own >= to) {   // (one lane)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (at < to && at + e[j] >= to) draw(__uint_as_float(r[j].x), (int)r[j].y, all);
+        at += e[j];
+      }
+    }
+  }
 }
 
 // KEEP: vectors of a lane that stay in LDS; EACH: scores of a thread that the list has room for
@@ -665,6 +713,12 @@ __global__ __launch_bounds__(THREADS) void k_truncate(TruncateArgs a) {
   if (min_p > 0.f) weigh.most = -128.0 * log2((double)fminf(min_p, 1.f));
   Border border{bad ? INFINITY : -INFINITY, -1};
   constexpr int kMost = EACH * THREADS;
+  const float u = SAMPLE ? a.u[row] : 0.f;
+  auto want = [&](u64 z) { return !(u > 0.f) ? (u64)1 : u >= 1.f ? z : floor_part(u, z) + 1; };
+  auto draw = [&](float v, int i, u64 all) {   // the drawn score, its index, the weights of all that stay
+    a.tokens[row] = i;
+    if (a.log_probs) a.log_probs[row] = (float)(((double)weigh.bits - weigh.below(v) / 128) * 0.69314718055994530942 - log((double)all));
+  };
   int n = INT_MAX;   // of the list, once that has all that stays
 #pragma clang loop unroll(disable)
   for (int stage = 0; stage < 2; ++stage) {   // top_k, top_p
@@ -698,9 +752,12 @@ __global__ __launch_bounds__(THREADS) void k_truncate(TruncateArgs a) {
       }
       if (!weights) target = 0;
     }
-    if (n <= kList) {
-      border = truncate_short(s, n, weigh, first ? top_k : INT_MAX, top_p, target);
-      break;   // (both at once)
+    if (n <= kList) {   // (both at once)
+      truncate_short<SAMPLE>(s, n, weigh, first ? top_k : INT_MAX, top_p, target, want, draw);
+      if (SAMPLE) return;
+      __syncthreads();
+      border = Border{alike(s.border.x), alike(s.border.i)};
+      break;
     }
     if (n <= kMost) {
       const List list(s, n);
@@ -721,15 +778,10 @@ __global__ __launch_bounds__(THREADS) void k_truncate(TruncateArgs a) {
       }
       return;
     }
-    const float u = a.u[row];
     auto stays = [&](float v, int i) -> bool { return (int)border.holds(v, i) & (int)(weigh.below(v) <= weigh.most); };
     auto weight = [&](float v) { return weigh.of(weigh.below(v)); };
-    auto want = [&](u64 z) { return !(u > 0.f) ? (u64)1 : u >= 1.f ? z : floor_part(u, z) + 1; };
     const u64 all = n <= kMost ? List(s, n).find(s, stays, weight, want) : x.find(s, stays, weight, want);
-    if (t == 0) {
-      a.tokens[row] = s.border.i;
-      if (a.log_probs) a.log_probs[row] = (float)(((double)weigh.bits - weigh.below(s.border.x) / 128) * 0.69314718055994530942 - log((double)all));
-    }
+    if (t == 0) draw(s.border.x, s.border.i, all);
   } else {
     T* out = (T*)a.out + (size_t)row * a.out_stride;
     const bool wide = (((uintptr_t)out ^ (uintptr_t)x.x) & 15) == 0;
