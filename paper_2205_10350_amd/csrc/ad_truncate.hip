@@ -13,9 +13,9 @@
 // 256 scores are ranked by comparing each with each; of more the step that holds the border is cut into equal parts of the floating point numbers between its least and its largest until 256 are left, or all are
 // equal and their indices decide.  Where the list has no room (2048) it takes the border's step alone, and the token is looked for over the row.
 //
-// What bounds it: a row of 32,000 scores with top_k 50 and top_p takes 12 us, 2 of them to read it and the rest eight steps of 0.5 to 2 us between barriers of 16 waves; with top_p alone 18.7 us, 8 of them the
-// histogram, 33 instructions a score, 9 of them in 64 bits, at 60 % of what one compute unit can issue.  32 rows 13.5 us; 416 rows of blocks truncated 48.5, where two turns of 256 rows overlap little (53 MB read and
-// written, 20 us at a copy's rate); 256 rows of 100,003 scores, settings of each row's own, 104 us: the slowest rows', where thousands of tokens stay and weights are taken twice (the others take 25; 102 MB).
+// What bounds it: a row of 32,000 scores with top_k 50 and top_p takes 12 us, 2 of them to read it and the rest eight steps of 0.5 to 2 us between barriers of 16 waves; with top_p alone 18.3 us, 8 of them the
+// histogram, 33 instructions a score, 9 of them in 64 bits, at 60 % of what one compute unit can issue.  32 rows 12.8 us; 416 rows of blocks truncated 48.9, where two turns of 256 rows overlap little (53 MB read and
+// written, 20 us at a copy's rate); 256 rows of 100,003 scores, settings of each row's own, 106 us: the slowest rows', where thousands of tokens stay and weights are taken twice (the others take 25; 102 MB).
 // (us, 32,000 scores top_p / 256 x 100,003 / 416 rows truncated; workgroups of 512 threads, 6 vectors of a lane in LDS, 25.6 / 138 / 59; of 256 39 / 344 / 121; of 1024, as here, 21.4 / 107 / 53.  Weights of the
 // histogram in 32 bits first, and in 64 where a border lies near: 19.3 / 129 / 57 where these were 19.8 / 103 / 49.)
 #include <hip/hip_runtime.h>
