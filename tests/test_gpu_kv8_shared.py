@@ -273,6 +273,9 @@ class Problem:
                 r += 1
 
 
+# (query heads that share a head, the texts' capacity) of all in one launch, of workgroups of 32 rows and of 128
+FORMS = [(1, None), (1, 1100), (32, None)]
+
 CASES = [
     # format, width, heads, query heads, sequences of each text, lengths of the texts, own tokens, rows, closed
     ("e4m3", 64, 2, 2, [3, 1], [64, 96], [0, 1, 40, 33], [1, 1, 1, 1], False),
@@ -313,10 +316,11 @@ def test_attention_over_shared_texts(case):
         r += m
 
 
+@pytest.mark.parametrize("group,capacity", FORMS)
 @pytest.mark.parametrize("closed", [False, True])
-def test_sequences_of_no_text_texts_of_no_sequence_and_empty_texts(closed):
+def test_sequences_of_no_text_texts_of_no_sequence_and_empty_texts(closed, group, capacity):
     text = [64, 32, 0, 96]
-    p = Problem("e4m3", 64, 2, 4, [0, 2, 1, 1], text, [10, 20, 0, 33, 5, 40], [2, 1, 3, 1, 1, 2], closed)
+    p = Problem("e4m3", 64, 2, 2 * max(group, 2), [0, 2, 1, 1], text, [10, 20, 0, 33, 5, 40], [2, 1, 3, 1, 1, 2], closed, capacity=capacity)
     p.first = [1, 1, 3, 4, 5]                  # sequences 0 and 5 of no text, text 0 of none, text 2 empty
     got = p.go()
     p.check(got)
@@ -361,12 +365,12 @@ def test_scores_of_all_sizes_and_other_scales(fmt, q_heads):
         p.check(p.go(scale=scale), scale=scale)
 
 
-@pytest.mark.parametrize("fmt,q_heads", [("e4m3", 1), ("e4m3", 32), ("i8", 32)])
-def test_tokens_that_are_not_finite_spoil_what_sees_them_and_nothing_else(fmt, q_heads):
-    clean = Problem(fmt, 64, 1, q_heads, [2, 2], [96, 64], [10, 40, 5, 50], [2, 2, 2, 2], True)
+@pytest.mark.parametrize("fmt,q_heads,capacity", [("e4m3", 1, None), ("e4m3", 1, 1100), ("e4m3", 32, None), ("i8", 32, None)])
+def test_tokens_that_are_not_finite_spoil_what_sees_them_and_nothing_else(fmt, q_heads, capacity):
+    clean = Problem(fmt, 64, 1, q_heads, [2, 2], [96, 64], [10, 40, 5, 50], [2, 2, 2, 2], True, capacity=capacity)
     want = clean.go()
     for where in ("text", "own"):
-        p = Problem(fmt, 64, 1, q_heads, [2, 2], [96, 64], [10, 40, 5, 50], [2, 2, 2, 2], True)
+        p = Problem(fmt, 64, 1, q_heads, [2, 2], [96, 64], [10, 40, 5, 50], [2, 2, 2, 2], True, capacity=capacity)
         if where == "text":
             p.tv[0, 50, 0, 3] = INF
             feed(p.shared, p.tk, p.tv, p.text, 96)
@@ -395,12 +399,14 @@ def test_many_texts_with_and_without_bounds(n_text, each):
     assert torch.equal(got, p.go(max_shared_rows=together, max_rows=3))
 
 
-def test_rows_lie_apart_and_what_is_no_row_stays():
-    p = Problem("e4m3", 64, 2, 2, [2, 1], [64, 32], [30, 4, 64], [3, 0, 5], False, k_max=40)
+@pytest.mark.parametrize("group,capacity", FORMS)
+def test_rows_lie_apart_and_what_is_no_row_stays(group, capacity):
+    heads = 2 * group
+    p = Problem("e4m3", 64, 2, heads, [2, 1], [64, 32], [30, 4, 64], [3, 0, 5], False, k_max=40, capacity=capacity)
     total, extra = 8, 2
-    wide = torch.full((total + extra, 3, 2, 64), NAN, dtype=torch.bfloat16, device="cuda")
+    wide = torch.full((total + extra, 3, heads, 64), NAN, dtype=torch.bfloat16, device="cuda")
     wide[:total, 1] = p.q.cuda()
-    out = torch.full((total + extra, 2, 2, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+    out = torch.full((total + extra, 2, heads, 64), 7.0, dtype=torch.bfloat16, device="cuda")
     got = p.go(q=wide[:, 1], out=out[:, 1], max_rows=5)
     p.check(got[:total])
     assert (out[total:] == 7).all() and (out[:, 0] == 7).all()
@@ -410,9 +416,10 @@ def test_rows_lie_apart_and_what_is_no_row_stays():
     assert torch.equal(out[:7, 1], got[:7]) and (out[7:, 1] == 7).all()
 
 
-def test_tables_are_held_to_the_buffers():
+@pytest.mark.parametrize("group,capacity", FORMS)
+def test_tables_are_held_to_the_buffers(group, capacity):
     """Tables that say something else than there is: no fault, and what they do not touch stays."""
-    p = Problem("e4m3", 32, 1, 1, [2, 2], [64, 32], [10, 20, 3, 40], [2, 2, 2, 2], False, k_max=8)
+    p = Problem("e4m3", 32, 1, group, [2, 2], [64, 32], [10, 20, 3, 40], [2, 2, 2, 2], False, k_max=8, capacity=capacity)
     want = p.go()
     for first, text in (([-5, 2, 9], [64, 32]), ([0, 2, 4], [10 ** 9, -7]), ([3, 1, 0], [64, 32]), ([4, 4, 4], [64, 32]), ([2 ** 31 - 1] * 3, [64, 32]), ([-2 ** 31] * 3, [64, 32])):
         p.go(seq_start=i32(first), shared_length=i32(text))
