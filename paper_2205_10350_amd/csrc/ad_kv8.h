@@ -86,7 +86,7 @@ void launch_kv8_attend_shared(const Kv8Dims& d, const void* cache, const Kv8Dims
                               int q_heads, const Kv8Rows& r, const Kv8Texts& x, int max_keys, int max_text_keys, float scale, void* ws, hipStream_t s);
 
 // Tokens begin[i] (null: 0; a multiple of 32) .. end[i] - 1 of sequence source[i] become the first ones of sequence place[i], i < n <= 4096, as if all were read before any is
-// written.  What the tables say is held to the caches' sizes and max_tokens; of entries with one place the first counts.
+// written.  What the tables say is held to the caches' sizes and max_tokens (growing: a block that this cuts, but that is complete in the source, is left out); of entries with one place the first counts.
 struct Kv8Moves {
   const int *source, *place, *begin, *end;
   int n, max_tokens;

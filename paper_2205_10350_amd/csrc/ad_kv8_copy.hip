@@ -3,7 +3,8 @@
 // A block's bytes and scales do not depend on where it lies, and copies begin at a block, so they are moved as they are; of a growing cache the incomplete block behind them is
 // moved within the bf16 ring, from the slot that it has in one cache to the one that it has in the other.  All entries of a call are read before any is written: a
 // workgroup takes the same bytes of the same block and head of all entries at once, holds them in registers, waits, and writes them; what one workgroup reads no other
-// writes.  Bound by memory, a byte read and a byte written for a value: 139 MB of 16 sequences, 16 heads, to another cache in 50 to 60 us, 67 MB of 16 sequences of width 128 within one in 28, 4.7 to 5 TB/s;
+// writes.  A growing cache holds a block in bf16 only while it is incomplete there: where the copy has no room for all of the source's tokens and would end inside a block that the source holds in 8 bits
+// alone, it ends with the block before.  Bound by memory, a byte read and a byte written for a value: 139 MB of 16 sequences, 16 heads, to another cache in 50 to 60 us, 67 MB of 16 sequences of width 128 within one in 28, 4.7 to 5 TB/s;
 // three copies of 301 tokens 4.7 us, a launch and two waits for memory.
 #include <hip/hip_runtime.h>
 
@@ -39,7 +40,9 @@ __global__ __launch_bounds__(THREADS) void k_kv8_copy(const unsigned char* origi
     Kv8Move v{0, 0};
     if (from >= 0 && from < df.n_seq && to >= 0 && to < dt.n_seq) {
       v.seqs = from | to << 16;
-      v.count = max(min(min(min(m.end[i], df.capacity) - first(i) * kKv8Block, dt.capacity), m.max_tokens), 0);
+      const int have = min(m.end[i], df.capacity) - first(i) * kKv8Block;
+      v.count = max(min(min(have, dt.capacity), m.max_tokens), 0);
+      if (!dt.closed && v.count / kKv8Block < have / kKv8Block) v.count = v.count / kKv8Block * kKv8Block;
       if (v.count) atomicMin(&taken[to], i);
     }
     moves[i] = v;
