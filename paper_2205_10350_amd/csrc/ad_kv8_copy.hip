@@ -23,6 +23,12 @@ __device__ __forceinline__ uint4 kv8_once(const unsigned char* p) {
   return __builtin_bit_cast(uint4, __builtin_nontemporal_load((const AD_GLOBAL four*)p));
 }
 
+// (first: the source's first block, first * 32 <= from_capacity.  What the source is to have is held to its cache before the first token is taken off: no table overflows a difference.)
+__host__ __device__ int kv8_copied(int first, int end, int from_capacity, int to_capacity, int max_tokens, bool closed) {
+  const int have = std::min(std::max(end, 0), from_capacity) - first * kKv8Block, count = std::max(std::min(std::min(have, to_capacity), max_tokens), 0);
+  return !closed && count / kKv8Block < have / kKv8Block ? count / kKv8Block * kKv8Block : count;
+}
+
 struct Kv8Move { int seqs, count; };   // source | place << 16; tokens (0: nothing)
 
 // blockIdx.x: part of a block, then block, y: head.  2^piece bytes of a block of all entries; behind the blocks of 8 bits the two halves of the ring's.
@@ -40,9 +46,7 @@ __global__ __launch_bounds__(THREADS) void k_kv8_copy(const unsigned char* origi
     Kv8Move v{0, 0};
     if (from >= 0 && from < df.n_seq && to >= 0 && to < dt.n_seq) {
       v.seqs = from | to << 16;
-      const int have = min(m.end[i], df.capacity) - first(i) * kKv8Block;
-      v.count = max(min(min(have, dt.capacity), m.max_tokens), 0);
-      if (!dt.closed && v.count / kKv8Block < have / kKv8Block) v.count = v.count / kKv8Block * kKv8Block;
+      v.count = kv8_copied(first(i), m.end[i], df.capacity, dt.capacity, m.max_tokens, dt.closed);
       if (v.count) atomicMin(&taken[to], i);
     }
     moves[i] = v;

@@ -92,3 +92,16 @@ def test_a_closed_copy_is_cut_anywhere():
         got = make(closed=True, capacity=capacity)
         got.copy(i32([1]), i32([0]), i32([300]), origin=origin, max_tokens=most)
         assert torch.equal(read(got, 0, 0, has), read(origin, 1, 0, has))
+
+
+def test_ends_and_begins_that_are_no_lengths():
+    """Ends far below 0 with begins above it, on both sides of what 32 bits hold: nothing is moved."""
+    kv = tokens(3, 100)
+    origin, cache = make(capacity=100), make(capacity=100)
+    for b in range(2):
+        feed(origin, b, kv, 0, 100)
+        feed(cache, b, kv, 0, 70)
+    before = cache.memory.clone()
+    for end, begin in ((-2 ** 31, 32), (-2 ** 31, 96), (-2 ** 31 + 31, 32), (-2 ** 31 + 95, 2 ** 31 - 1), (-2 ** 31, -2 ** 31), (-1, 64), (0, 32), (31, 32), (32, 32)):
+        cache.copy(i32([0, 1]), i32([1, 0]), i32([end, end]), begin=i32([begin, begin]), origin=origin)
+        assert torch.equal(cache.memory, before), (end, begin)
