@@ -374,7 +374,7 @@ int ad_kv8_attend_shared(const ad_kv8_config* cfg, const void* cache, const ad_k
  * and both grow or both are closed; they may be one (same description, begin = NULL) or must not overlap.  begin: multiples of 32 (NULL: 0).  end[i]: any length that the source may be
  * taken back to; the copy may be taken back to any multiple of 32, or within its last block while that is incomplete.  Blocks are copied as they are held: the copy reads as the source does, bit for bit.  What is outside either
  * cache or beyond max_tokens tokens of an entry is left out, and of a growing cache also the tokens in front of such a cut in a block that ends before end[i] (a block is held in bf16 only while it
- * is incomplete): the copy then ends at a multiple of 32.  Of entries with the same place the first counts. */
+ * is incomplete): the copy then ends at a multiple of 32.  Of entries with the same place the first whose sequences are within the caches counts, whether it has tokens or not. */
 int ad_kv8_copy(const ad_kv8_config* from_cfg, const void* from, const ad_kv8_config* cfg, void* cache, const int32_t* source, const int32_t* place, const int32_t* begin,
                 const int32_t* end, int32_t n, int32_t max_tokens, void* hip_stream);
 

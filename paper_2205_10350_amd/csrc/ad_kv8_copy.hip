@@ -47,7 +47,7 @@ __global__ __launch_bounds__(THREADS) void k_kv8_copy(const unsigned char* origi
     if (from >= 0 && from < df.n_seq && to >= 0 && to < dt.n_seq) {
       v.seqs = from | to << 16;
       v.count = kv8_copied(first(i), m.end[i], df.capacity, dt.capacity, m.max_tokens, dt.closed);
-      if (v.count) atomicMin(&taken[to], i);
+      atomicMin(&taken[to], i);   // (one of no tokens, too)
     }
     moves[i] = v;
   }

@@ -238,7 +238,7 @@ class Kv8Cache:
         """Sequences forked, moved together or taken over from another cache: the first end[i] tokens of sequence source[i] of `origin` (a cache of the same heads and format;
         default: this one) become those of this cache's sequence place[i], as if all were read before any is written.  source, place, end: int32 [n] on the device.  `begin`
         (int32 [n], multiples of 32, from another cache only): tokens begin[i] .. end[i] - 1 become the first ones.  end[i] is any length that the source may be taken back to.  Of
-        entries with one place the first counts; what lies outside the caches is left out.  `max_tokens`: at least the most tokens of an entry (default: the capacity).  A growing cache's
+        entries with one place the first counts (also if it has no tokens); what lies outside the caches is left out.  `max_tokens`: at least the most tokens of an entry (default: the capacity).  A growing cache's
         copy that this or the capacity cuts short inside one of the source's complete blocks ends with the block before."""
         i = self.index
         if origin is not None and (not isinstance(origin, Kv8Cache) or origin.index != i):

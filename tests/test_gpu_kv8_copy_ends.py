@@ -105,3 +105,23 @@ def test_ends_and_begins_that_are_no_lengths():
     for end, begin in ((-2 ** 31, 32), (-2 ** 31, 96), (-2 ** 31 + 31, 32), (-2 ** 31 + 95, 2 ** 31 - 1), (-2 ** 31, -2 ** 31), (-1, 64), (0, 32), (31, 32), (32, 32)):
         cache.copy(i32([0, 1]), i32([1, 0]), i32([end, end]), begin=i32([begin, begin]), origin=origin)
         assert torch.equal(cache.memory, before), (end, begin)
+
+
+def test_of_entries_with_one_place_the_first_counts_without_tokens_too():
+    kv = tokens(4, 100)
+    got, want = (make(6, capacity=100, k_max=100) for _ in range(2))
+    for cache in (got, want):
+        for b, n in enumerate((100, 40, 64)):
+            feed(cache, b, kv, 0, n)
+    got.copy(i32([0, 1, 2, 1]), i32([3, 3, 4, 4]), i32([0, 40, 64, 40]))
+    want.copy(i32([2]), i32([4]), i32([64]))
+    assert torch.equal(got.memory, want.memory)
+    # an entry of a sequence or place that is not there is none
+    got.copy(i32([9, 1, -1, 2]), i32([3, 3, 5, 5]), i32([0, 40, 40, 64]))
+    want.copy(i32([1, 2]), i32([3, 5]), i32([40, 64]))
+    assert torch.equal(got.memory, want.memory)
+    # nor does one that begins behind its end, from another cache, leave its place to the next
+    other = make(6, capacity=100)
+    before = other.memory.clone()
+    other.copy(i32([0, 1]), i32([3, 3]), i32([64, 40]), begin=i32([64, 0]), origin=got)
+    assert torch.equal(other.memory, before)
