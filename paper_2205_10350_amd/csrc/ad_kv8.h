@@ -92,6 +92,7 @@ struct Kv8Moves {
   int n, max_tokens;
 };
 __host__ __device__ int kv8_copied(int first, int end, int from_capacity, int to_capacity, int max_tokens, bool closed);   // tokens that an entry moves from the source's block `first` on
+bool kv8_copy_fits(const Kv8Dims& from, const Kv8Dims& to, int n, int max_tokens);   // its workgroups are fewer than a launch may have
 void launch_kv8_copy(const Kv8Dims& from, const void* origin, const Kv8Dims& to, void* cache, const Kv8Moves& m, hipStream_t s);
 
 }  // namespace ad

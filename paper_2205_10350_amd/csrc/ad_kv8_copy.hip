@@ -104,15 +104,33 @@ __global__ __launch_bounds__(THREADS) void k_kv8_copy(const unsigned char* origi
     if (find_scale(j, sf, st)) gstore(st, y[j]);
 }
 
+// How a copy is launched: blocks of 8 bits that an entry has at most, and the pieces that they are cut into.
+struct Kv8CopyShape {
+  int threads, blocks, piece, parts;   // 2^piece bytes of a block, `parts` of them
+  size_t along;                        // workgroups along x
+};
+static Kv8CopyShape copy_shape(const Kv8Dims& from, const Kv8Dims& to, int n, int max_tokens) {
+  Kv8CopyShape c;
+  const int tokens = std::min({max_tokens, from.capacity, to.capacity});
+  c.blocks = to.closed ? (tokens + kKv8Block - 1) / kKv8Block : tokens / kKv8Block;
+  c.threads = n <= 256 ? 256 : 1024;
+  c.piece = to.width == 32 ? 11 : to.width == 64 ? 12 : 13;   // (a block's bytes are 64 a column)
+  c.parts = 1;
+  while (((size_t)n << c.piece) > (size_t)c.threads * kChunks * 16) { --c.piece; c.parts *= 2; }   // (32 bytes at least: 4096 entries)
+  c.along = (size_t)(c.blocks + (to.closed ? 0 : 2)) * c.parts;
+  return c;
+}
+// (a launch takes less than 2^32 lanes along x)
+bool kv8_copy_fits(const Kv8Dims& from, const Kv8Dims& to, int n, int max_tokens) {
+  const Kv8CopyShape c = copy_shape(from, to, n, max_tokens);
+  return c.along * c.threads < ((size_t)1 << 32);
+}
 void launch_kv8_copy(const Kv8Dims& from, const void* origin, const Kv8Dims& to, void* cache, const Kv8Moves& m, hipStream_t s) {
-  const int tokens = std::min({m.max_tokens, from.capacity, to.capacity}), blocks = to.closed ? (tokens + kKv8Block - 1) / kKv8Block : tokens / kKv8Block;
-  const int threads = m.n <= 256 ? 256 : 1024;
-  int piece = to.width == 32 ? 11 : to.width == 64 ? 12 : 13, parts = 1;   // (a block's bytes are 64 a column)
-  while (((size_t)m.n << piece) > (size_t)threads * kChunks * 16) { --piece; parts *= 2; }   // (32 bytes at least: 4096 entries)
-  const dim3 grid((unsigned)((blocks + (to.closed ? 0 : 2)) * parts), to.heads);
+  const Kv8CopyShape c = copy_shape(from, to, m.n, m.max_tokens);
+  const dim3 grid((unsigned)c.along, to.heads);
   const size_t lds = (size_t)m.n * 8 + (size_t)to.n_seq * 4;
-  if (threads == 256) k_kv8_copy<256><<<grid, 256, lds, s>>>((const unsigned char*)origin, (unsigned char*)cache, m, from, to, blocks, piece, parts);
-  else k_kv8_copy<1024><<<grid, 1024, lds, s>>>((const unsigned char*)origin, (unsigned char*)cache, m, from, to, blocks, piece, parts);
+  if (c.threads == 256) k_kv8_copy<256><<<grid, 256, lds, s>>>((const unsigned char*)origin, (unsigned char*)cache, m, from, to, c.blocks, c.piece, c.parts);
+  else k_kv8_copy<1024><<<grid, 1024, lds, s>>>((const unsigned char*)origin, (unsigned char*)cache, m, from, to, c.blocks, c.piece, c.parts);
 }
 
 }  // namespace ad

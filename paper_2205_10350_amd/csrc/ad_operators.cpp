@@ -161,6 +161,7 @@ int ad_kv8_copy(const ad_kv8_config* from, const void* origin, const ad_kv8_conf
   if (n < 0 || n > c->n_seq || max_tokens < 0) return refuse("ad_kv8_copy: n outside [0, n_seq] or max_tokens < 0");
   if (n == 0 || max_tokens == 0) return AD_OK;
   if (!source || !place || !end) return refuse("ad_kv8_copy: null buffer");
+  if (!kv8_copy_fits(d, t, n, max_tokens)) return refuse("ad_kv8_copy: more workgroups than a launch takes (entries x tokens)");
   launch_kv8_copy(d, origin, t, cache, Kv8Moves{source, place, begin, end, n, max_tokens}, (hipStream_t)hip_stream);
   return launched("ad_kv8_copy");
 }

@@ -31,3 +31,13 @@ def test_what_is_moved_lies_within_both_caches(copied, capacity, closed):
             want -= want % 32
         assert got == want, (first, end, capacity, to, most)
         assert 0 <= got <= min(to, most) and 32 * first + got <= capacity
+
+
+def test_copies_of_more_workgroups_than_a_launch_takes_are_refused():
+    """Some 270 GB of one head that a single call would move; device pointers are made-up addresses that the refused call does not touch."""
+    import paper_2205_10350_amd as ad
+    for width, n, capacity in ((128, 257, 1 << 23), (128, 257, 1 << 22), (32, 257, 1 << 24), (64, 129, 1 << 24), (128, 4096, 1 << 24)):
+        c = ad.AdKv8Config(n, 1, width, capacity, 1, ad.AD_KV_E4M3, 0)
+        at = ctypes.c_void_p(1 << 30)
+        assert ad.lib().ad_kv8_copy(ctypes.byref(c), at, ctypes.byref(c), at, at, at, None, at, n, capacity, None) == ad.AD_EINVAL, (width, n, capacity)
+        assert "workgroups" in (ad.lib().ad_last_error(None) or b"").decode()
