@@ -269,7 +269,7 @@ template <typename T, int THREADS, int KEEP> struct TruncateRow {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const double t = weigh.below(v[h + e]);
-          w[e] = weigh.near(t);   // (meant for those that are not in the last bin)
+          w[e] = weigh.of(t);   // (at temperatures below 56e-30 a bin is wider than T / 28: what lies in the first ones may weigh nothing, too)
           at[e] = weigh.place(v[h + e]);
           tail += (int)(at[e] >= (float)(kBins - 1)) & (int)(t <= Weigh::kNothing);
         }
