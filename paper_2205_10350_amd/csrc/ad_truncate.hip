@@ -4,9 +4,9 @@
 // least number whose weights sum to p of theirs or more (one at least); of them those with w >= min_p.  So what stays is a front of that order: everything before a border
 // (score, index).  The drawn token is the least index whose weights up to it, of what stays, exceed u of all of that.
 //
-// Weights are whole numbers of 2^-S, S = min(51, 62 - the bits of the vocabulary): w is rounded to nearest and to 1 at least (what a double has no number for is 0), and all of a
-// row sum to less than 2^63.  Whole sums are exact, so neither atomics nor the launch's shape change a border or a token, and p Z and u Z are compared exactly.  What rounding moves a border by,
-// 2^-S a token, is some 10^-12 of the sum at most: a drawn number falls there once in 10^8 draws.
+// Weights are whole numbers of 2^-S, S = min(51, 62 - the bits of the vocabulary): w rounded to nearest, so 0 below half of that (such a token stays where no cut takes it, and is never drawn), and all of a
+// row sum to less than 2^63.  Whole sums are exact, so neither atomics nor the launch's shape change a border or a token, and p Z and u Z are compared exactly.  Rounding moves a sum, and so a border, by
+// V 2^-(S + 1) of the largest weight at most for V tokens (3.3e-13 of it more by the exponential): 1.1e-10 for 32,000 tokens, 1.4e-9 for 100,003, 2.4e-7 for 2^20.
 //
 // One workgroup a row, which it keeps in LDS as far as that goes (32,768 fp32 scores, 65,536 bf16).  With top_k the k-th largest of the largest scores of 2048 parts of the row bounds the border from below; else
 // a histogram of all weights in steps of T / 28 below the maximum says which step holds it.  What lies up to there is gathered, in its order, into a list in LDS, where everything else is done: up to
@@ -122,8 +122,7 @@ struct Weigh {
   const double* table;  // kPowers
   // 128 times the power of two that a score's weight lies below the maximum's 1 (the difference is exact; at temperatures near 0 a difference of rounded products would not do)
   __device__ __forceinline__ double below(float v) const { return ((double)m - (double)v) * rate; }
-  static constexpr double kNothing = 1074.0 * 128;   // what lies further below has no double
-  // The weight 2^(S - t / 128), 0 <= t <= 12800, in whole numbers, 1 at least: 2^(-f / 128), 0 <= f < 1, by a polynomial (1 at 0 and off by 3.3e-13 at most: least maximum error), the other 127 parts by
+  // The weight 2^(S - t / 128), 0 <= t <= 12800, in whole numbers: 2^(-f / 128), 0 <= f < 1, by a polynomial (1 at 0 and off by 3.3e-13 at most: least maximum error), the other 127 parts by
   // a table, the whole part straight into the exponent, and the product rounded to a whole number as it is added to 2^52.
   __device__ __forceinline__ u64 near(double t) const {
     const int n = (int)t;
@@ -134,11 +133,10 @@ struct Weigh {
     p = fma(p, f, 1.0);
     const long long b = __builtin_bit_cast(long long, table[n & 127]);
     const unsigned hi = (unsigned)(b >> 32) + ((unsigned)(bits - (n >> 7)) << 20);
-    const u64 w = __builtin_bit_cast(u64, fma(p, __builtin_bit_cast(double, (long long)((u64)hi << 32 | (unsigned)b)), 4503599627370496.0)) & 0xfffffffffffffull;   // (<= 2^51)
-    return w | (u64)(w == 0);
+    return __builtin_bit_cast(u64, fma(p, __builtin_bit_cast(double, (long long)((u64)hi << 32 | (unsigned)b)), 4503599627370496.0)) & 0xfffffffffffffull;   // (<= 2^51)
   }
-  __device__ __forceinline__ u64 of(double t) const { return t > kNothing ? 0 : near(fmin(t, 12800.0)); }
-  // The histogram's bin: 28 to a T, so that what falls into the last one lies 36.5 T or more below the maximum and weighs 1 or nothing.
+  __device__ __forceinline__ u64 of(double t) const { return near(fmin(t, 12800.0)); }   // (2^-100 of the largest is nothing)
+  // The histogram's bin: 28 to a T, so that what falls into the last one lies 36.5 T or more below the maximum and weighs nothing (half of 2^-51 is 36.04 T below it).
   // (by halves: the difference itself may be beyond fp32)
   __device__ __forceinline__ float place(float v) const { return fmaf(v, -0.5f, half) * step; }
   __device__ __forceinline__ int bin(float v) const { return (int)fminf(place(v), (float)(kBins - 1)); }
@@ -257,9 +255,8 @@ template <typename T, int THREADS, int KEEP> struct TruncateRow {
       for (int e = 0; e < kVec; ++e) f(v[e], index(c) + e);
     });
   }
-  // Weights of all, bin by bin; their sum goes with them.  What is in the last bin weighs 1 (or nothing) and is counted apart.
+  // Weights of all, bin by bin.  What would go into the last bin weighs nothing.
   template <typename S> __device__ __forceinline__ void weigh_all(S& s, const Weigh& weigh) const {
-    unsigned tail = 0;
     // (weights of four scores at once, without a branch: a score's is a chain of ten steps in 64 bits)
     vectors([&](int, const float (&v)[kVec]) {
 #pragma unroll
@@ -268,17 +265,14 @@ template <typename T, int THREADS, int KEEP> struct TruncateRow {
         float at[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const double t = weigh.below(v[h + e]);
-          w[e] = weigh.of(t);   // (at temperatures below 56e-30 a bin is wider than T / 28: what lies in the first ones may weigh nothing, too)
+          w[e] = weigh.of(weigh.below(v[h + e]));   // (at temperatures below 56e-30 a bin is wider than T / 28: what lies in the first ones may weigh nothing, too)
           at[e] = weigh.place(v[h + e]);
-          tail += (int)(at[e] >= (float)(kBins - 1)) & (int)(t <= Weigh::kNothing);
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e)
           if (at[e] < (float)(kBins - 1)) atomicAdd(&s.hist[(int)at[e]], w[e]);
       }
     });
-    if (tail) atomicAdd(&s.hist[kBins - 1], (u64)tail);
   }
   // Those with pred(score) into the list, in their order, if they go there; how many there are.  may(score) of the largest of every eighth vector: whether one of these may have one.
   template <typename S, typename M, typename P> __device__ __forceinline__ int gather(S& s, const float (&most)[8], const M& may, const P& pred) const {

@@ -1,4 +1,4 @@
-"""Truncated distributions where a row's many small weights matter: temperatures far below the scores' differences."""
+"""Truncated distributions where a row's many small weights matter: temperatures far below the scores' differences, long tails of large vocabularies."""
 import numpy as np
 import pytest
 
@@ -15,7 +15,7 @@ def f32(x):
     return torch.tensor(np.asarray(x, np.float32), device="cuda")
 
 
-def check(x, u, rows):
+def check(x, u, rows, tolerance=log_prob_tolerance):
     """Tokens, logarithms of their probabilities and truncated scores of x [rows, vocab]; rows: each row's (T, k, p, q)."""
     cut = dict(zip(("temperature", "top_k", "top_p", "min_p"), (f32([r[0] for r in rows]), torch.tensor([r[1] for r in rows], dtype=torch.int32, device="cuda"), f32([r[2] for r in rows]),
                                                                 f32([r[3] for r in rows]))))
@@ -26,7 +26,7 @@ def check(x, u, rows):
         setting = float(np.float32(t)), k, float(np.float32(p)), float(np.float32(q))
         want, lp = sample(xs[r], float(np.float32(u[r])), *setting)
         assert int(tokens[r]) == want, (r, setting, int(tokens[r]), want)
-        assert abs(float(log_probs[r]) - lp) <= log_prob_tolerance(lp, x.shape[1]), (r, setting, float(log_probs[r]), lp)
+        assert abs(float(log_probs[r]) - lp) <= tolerance(lp, x.shape[1]), (r, setting, float(log_probs[r]), lp)
         stay = kept(xs[r], *setting)
         assert np.array_equal(scores[r], np.where(stay, xs[r], -INF)), (r, setting, int((scores[r] > -INF).sum()), int(stay.sum()))
 
@@ -45,3 +45,19 @@ def test_temperatures_far_below_the_scores(vocab, near):
             rows.append((t, 0, p, 0.0))
         rows[-2] = (t, 40, 0.9, 0.0)
     check(f32(np.stack(x)), rng.random(len(rows)).astype(np.float32), rows)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("vocab,u", [(32000, 1e-10), (100003, 1e-9), (300007, 1e-8), (1 << 20, 1e-7)])
+def test_a_tail_has_the_share_that_its_weights_have(vocab, u, bf16):
+    """One token far above all others, which together weigh less than 1e-11 of it: u and top_p next to their ends find that token, wherever it stands; top_k and min_p as ever."""
+    rng = np.random.default_rng(vocab)
+    rows = [(1.0, 0, 1.0, 0.0), (1.0, 0, 1 - 2.0 ** -24, 0.0), (0.25, 0, 1.0, 0.0), (0.25, 0, 1 - 2.0 ** -24, 0.0), (1.0, 1000, 1 - 2.0 ** -24, 0.0), (1.0, 1000, 1.0, 0.0), (1.0, 0, 1.0, 1e-30),
+            (1.0, 0, 0.5, 0.0)]
+    x = -(40 + 60 * rng.random((len(rows), vocab)))
+    x[2:4] *= 0.25
+    for r in range(len(rows)):
+        x[r, vocab - 1 if r % 2 == 0 else vocab // 2] = 0.0
+    x = torch.tensor(x, dtype=torch.float32)
+    # the result's rounding and the 64-bit steps: here no weight that counts is near half a unit, and those that do not sum to less than 2^-40
+    check((x.to(torch.bfloat16) if bf16 else x).cuda(), [u] * len(rows), rows, lambda value, vocab: 2.0 ** -24 * abs(value) + 2.0 ** -39)
