@@ -411,8 +411,9 @@ int ad_accept_sampled(const void* logits, int32_t dtype, int64_t logits_stride, 
  *   top_p        p; 1 or more: all, 0 or less: one (NULL: all)
  *   min_p        q; 0 or less: all, more than 1 as 1 (NULL: all)
  * row_start DEVICE [n_seq + 1]: the packed rows of each sequence, n_seq <= 4096; rows of no sequence are left as they were.  NULL: row b is sequence b, n_seq = rows.
- * logits as ad_accept_sampled's, rows < 2^22.  Weights are whole numbers of 2^-S of the largest (S = min(51, 62 - bits of vocab)), rounded to nearest, whose sums are exact: a row's
- * result depends on its scores and settings alone.  A token of less than half of 2^-S weighs nothing: it stays unless a cut takes it, and is never drawn.  A row without a distribution (no finite score, a NaN or +inf among them, T not a positive number, p or q NaN) gives AD_NEVER, or -inf throughout.
+ * logits as ad_accept_sampled's, vocab <= 2^20, rows < 2^22.  Weights are whole numbers of 2^-S of the largest (S = min(51, 64 - bits of vocab)), rounded to nearest, whose sums are exact:
+ * a row's result depends on its scores and settings alone.  Rounding moves a sum by vocab 2^-(S + 1) of the largest weight at most: 2.8e-11 at 32,000, 2^-24 (half a step of u and p below 1) at 2^20.  A token of less than half of 2^-S weighs nothing: it stays unless a cut takes it, and is never drawn.
+ * A row without a distribution (no finite score, a NaN or +inf among them, T not a positive number, p or q NaN) gives AD_NEVER, or -inf throughout.
  * The calls enqueue one kernel on `hip_stream` of the current device, need no workspace and may be captured into graphs.
  *
  * ad_sample_tokens draws: the least token t whose weights, summed over the tokens up to it that stay, exceed u times those of all that stay.

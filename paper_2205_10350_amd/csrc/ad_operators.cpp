@@ -207,7 +207,7 @@ static int truncate_common(const char* what, const void* logits, int32_t dtype, 
     return refuse(msg);
   };
   if (dtype != AD_F32 && dtype != AD_BF16) return no("dtype must be AD_F32 or AD_BF16");
-  if (vocab < 1 || vocab > (1 << 24)) return no("vocab outside [1, 2^24]");
+  if (vocab < 1 || vocab > (1 << 20)) return no("vocab outside [1, 2^20]");   // (beyond it the weights' rounding could be seen in fp32 settings)
   if (rows < 0 || rows >= (1 << 22)) return no("rows outside [0, 2^22)");
   if (row_start ? n_seq < 1 || n_seq > 4096 : n_seq != rows) return no("n_seq outside [1, 4096], or without row_start not the rows");
   if (rows == 0) return AD_OK;

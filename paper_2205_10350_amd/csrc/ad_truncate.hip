@@ -4,9 +4,10 @@
 // least number whose weights sum to p of theirs or more (one at least); of them those with w >= min_p.  So what stays is a front of that order: everything before a border
 // (score, index).  The drawn token is the least index whose weights up to it, of what stays, exceed u of all of that.
 //
-// Weights are whole numbers of 2^-S, S = min(51, 62 - the bits of the vocabulary): w rounded to nearest, so 0 below half of that (such a token stays where no cut takes it, and is never drawn), and all of a
-// row sum to less than 2^63.  Whole sums are exact, so neither atomics nor the launch's shape change a border or a token, and p Z and u Z are compared exactly.  Rounding moves a sum, and so a border, by
-// V 2^-(S + 1) of the largest weight at most for V tokens (3.3e-13 of it more by the exponential): 1.1e-10 for 32,000 tokens, 1.4e-9 for 100,003, 2.4e-7 for 2^20.
+// Weights are whole numbers of 2^-S, S = min(51, 64 - the bits of the vocabulary): w rounded to nearest, so 0 below half of that (such a token stays where no cut takes it, and is never drawn), and all of a
+// row sum to less than 2^64.  Whole sums are exact, so neither atomics nor the launch's shape change a border or a token, and p Z and u Z are compared exactly.  Rounding moves a sum, and so a border, by
+// V 2^-(S + 1) of the largest weight at most for V tokens (3.3e-13 of it more by the exponential): 2.8e-11 for 32,000 tokens, 3.6e-10 for 100,003,
+// and for 2^20, the most that are accepted, 2^-24, half a step of the fp32 numbers p and u below 1.
 //
 // One workgroup a row, which it keeps in LDS as far as that goes (32,768 fp32 scores, 65,536 bf16).  With top_k the k-th largest of the largest scores of 2048 parts of the row bounds the border from below; else
 // a histogram of all weights in steps of T / 28 below the maximum says which step holds it.  What lies up to there is gathered, in its order, into a list in LDS, where everything else is done: up to
@@ -62,7 +63,7 @@ __device__ __forceinline__ unsigned __int128 part_of(float f, u64 z, int& shift)
   int e;
   const unsigned m = (unsigned)(frexpf(f, &e) * 16777216.f);
   shift = 24 - e;
-  return (unsigned __int128)m * z;   // < 2^87
+  return (unsigned __int128)m * z;   // < 2^88
 }
 __device__ __forceinline__ u64 floor_part(float f, u64 z) {
   int s;
@@ -703,7 +704,7 @@ __global__ __launch_bounds__(THREADS) void k_truncate(TruncateArgs a) {
   bad = __any(s.lo[lane % kWaves] != 0.f);
   bad = bad || m == -INFINITY;   // no distribution
   m = alike(m);
-  Weigh weigh{m, 0.5f * m, fminf((float)(rate * (56 * 0.69314718055994530942 / 128)), 1e30f), rate, INFINITY, min(51, 62 - (32 - __clz(a.vocab))), s.table};
+  Weigh weigh{m, 0.5f * m, fminf((float)(rate * (56 * 0.69314718055994530942 / 128)), 1e30f), rate, INFINITY, min(51, 64 - (32 - __clz(a.vocab))), s.table};
   if (min_p > 0.f) weigh.most = -128.0 * log2((double)fminf(min_p, 1.f));
   Border border{bad ? INFINITY : -INFINITY, -1};
   constexpr int kMost = EACH * THREADS;

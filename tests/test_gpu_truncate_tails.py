@@ -61,3 +61,34 @@ def test_a_tail_has_the_share_that_its_weights_have(vocab, u, bf16):
     x = torch.tensor(x, dtype=torch.float32)
     # the result's rounding and the 64-bit steps: here no weight that counts is near half a unit, and those that do not sum to less than 2^-40
     check((x.to(torch.bfloat16) if bf16 else x).cuda(), [u] * len(rows), rows, lambda value, vocab: 2.0 ** -24 * abs(value) + 2.0 ** -39)
+
+
+@pytest.mark.parametrize("vocab", [32000, 300007, (1 << 20) - 1, 1 << 20])
+def test_the_rounding_of_many_small_weights_is_bounded(vocab):
+    """Tails whose weights all lie next to half of a power of two, where rounding takes or adds the most: the drawn token and the front that stays are those of a sum that is off by
+    vocab 2^-(S + 1) of the largest weight at most, S = min(51, 64 - bits of vocab) (and 2^-40 for the exponentials)."""
+    bound = vocab * 2.0 ** -(min(51, 64 - vocab.bit_length()) + 1) + 2.0 ** -40
+    rng = np.random.default_rng(vocab)
+    x, u, p = [], [], []
+    for bits in range(34, 54):
+        for factor in (0.49, 0.51, 0.745):
+            row = np.full(vocab, np.log(factor) - bits * np.log(2.0))
+            row[rng.integers(vocab)] = 0.0
+            x.append(row)
+            mass = vocab * factor * 2.0 ** -bits
+            mass /= 1 + mass
+            u.append(rng.choice([mass * rng.random(), rng.random(), 1 - 2.0 ** -24, 2.0 ** -24]))
+            p.append(rng.choice([1 - mass * rng.random(), 1 - 2.0 ** -24, 0.5]))
+    for lo in range(0, len(x), 20):
+        at, uu, pp = f32(np.stack(x[lo:lo + 20])), np.float32(u[lo:lo + 20]), np.minimum(np.float32(p[lo:lo + 20]), np.float32(1 - 2.0 ** -24))
+        tokens, scores = ad.sample_tokens(at, f32(uu)).cpu().numpy(), ad.truncate_scores(at, top_p=f32(pp)).cpu().numpy()
+        w = np.exp(at.double().cpu().numpy()).astype(np.longdouble)      # (a million additions to 1 would lose the smallest in 64 bits)
+        for r in range(len(at)):
+            sums = np.cumsum(w[r])
+            assert (sums[tokens[r]] - w[r, tokens[r]]) - bound <= float(uu[r]) * sums[-1] <= sums[tokens[r]] + bound, (lo + r, uu[r], tokens[r])
+            stay = scores[r] > -INF
+            kept_sum = np.sort(w[r, stay])[::-1].cumsum()
+            least = w[r, stay].min() if stay.sum() > 1 else w[r, stay][0]
+            assert kept_sum[-1] >= float(pp[r]) * sums[-1] - bound and kept_sum[-1] - least <= float(pp[r]) * sums[-1] + bound, (lo + r, pp[r], int(stay.sum()))
+            border = np.flatnonzero(stay & (w[r] < 1))                # (equal scores: the lower indices)
+            assert len(border) == 0 or np.array_equal(border, np.flatnonzero(w[r] < 1)[:len(border)])

@@ -106,3 +106,11 @@ def test_plain_forms():
     assert sample(x, 0.5, k=2) == (1, pytest.approx(math.log(4 / 7))) and sample(x, 0.6, k=2)[0] == 3
     assert sample([math.nan, 1.0], 0.5)[0] == sample([-math.inf] * 2, 0.5)[0] == sample([1.0, 2.0], 0.5, temperature=0.0)[0] == sample([1.0, 2.0], 0.5, p=math.nan)[0] == -1
     assert log_prob_tolerance(-1.0, 32000) < 1e-6
+
+
+def test_vocabularies_whose_weights_would_be_too_coarse_are_refused():
+    """Weights are 64-bit whole numbers whose sum must fit, too: past 2^20 tokens their rounding could move a sum by more than half a step of an fp32 number below 1."""
+    for vocab in ((1 << 20) + 1, 1 << 21, 1 << 24):
+        assert ad.lib().ad_sample_tokens(P, ad.AD_F32, vocab, vocab, None, None, None, None, None, 8, P, 8, P, None, None) == ad.AD_EINVAL and "2^20" in message()
+        assert ad.lib().ad_truncate_scores(P, ad.AD_BF16, vocab, vocab, None, None, None, None, None, 8, 8, FAR, vocab, None) == ad.AD_EINVAL and "2^20" in message()
+    assert ad.lib().ad_sample_tokens(P, ad.AD_F32, 1 << 20, 1 << 20, None, None, None, None, None, 0, P, 0, P, None, None) == ad.AD_OK     # (no rows)
