@@ -36,9 +36,8 @@ __device__ __forceinline__ int shared_row(const Kv8Rows& t, const Kv8Texts& x, i
 __device__ __forceinline__ Kv8Seq shared_seq(const Kv8Rows& t, const Kv8Texts& x, int g, const Kv8Dims& d) {
   Kv8Seq s;
   s.row0 = shared_row(t, x, g);
-  s.n = shared_row(t, x, g + 1) - s.row0;
-  if (s.row0 < 0 || s.row0 > t.rows) s.n = 0;
-  s.n = min(min(s.n, x.max_rows), t.rows - s.row0);
+  s.n = kv8_held(s.row0, (long long)shared_row(t, x, g + 1) - s.row0, t.rows, x.max_rows);
+  s.row0 = min(max(s.row0, 0), t.rows);   // (rows are told from a text's by differences)
   s.base = min(max(x.length[g], 0), d.capacity);
   if (!d.closed) s.base = s.base / kKv8Block * kKv8Block;   // (whole blocks, those in 8 bits)
   return s;
@@ -300,7 +299,7 @@ __global__ __launch_bounds__(256, kv8_waves(DH, 1)) void k_kv8_attend_short(cons
   if (g >= 0 && b < sh.texts.seq_start[g + 1]) {
     const Kv8Seq t = shared_seq(a.rows, sh.texts, g, ds);
     text.base = min(t.base, sh.split_blocks * kKv8Block);
-    sq.n = sq.row0 < t.row0 ? 0 : min(sq.n, t.row0 + t.n - sq.row0);   // (beyond the bound on a text's rows: left as they were)
+    sq.n = sq.row0 < t.row0 ? 0 : max(min(sq.n, t.row0 + t.n - sq.row0), 0);   // (beyond the bound on a text's rows: left as they were)
   }
   const int m_rows = sq.n * a.group, row0 = tile * 16;
   if (row0 >= m_rows) return;
