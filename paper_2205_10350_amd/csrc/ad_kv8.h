@@ -52,12 +52,16 @@ struct Kv8Rows {
   const int *start, *count, *base;
   int stride, rows, max_rows, n_seq;
 };
-// the rows of a sequence whose table says n from packed row row0 on: 0 or more, whatever it says (times the query heads that share a head a number below 0 could become one above it)
-constexpr int kv8_held(int row0, long long n, int rows, int max_rows) {
-  return row0 < 0 || row0 > rows || n <= 0 ? 0 : (int)std::min(n, (long long)std::min(max_rows, rows - row0));
+// How long a range is that a table says (below 0: of one that 32 bits do not hold, which begins below 0), and the rows of a sequence of n from packed row row0 on: 0 or more, whatever the table says (times the
+// query heads that share a head a number below 0 could become one above it).
+constexpr int kv8_range(int from, int to) { return (int)((unsigned)std::max(from, to) - (unsigned)from); }
+constexpr int kv8_held(int row0, int n, int rows, int max_rows) {
+  if (row0 < 0 || row0 > rows) n = 0;
+  return std::max(std::min(std::min(n, max_rows), (int)((unsigned)rows - (unsigned)row0)), 0);
 }
-static_assert(kv8_held(INT_MIN, 1ll << 32, 8, 8) == 0 && kv8_held(-1, INT_MIN, 8, 8) == 0 && kv8_held(INT_MAX, -(1ll << 32), 8, 8) == 0 && kv8_held(3, (long long)INT_MIN - 3, 8, 8) == 0 &&
-              kv8_held(9, 1, 8, 8) == 0 && kv8_held(8, 1, 8, 8) == 0 && kv8_held(3, INT_MAX, 8, 8) == 5 && kv8_held(3, INT_MAX, 8, 2) == 2 && kv8_held(0, 8, 8, 8) == 8);
+static_assert(kv8_held(INT_MIN, kv8_range(INT_MIN, INT_MAX), 8, 8) == 0 && kv8_held(-1, kv8_range(-1, INT_MIN), 8, 8) == 0 && kv8_held(INT_MAX, kv8_range(INT_MAX, INT_MIN), 8, 8) == 0 &&
+              kv8_held(3, kv8_range(3, INT_MIN), 8, 8) == 0 && kv8_held(9, 1, 8, 8) == 0 && kv8_held(8, 1, 8, 8) == 0 && kv8_held(3, kv8_range(3, INT_MAX), 8, 8) == 5 &&
+              kv8_held(3, INT_MAX, 8, 2) == 2 && kv8_held(0, 8, 8, 8) == 8 && kv8_held(3, INT_MIN, 8, 8) == 0);
 // How a launch deals out a sequence's pieces of 2^shift / mul rows: as many to every sequence as max_rows have, or, where most of those would not be there, packed:
 // sequence b's begin at (start[b] mul >> shift) + extra b, and each workgroup looks its sequence up.  (256 sequences of 25 rows over closed caches of 400 tokens, us without a bound:
 // by sequence 653, packed 57, with max_rows = 25 and by sequence 50.)

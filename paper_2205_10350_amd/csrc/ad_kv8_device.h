@@ -13,10 +13,11 @@ __device__ __forceinline__ Kv8Seq kv8_seq(const Kv8Rows& t, int b, int capacity,
   const size_t at = (size_t)b * t.stride;
   Kv8Seq s;
   s.row0 = t.start[at];
-  s.n = kv8_held(s.row0, t.count ? t.count[at] : (long long)t.start[at + t.stride] - s.row0, t.rows, t.max_rows);
+  s.n = t.count ? t.count[at] : kv8_range(s.row0, t.start[at + t.stride]);
   s.base = t.base ? t.base[at] : 0;
   if (s.base < 0) s.n = 0;
   s.base = min(max(s.base, 0), capacity);
+  s.n = kv8_held(s.row0, s.n, t.rows, t.max_rows);
   if (placed) s.n = min(s.n, capacity - s.base);
   return s;
 }

@@ -36,7 +36,7 @@ __device__ __forceinline__ int shared_row(const Kv8Rows& t, const Kv8Texts& x, i
 __device__ __forceinline__ Kv8Seq shared_seq(const Kv8Rows& t, const Kv8Texts& x, int g, const Kv8Dims& d) {
   Kv8Seq s;
   s.row0 = shared_row(t, x, g);
-  s.n = kv8_held(s.row0, (long long)shared_row(t, x, g + 1) - s.row0, t.rows, x.max_rows);
+  s.n = kv8_held(s.row0, kv8_range(s.row0, shared_row(t, x, g + 1)), t.rows, x.max_rows);
   s.row0 = min(max(s.row0, 0), t.rows);   // (rows are told from a text's by differences)
   s.base = min(max(x.length[g], 0), d.capacity);
   if (!d.closed) s.base = s.base / kKv8Block * kKv8Block;   // (whole blocks, those in 8 bits)
