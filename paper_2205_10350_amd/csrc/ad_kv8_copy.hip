@@ -5,7 +5,7 @@
 // workgroup takes the same bytes of the same block and head of all entries at once, holds them in registers, waits, and writes them; what one workgroup reads no other
 // writes.  A growing cache holds a block in bf16 only while it is incomplete there: where the copy has no room for all of the source's tokens and would end inside a block that the source holds in 8 bits
 // alone, it ends with the block before.  Bound by memory, a byte read and a byte written for a value: 139 MB of 16 sequences, 16 heads, to another cache in 50 to 60 us, 67 MB of 16 sequences of width 128 within one in 28, 4.7 to 5 TB/s;
-// three copies of 301 tokens 4.7 us, a launch and two waits for memory.
+// three copies of 301 tokens 5.0 us, a launch and two waits for memory.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

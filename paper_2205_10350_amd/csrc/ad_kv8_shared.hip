@@ -340,6 +340,7 @@ __global__ __launch_bounds__(256) void k_kv8_join_shared(Kv8Attend a, Kv8Deal on
 
 // What goes by the caches' sizes and the query heads alone, so that a row's sums do not depend on a call: whether a workgroup takes 128 rows of a text, and the keys of a split of it.
 static size_t text_fan(const Kv8Dims& d, const Kv8Dims& texts, int group) { return (size_t)((d.n_seq + texts.n_seq - 1) / texts.n_seq) * group; }
+// (32 from the table above, in e4m3; i8, whose bytes cost more to unpack, was measured beyond it alone, 32 x 8.)
 static bool text_many(const Kv8Dims& d, const Kv8Dims& texts, int group) { return text_fan(d, texts, group) >= 32; }
 // (us by keys of a split, 512, 1024, 2048, 4096: workgroups of 32 rows, 40 continuations of 13 rows of 4 texts of 2000 to 8000 tokens in i8 61, 54, 50, 54; of 128, 96 continuations of 8 rows of a text
 // of 8192 69, 60, 69, -, 64 of 4 query heads of 2 texts of 16,000 to 32,000 72, 62, 67, -)
@@ -352,7 +353,8 @@ static int text_split_keys(const Kv8Dims& d, const Kv8Dims& texts, int group) {
 }
 // Short texts and few continuations: each continuation's workgroups read the text for themselves.  (Four texts, 16 heads of width 64, continuations with up to 300 tokens, us a replay in one launch / in two, by
 // continuations of a text, rows and tokens of a text: 2 x 1, 512 6.9 / 9.5, 1024 8.4 / 9.5, 2048 11.2 / 10.6; 8 x 1, 512 8.5 / 10.6, 1024 11.6 / 11.5; 8 x 8, 1024 12.2 / 14.9; 16 x 1, 512 11.9 / 13.7, 1024
-// 16.5 / 14.9; 16 x 8, 1024 17.3 / 23.4; 31 x 1, 512 19.6 / 19.8; 31 x 8, 512 20.0 / 32.7; 64 x 1, 512 33.7 / 27.2.)
+// 16.5 / 14.9; 16 x 8, 1024 17.3 / 23.4; 31 x 1, 512 19.6 / 19.8; 31 x 8, 512 20.0 / 32.7; 64 x 1, 512 33.7 / 27.2.
+// A continuation's rows in a call may not decide, so that a row's sums do not depend on it: 16 x 1 and 8 x 1 over 1024 tokens lose 1.6 and 0.1 us for the 6.1 that 16 x 8 gains.)
 static bool text_short(const Kv8Dims& d, const Kv8Dims& texts, int group) {
   return !text_many(d, texts, group) && texts.capacity <= 1024 && text_fan(d, texts, group) * texts.capacity <= 16384 && kv8_split_keys(d) >= d.capacity;
 }

@@ -14,10 +14,10 @@
 // 256 scores are ranked by comparing each with each; of more the step that holds the border is cut into equal parts of the floating point numbers between its least and its largest until 256 are left, or all are
 // equal and their indices decide.  Where the list has no room (2048) it takes the border's step alone, and the token is looked for over the row.
 //
-// What bounds it: a row of 32,000 scores with top_k 50 and top_p takes 12 us, 2 of them to read it and the rest eight steps of 0.5 to 2 us between barriers of 16 waves; with top_p alone 18.3 us, 8 of them the
-// histogram, 33 instructions a score, 9 of them in 64 bits, at 60 % of what one compute unit can issue.  32 rows 12.8 us; 416 rows of blocks truncated 48.9, where two turns of 256 rows overlap little (53 MB read and
-// written, 20 us at a copy's rate); 256 rows of 100,003 scores, settings of each row's own, 106 us: the slowest rows', where thousands of tokens stay and weights are taken twice (the others take 25; 102 MB).
-// (us, 32,000 scores top_p / 256 x 100,003 / 416 rows truncated; workgroups of 512 threads, 6 vectors of a lane in LDS, 25.6 / 138 / 59; of 256 39 / 344 / 121; of 1024, as here, 21.4 / 107 / 53.  Weights of the
+// What bounds it: a row of 32,000 scores with top_k 50 and top_p takes 12 us, 2 of them to read it and the rest eight steps of 0.5 to 2 us between barriers of 16 waves; with top_p alone 16.0 us, 6.0 of them the
+// histogram, 28 instructions a score, 10 of them in 64 bits, on one compute unit.  32 rows 12.9 us; 416 rows of blocks truncated 47.8, where two turns of 256 rows overlap little (53 MB read and
+// written, 20 us at a copy's rate); 256 rows of 100,003 scores, settings of each row's own, 98.5 us: the slowest rows', where thousands of tokens stay and weights are taken twice (the others take 25; 102 MB).
+// (Steps on the way, us, 32,000 scores top_p / 256 x 100,003 / 416 rows truncated; workgroups of 512 threads, 6 vectors of a lane in LDS, 25.6 / 138 / 59; of 256 39 / 344 / 121; of 1024, as here, 21.4 / 107 / 53.  Weights of the
 // histogram in 32 bits first, and in 64 where a border lies near: 19.3 / 129 / 57 where these were 19.8 / 103 / 49.)
 #include <hip/hip_runtime.h>
 #include <limits.h>
@@ -168,7 +168,7 @@ template <int THREADS, int EACH> struct TruncateShared {
 };
 
 // A row's scores, 16 bytes at a time from the 16-byte boundary at or before the first: wave w of a workgroup has pieces (w per .. (w + 1) per - 1) of 64 vectors, a lane one of each.  The
-// first KEEP of a lane stay in LDS (where each lane reads only what it wrote).
+// first KEEP of a lane stay in LDS, where each lane reads what it wrote; in find, behind barriers, all waves read what one of them wrote.
 template <typename T, int THREADS, int KEEP> struct TruncateRow {
   static constexpr int kVec = 16 / (int)sizeof(T);
   const T* x;
@@ -258,7 +258,7 @@ template <typename T, int THREADS, int KEEP> struct TruncateRow {
   }
   // Weights of all, bin by bin.  What would go into the last bin weighs nothing.
   template <typename S> __device__ __forceinline__ void weigh_all(S& s, const Weigh& weigh) const {
-    // (weights of four scores at once, without a branch: a score's is a chain of ten steps in 64 bits)
+    // (a score's weight is a chain of ten steps in 64 bits: the table's numbers of four are looked up together)
     vectors([&](int, const float (&v)[kVec]) {
 #pragma unroll
       for (int h = 0; h < kVec; h += 4) {

@@ -318,7 +318,7 @@ def sample_tokens(logits, u, temperature=None, top_k=None, top_p=None, min_p=Non
     """Tokens drawn from truncated distributions by given random numbers (include/ad.h, "truncated distributions"): tokens [rows] int32, with log_probs=True also the
     logarithms of their probabilities [rows] fp32.
 
-    logits [rows, vocab] fp32 or bf16 (rows may lie apart), u [rows] fp32 uniform in [0, 1).  temperature fp32, top_k int32, top_p fp32, min_p fp32: None or a tensor on the
+    logits [rows, vocab] fp32 or bf16 (rows may lie apart; a vocabulary of up to 2^20), u [rows] fp32 uniform in [0, 1).  temperature fp32, top_k int32, top_p fp32, min_p fp32: None or a tensor on the
     device with a setting for each row, or with row_start [n_seq + 1] int32 for each sequence, whose rows are row_start[b] .. row_start[b + 1] - 1."""
     import torch
     args, i, rows = _cut(logits, temperature, top_k, top_p, min_p, row_start)

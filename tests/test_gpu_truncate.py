@@ -1,5 +1,6 @@
 """Tokens drawn from truncated distributions and truncated scores through the public entry points, against the plain 64-bit form.  Tokens and what stays are whole
-numbers and truth values: they have to be equal (a drawn number or a sum within 1e-11 of a border, where 64 bits may fall either way, does not occur in these draws)."""
+numbers and truth values: they have to be equal (a drawn number or a sum within vocab 2^-(S + 1) of a border, S = min(51, 64 - bits of vocab), where weights in whole numbers may fall on the other side,
+does not occur in these draws: 3e-11 of the largest weight at 32,000 scores, 4e-9 at 300,007)."""
 import itertools
 import math
 

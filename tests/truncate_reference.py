@@ -45,6 +45,7 @@ def sample(x, u, temperature=1.0, k=0, p=1.0, q=0.0):
 
 
 def log_prob_tolerance(value, vocab):
-    """The fp32 result's rounding, 2^-24 of it; weights are whole numbers of 2^-S of the largest, S = min(51, 62 - bits of vocab), each off by one at most, which beside a sum of
-    1 or more moves its logarithm by vocab 2^-S; the rest (64-bit exponentials to 7e-15, a logarithm, three additions of numbers below 2^11) is below 2^-40."""
+    """The fp32 result's rounding, 2^-24 of it; weights are whole numbers of 2^-S of the largest, S = min(51, 64 - bits of vocab), each off by half at most, which beside a sum of
+    1 or more moves its logarithm by vocab 2^-(S + 1): an eighth of the second number here (up to 2^13 scores: half of it at most); the rest (exponentials to 3.3e-13, a logarithm, three additions of numbers below 2^6,
+    as a drawn token weighs a unit or more) is below 2^-41, half of the third."""
     return 2.0 ** -24 * abs(value) + vocab * 2.0 ** -min(51, 62 - vocab.bit_length()) + 2.0 ** -40
